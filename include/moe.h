@@ -269,6 +269,111 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
                              void* x1_out, void* moe_in_out, float* logits_out,
                              void* ws, size_t ws_bytes, void* stream);
 
+/* ---- several new tokens per sequence: rotary positions, a quantised key/value cache, attention for drafted tokens ----
+ *
+ * A step that verifies drafted tokens (or takes a chunk of a prompt) has n_draft rows per sequence instead of one: row
+ * b * n_draft + i is token i of sequence b.  Its calls, in the order of a step:
+ *   moe_rope             query and key heads of the projection's rows, in place
+ *   moe_tree_attention   over the cache and the drafted tokens themselves, which are not in the cache
+ *   moe_cache_write      of the rows that were accepted (and of a prompt's rows), quantised on the way if the cache is
+ * moe_draft_block_forward is such a step of a whole decoder block.  Rows are given as a pointer and a distance between rows
+ * in elements (so that heads may be columns of a wider projection); distances are at least the row's width, at most 2^24,
+ * and multiples of 8 (float: 4).  Calls take up to 2^30 rows.  Outputs may overlap no input unless said otherwise. */
+
+/* Rotary positions.  rot_dim dimensions of each head turn in rot_dim / 2 pairs, pair i of position p by the angle p f_i:
+ *   (x, y) -> amplitude (x cos - y sin, y cos + x sin),      f_i = base^(-2 i / rot_dim) scaled as `scaling` says:
+ *   MOE_ROPE_PLAIN     f_i
+ *   MOE_ROPE_LINEAR    f_i / factor
+ *   MOE_ROPE_BY_PARTS  f_i (g + (1 - g) / factor), g = clamp((r - low) / (high - low), 0, 1), r = original_len f_i / (2 pi):
+ *                      pairs that turn more than `high` times over the trained length keep their frequency, those that
+ *                      turn fewer than `low` times are slowed down by `factor`.
+ * Pair i is (i, i + rot_dim / 2) or (2 i, 2 i + 1); dimensions from rot_dim on are passed on.  head_dim and rot_dim are
+ * multiples of 8, 8 <= rot_dim <= head_dim <= 512.  Fields that a scaling does not use are ignored. */
+typedef enum { MOE_ROPE_HALF = 0, MOE_ROPE_INTERLEAVED = 1 } moe_rope_layout_t;
+typedef enum { MOE_ROPE_PLAIN = 0, MOE_ROPE_LINEAR = 1, MOE_ROPE_BY_PARTS = 2 } moe_rope_scaling_t;
+typedef struct {
+    int32_t head_dim, rot_dim;
+    int32_t layout;        /* moe_rope_layout_t                                  */
+    int32_t dtype;         /* moe_dtype_t of x and out                           */
+    int32_t scaling;       /* moe_rope_scaling_t                                 */
+    float amplitude;       /* finite; 1 for plain rotation                       */
+    double base;           /* finite, > 1                                        */
+    double factor;         /* finite, > 0                                        */
+    double original_len;   /* finite, > 0: positions that the model was trained on */
+    double low, high;      /* finite, low < high                                 */
+} moe_rope_t;
+
+/* moe_rope_frequencies -- turns [rot_dim / 2], a HOST array: f_i / (2 pi), turns per position.  Pure host arithmetic; a
+ * program does this once and keeps a copy in device memory for moe_rope. */
+int moe_rope_frequencies(const moe_rope_t* rope, double* turns);
+
+/* moe_rope -- n_heads consecutive heads of n_rows rows turned to their positions.
+ *   x, out  [n_rows, n_heads * head_dim] at distances x_stride, out_stride; out may be x with the same distance
+ *   turns   [rot_dim / 2] double, as moe_rope_frequencies gave them
+ *   pos     [n_rows]; a row whose position is negative is left out: its row of out stays as it is
+ * Angles are formed and reduced in 64 bits, so that far positions lose nothing; everything else is done in 32 bits and
+ * rounded once. */
+int moe_rope(const moe_rope_t* rope, int32_t n_rows, int32_t n_heads, const void* x, int64_t x_stride, const double* turns,
+             const int32_t* pos, void* out, int64_t out_stride, void* stream);
+
+/* Key/value caches: k_cache, v_cache [n_seq, n_kv_heads, max_len, head_dim] (moe_decode_block_forward's with
+ * n_kv_heads = n_heads and MOE_CACHE_BF16), elements and scales by `kind`:
+ *   MOE_CACHE_BF16  bf16; no scales (k_scale, v_scale NULL)
+ *   MOE_CACHE_FP8   e4m3 bytes (largest value 448)
+ *   MOE_CACHE_FP4   e2m1, two to a byte, the lower index in the lower four bits (largest value 6)
+ * The last two have k_scale, v_scale [n_seq, n_kv_heads, max_len, head_dim / 32] bytes: elements 32 j .. 32 j + 31 of a row
+ * share the power of two 2^(byte - 127), the smallest from 2^-100 on with which the largest of them fits the format
+ * (and at most 2^119 or 2^125, so that no value leaves bf16: beyond 448 2^119 or 6 2^125 stands the format's largest);
+ * elements are rounded to the nearest, ties to even.  A block that holds an infinity or NaN has scale byte 255 and reads as
+ * NaN throughout.  What a cache holds is exact in bf16.
+ * n_heads (a multiple of n_kv_heads) is the number of query heads; head_dim is 64 or 128. */
+typedef enum { MOE_CACHE_BF16 = 0, MOE_CACHE_FP8 = 1, MOE_CACHE_FP4 = 2 } moe_cache_kind_t;
+typedef struct {
+    int32_t n_seq;         /* sequences                                          */
+    int32_t n_heads;       /* query heads, at most 1024                          */
+    int32_t n_kv_heads;    /* key/value heads                                    */
+    int32_t head_dim;      /* 64 or 128                                          */
+    int32_t max_len;       /* positions per sequence, at most 2^24               */
+    int32_t kind;          /* moe_cache_kind_t                                   */
+} moe_cache_shape_t;
+
+/* Bytes of k_cache (v_cache has as many), and of k_scale; 0 for an invalid shape, and for the scales of a bf16 cache. */
+size_t moe_cache_bytes(const moe_cache_shape_t* cache);
+size_t moe_cache_scale_bytes(const moe_cache_shape_t* cache);
+
+/* moe_cache_write -- row r's keys and values (k, v [n_rows, n_kv_heads * head_dim] bf16) become position pos[r] of
+ * sequence seq[r].  Rows whose sequence or position lies outside the cache (-1 for rows that are not wanted) are left out.
+ * Of two rows with the same sequence and position what the cache then holds is unspecified.  Positions that no row names
+ * stay as they are. */
+int moe_cache_write(const moe_cache_shape_t* cache, int32_t n_rows, const void* k, int64_t k_stride, const void* v,
+                    int64_t v_stride, const int32_t* seq, const int32_t* pos, void* k_cache, void* v_cache,
+                    uint8_t* k_scale, uint8_t* v_scale, void* stream);
+
+/* moe_cache_read -- the reverse: rows of k, v become what the cache holds at (seq[r], pos[r]), in bf16; rows whose
+ * sequence or position lies outside the cache stay as they are.  The same place may be read by several rows. */
+int moe_cache_read(const moe_cache_shape_t* cache, int32_t n_rows, const void* k_cache, const void* v_cache,
+                   const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* seq, const int32_t* pos, void* k,
+                   int64_t k_stride, void* v, int64_t v_stride, void* stream);
+
+/* moe_tree_attention -- attention of n_draft (1 to 256) new tokens per sequence over its cached positions and over each
+ * other.  With T = n_seq * n_draft rows, row b * n_draft + i for token i of sequence b:
+ *   q     [T, n_heads * head_dim], k, v [T, n_kv_heads * head_dim] bf16 (rotated, if the model has rotary positions);
+ *         query head h reads key/value head h / (n_heads / n_kv_heads)
+ *   lens  [n_seq] cached positions that are seen (clamped into 0..max_len)
+ *   counts[n_seq] drafted tokens of the sequence (clamped into 0..n_draft), or NULL: n_draft each
+ *   tree  [n_seq, n_draft, ceil(n_draft / 32)] bit masks: token i sees drafted token j if bit j % 32 of word j / 32 of its
+ *         row is set; NULL: token i sees tokens 0..i.  Bits from counts[b] on are ignored.
+ *   out   [T, n_heads * head_dim]: out[b, i, h] = softmax(q . K^T / sqrt(head_dim)) V over what it sees; exactly 0 if it
+ *         sees nothing.  Rows from counts[b] on stay as they are.
+ * Keys and values that a token does not see have no part in its result, whatever they hold.  Softmax statistics and sums
+ * are in 32 bits; the probabilities are rounded to bf16 for the product with the values.  The caches are only read.
+ * n_seq * n_draft * n_heads is below 2^31.  ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */
+size_t moe_tree_attention_workspace_bytes(const moe_cache_shape_t* cache, int32_t n_draft);
+int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const void* q, int64_t q_stride, const void* k,
+                       int64_t k_stride, const void* v, int64_t v_stride, const void* k_cache, const void* v_cache,
+                       const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* lens, const int32_t* counts,
+                       const int32_t* tree, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
+
 /* Stage timing of moe_layer_forward, for benchmarks (the paper reports the MoE
  * kernels' latency as a whole, Sec. 5.4; this splits it per kernel).
  * moe_profile_enable(n > 0) creates events for the next n calls (the one place

@@ -23,11 +23,15 @@ MOE_F32, MOE_BF16 = 0, 1
 MOE_OK = 0
 MOE_FLAG_PACKED_WEIGHTS = 1
 MOE_FLAG_PACKED_GATE = 2
+MOE_ROPE_HALF, MOE_ROPE_INTERLEAVED = 0, 1
+MOE_ROPE_PLAIN, MOE_ROPE_LINEAR, MOE_ROPE_BY_PARTS = 0, 1, 2
+MOE_CACHE_BF16, MOE_CACHE_FP8, MOE_CACHE_FP4 = 0, 1, 2
 ENTRY_POINTS = ("moe_workspace_bytes", "moe_status_string", "moe_version", "moe_packed_weights_bytes",
                 "moe_pack_weights", "moe_packed_gate_bytes", "moe_pack_gate", "moe_gate", "moe_gate_noalloc",
                 "moe_gate_noalloc_bytes", "moe_gate_noalloc_max_bytes", "moe_dispatch",
                 "moe_expert_ffn", "moe_expert_ffn_slice", "moe_expert_ffn_slice_reduce", "moe_combine", "moe_layer_forward", "moe_decode_block_workspace_bytes",
-                "moe_decode_block_forward", "moe_profile_enable", "moe_profile_select",
+                "moe_decode_block_forward", "moe_rope_frequencies", "moe_rope", "moe_cache_bytes", "moe_cache_scale_bytes",
+                "moe_cache_write", "moe_cache_read", "moe_tree_attention_workspace_bytes", "moe_tree_attention", "moe_profile_enable", "moe_profile_select",
                 "moe_profile_stride", "moe_profile_calls",
                 "moe_profile_stage_count", "moe_profile_stage_name", "moe_profile_elapsed")
 
@@ -47,6 +51,15 @@ BLOCK_WEIGHT_FIELDS = ("ln1_gamma", "ln1_beta", "Wqkv", "bqkv", "Wo", "bo", "ln2
 
 class MoeBlockWeights(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in BLOCK_WEIGHT_FIELDS]
+
+
+class MoeRope(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("head_dim", "rot_dim", "layout", "dtype", "scaling")] + [("amplitude", ctypes.c_float)] + \
+        [(n, ctypes.c_double) for n in ("base", "factor", "original_len", "low", "high")]
+
+
+class MoeCacheShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_heads", "n_kv_heads", "head_dim", "max_len", "kind")]
 
 
 class MoeError(RuntimeError):
@@ -107,6 +120,23 @@ def load_library() -> ctypes.CDLL:
     lib.moe_decode_block_forward.restype = i32
     lib.moe_decode_block_forward.argtypes = [sp, ctypes.POINTER(MoeBlockShape), ctypes.POINTER(MoeBlockWeights)] + \
         [vp] * 8 + [vp, st, vp]
+    rp, cp, i64 = ctypes.POINTER(MoeRope), ctypes.POINTER(MoeCacheShape), ctypes.c_int64
+    lib.moe_rope_frequencies.restype = i32
+    lib.moe_rope_frequencies.argtypes = [rp, vp]
+    lib.moe_rope.restype = i32
+    lib.moe_rope.argtypes = [rp, i32, i32, vp, i64, vp, vp, vp, i64, vp]
+    lib.moe_cache_bytes.restype = st
+    lib.moe_cache_bytes.argtypes = [cp]
+    lib.moe_cache_scale_bytes.restype = st
+    lib.moe_cache_scale_bytes.argtypes = [cp]
+    lib.moe_cache_write.restype = i32
+    lib.moe_cache_write.argtypes = [cp, i32, vp, i64, vp, i64] + [vp] * 7
+    lib.moe_cache_read.restype = i32
+    lib.moe_cache_read.argtypes = [cp, i32] + [vp] * 6 + [vp, i64, vp, i64, vp]
+    lib.moe_tree_attention_workspace_bytes.restype = st
+    lib.moe_tree_attention_workspace_bytes.argtypes = [cp, i32]
+    lib.moe_tree_attention.restype = i32
+    lib.moe_tree_attention.argtypes = [cp, i32] + [vp, i64] * 3 + [vp] * 7 + [vp, i64, vp, st, vp]
     lib.moe_profile_enable.restype = i32
     lib.moe_profile_enable.argtypes = [i32]
     lib.moe_profile_select.restype = i32
@@ -379,6 +409,151 @@ def moe_decode_block_forward(shape, block, weights: dict, x, k_cache, v_cache, p
         _ptr(out, el, T * d, "out"), _ptr(x1_out, el, T * d, "x1_out"), _ptr(moe_in_out, el, T * d, "moe_in_out"),
         _ptr(logits_out, f32, T * E, "logits_out"), wsp, wsn, _stream())
     _check("moe_decode_block_forward", rc)
+
+
+# ---- several new tokens per sequence ---------------------------------------------------------------------------
+
+def _here(*tensors) -> None:
+    """The launch goes to the current device: tensors of another one are refused."""
+    device = torch._C._cuda_getDevice()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != device:
+            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
+
+
+def _rows(t: torch.Tensor, dtype: torch.dtype, rows: int, cols: int, name: str):
+    """(address, distance between rows in elements) of [rows, cols], whose rows may be columns of wider ones."""
+    if not t.is_cuda:
+        raise ValueError(f"{name}: device tensor required")
+    if t.dtype != dtype:
+        raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
+    if tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
+    if t.stride(1) != 1 and cols > 1:
+        raise ValueError(f"{name}: the elements of a row have to be adjacent")
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def make_rope(head_dim: int, rot_dim: int, layout, dtype, base: float = 10000.0, amplitude: float = 1.0, scaling="plain",
+              factor: float = 1.0, original_len: float = 1.0, low: float = 1.0, high: float = 4.0) -> MoeRope:
+    """layout: "half" or "interleaved"; scaling: "plain", "linear" or "by_parts" (or the MOE_ROPE_* numbers)."""
+    if isinstance(layout, str):
+        layout = {"half": MOE_ROPE_HALF, "interleaved": MOE_ROPE_INTERLEAVED}[layout]
+    if isinstance(scaling, str):
+        scaling = {"plain": MOE_ROPE_PLAIN, "linear": MOE_ROPE_LINEAR, "by_parts": MOE_ROPE_BY_PARTS}[scaling]
+    if isinstance(dtype, torch.dtype):
+        dtype = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}[dtype]
+    elif isinstance(dtype, str):
+        dtype = {"f32": MOE_F32, "bf16": MOE_BF16}[dtype]
+    return MoeRope(head_dim, rot_dim, int(layout), int(dtype), int(scaling), amplitude, base, factor, original_len, low, high)
+
+
+def moe_rope_frequencies(rope: MoeRope, device="cuda") -> torch.Tensor:
+    """Turns per position [rot_dim / 2], float64, on `device`: the `turns` of moe_rope."""
+    host = torch.empty(max(rope.rot_dim, 2) // 2, dtype=torch.float64)
+    _check("moe_rope_frequencies", load_library().moe_rope_frequencies(ctypes.byref(rope), host.data_ptr()))
+    return host.to(device)
+
+
+def moe_rope(rope: MoeRope, x, turns, pos, out) -> None:
+    """x, out: [rows, heads * head_dim], columns of wider rows if need be; out may be x."""
+    dtype = torch.float32 if rope.dtype == MOE_F32 else torch.bfloat16
+    rows, cols = x.shape
+    if rows == 0:
+        return
+    if cols == 0 or cols % rope.head_dim:
+        raise ValueError(f"x: {cols} columns are no heads of {rope.head_dim}")
+    _here(x, turns, pos, out)
+    xp, xs = _rows(x, dtype, rows, cols, "x")
+    op, os_ = _rows(out, dtype, rows, cols, "out")
+    rc = load_library().moe_rope(ctypes.byref(rope), rows, cols // rope.head_dim, xp, xs, _ptr(turns, torch.float64, rope.rot_dim // 2, "turns"),
+                                 _ptr(pos, torch.int32, rows, "pos"), op, os_, _stream())
+    _check("moe_rope", rc)
+
+
+def make_cache_shape(n_seq: int, n_heads: int, n_kv_heads: int, head_dim: int, max_len: int, kind) -> MoeCacheShape:
+    """kind: "bf16", "fp8" or "fp4" (or the MOE_CACHE_* numbers)."""
+    if isinstance(kind, str):
+        kind = {"bf16": MOE_CACHE_BF16, "fp8": MOE_CACHE_FP8, "fp4": MOE_CACHE_FP4}[kind]
+    return MoeCacheShape(n_seq, n_heads, n_kv_heads, head_dim, max_len, int(kind))
+
+
+def moe_cache_bytes(cache: MoeCacheShape) -> int:
+    return int(load_library().moe_cache_bytes(ctypes.byref(cache)))
+
+
+def moe_cache_scale_bytes(cache: MoeCacheShape) -> int:
+    return int(load_library().moe_cache_scale_bytes(ctypes.byref(cache)))
+
+
+def alloc_cache(cache: MoeCacheShape, device="cuda"):
+    """(k_cache, v_cache, k_scale, v_scale): bf16, or uint8 with [n_seq, n_kv_heads, max_len, head_dim / 32] scales; scales None for bf16."""
+    if moe_cache_bytes(cache) == 0:
+        raise MoeError("moe_cache_bytes", -1, "invalid shape")
+    B, G, L, dh = cache.n_seq, cache.n_kv_heads, cache.max_len, cache.head_dim
+    if cache.kind == MOE_CACHE_BF16:
+        return *(torch.zeros((B, G, L, dh), dtype=torch.bfloat16, device=device) for _ in "kv"), None, None
+    cols = dh if cache.kind == MOE_CACHE_FP8 else dh // 2
+    return *(torch.zeros((B, G, L, cols), dtype=torch.uint8, device=device) for _ in "kv"), \
+        *(torch.zeros((B, G, L, dh // 32), dtype=torch.uint8, device=device) for _ in "kv")
+
+
+def _cache_args(cache, k_cache, v_cache, k_scale, v_scale):
+    total = cache.n_seq * cache.n_kv_heads * cache.max_len
+    if cache.kind == MOE_CACHE_BF16:
+        el, n = torch.bfloat16, total * cache.head_dim
+    else:
+        el, n = torch.uint8, total * cache.head_dim // (1 if cache.kind == MOE_CACHE_FP8 else 2)
+    x = total * (cache.head_dim // 32)
+    return (_ptr(k_cache, el, n, "k_cache"), _ptr(v_cache, el, n, "v_cache"), _ptr(k_scale, torch.uint8, x, "k_scale"),
+            _ptr(v_scale, torch.uint8, x, "v_scale"))
+
+
+def moe_cache_write(cache, k, v, seq, pos, k_cache, v_cache, k_scale, v_scale) -> None:
+    """k, v: [rows, n_kv_heads * head_dim] bf16, columns of wider rows if need be; seq, pos: [rows] int32."""
+    rows, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
+    if rows == 0:
+        return
+    _here(k, v, seq, pos, k_cache, v_cache, k_scale, v_scale)
+    rc = load_library().moe_cache_write(
+        ctypes.byref(cache), rows, *_rows(k, torch.bfloat16, rows, cols, "k"), *_rows(v, torch.bfloat16, rows, cols, "v"),
+        _ptr(seq, torch.int32, rows, "seq"), _ptr(pos, torch.int32, rows, "pos"), *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _stream())
+    _check("moe_cache_write", rc)
+
+
+def moe_cache_read(cache, k_cache, v_cache, k_scale, v_scale, seq, pos, k, v) -> None:
+    """The reverse of moe_cache_write: fills the rows of k and v."""
+    rows, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
+    if rows == 0:
+        return
+    _here(k, v, seq, pos, k_cache, v_cache, k_scale, v_scale)
+    rc = load_library().moe_cache_read(
+        ctypes.byref(cache), rows, *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _ptr(seq, torch.int32, rows, "seq"),
+        _ptr(pos, torch.int32, rows, "pos"), *_rows(k, torch.bfloat16, rows, cols, "k"), *_rows(v, torch.bfloat16, rows, cols, "v"), _stream())
+    _check("moe_cache_read", rc)
+
+
+def moe_tree_attention_workspace_bytes(cache: MoeCacheShape, n_draft: int) -> int:
+    return int(load_library().moe_tree_attention_workspace_bytes(ctypes.byref(cache), int(n_draft)))
+
+
+@functools.lru_cache(maxsize=256)
+def _tree_workspace_need(cache: bytes, n_draft: int) -> int:
+    return moe_tree_attention_workspace_bytes(MoeCacheShape.from_buffer_copy(cache), n_draft)
+
+
+def moe_tree_attention(cache, n_draft: int, q, k, v, k_cache, v_cache, k_scale, v_scale, lens, counts, tree, out, ws) -> None:
+    """q, out: [n_seq * n_draft, n_heads * head_dim], k, v: [n_seq * n_draft, n_kv_heads * head_dim] bf16, columns of wider rows if
+    need be; counts and tree may be None."""
+    bf, i32 = torch.bfloat16, torch.int32
+    T, qw, kw = cache.n_seq * n_draft, cache.n_heads * cache.head_dim, cache.n_kv_heads * cache.head_dim
+    _here(q, k, v, k_cache, v_cache, k_scale, v_scale, lens, counts, tree, out, ws)
+    wsp, wsn = _ws(cache, ws, _tree_workspace_need(bytes(cache), n_draft))
+    rc = load_library().moe_tree_attention(
+        ctypes.byref(cache), n_draft, *_rows(q, bf, T, qw, "q"), *_rows(k, bf, T, kw, "k"), *_rows(v, bf, T, kw, "v"),
+        *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _ptr(lens, i32, cache.n_seq, "lens"), _ptr(counts, i32, cache.n_seq, "counts"),
+        _ptr(tree, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, bf, T, qw, "out"), wsp, wsn, _stream())
+    _check("moe_tree_attention", rc)
 
 
 def moe_profile_enable(max_calls: int) -> None:

@@ -1,6 +1,8 @@
 // C ABI of the library: argument checks, workspace carving and launch sequencing.
 // Every check happens on the host before the first HIP call.
 #include <algorithm>
+#include <cmath>
+#include <initializer_list>
 #include <vector>
 
 #include "call_tag.h"
@@ -1133,6 +1135,160 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
                                at<void>(ws, L.moe_ws), ws_layout(shape).total, x1, stream);
     g_prof.cur = -1;
     return rc;
+}
+
+// ---- several new tokens per sequence ------------------------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+constexpr long long kMaxRowStride = 1ll << 24;
+constexpr int kMaxRows = 1 << 30;
+
+// a distance between rows of `width` elements, pieces of `mult` elements
+bool row_stride_ok(long long stride, long long width, int mult) { return stride >= width && stride <= kMaxRowStride && stride % mult == 0; }
+
+int check_rope(const moe_rope_t* r) {
+    if (!r) return MOE_ERR_INVALID_ARG;
+    if (r->layout != MOE_ROPE_HALF && r->layout != MOE_ROPE_INTERLEAVED) return MOE_ERR_INVALID_ARG;
+    if (r->dtype != MOE_F32 && r->dtype != MOE_BF16) return MOE_ERR_INVALID_ARG;
+    if (r->head_dim < 1 || r->rot_dim < 1 || r->rot_dim > r->head_dim || !std::isfinite(r->amplitude)) return MOE_ERR_INVALID_ARG;
+    if (!std::isfinite(r->base) || !(r->base > 1.0)) return MOE_ERR_INVALID_ARG;
+    if (r->scaling < MOE_ROPE_PLAIN || r->scaling > MOE_ROPE_BY_PARTS) return MOE_ERR_INVALID_ARG;
+    if (r->scaling != MOE_ROPE_PLAIN && (!std::isfinite(r->factor) || !(r->factor > 0.0))) return MOE_ERR_INVALID_ARG;
+    if (r->scaling == MOE_ROPE_BY_PARTS && (!std::isfinite(r->original_len) || !(r->original_len > 0.0) || !std::isfinite(r->low) ||
+                                            !std::isfinite(r->high) || !(r->low < r->high)))
+        return MOE_ERR_INVALID_ARG;
+    if (r->head_dim % 8 || r->rot_dim % 8 || r->head_dim > 512) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+int check_cache(const moe_cache_shape_t* c) {
+    if (!c) return MOE_ERR_INVALID_ARG;
+    if (c->n_seq < 1 || c->n_heads < 1 || c->n_kv_heads < 1 || c->n_heads % c->n_kv_heads || c->head_dim < 1 || c->max_len < 1)
+        return MOE_ERR_INVALID_ARG;
+    if (c->kind < MOE_CACHE_BF16 || c->kind > MOE_CACHE_FP4) return MOE_ERR_INVALID_ARG;
+    if ((c->head_dim != 64 && c->head_dim != 128) || c->n_heads > 1024 || c->max_len > (1 << 24)) return MOE_ERR_UNSUPPORTED;
+    if ((long long)c->n_seq * c->n_heads >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+size_t cache_rows_total(const moe_cache_shape_t* c) { return (size_t)c->n_seq * c->n_kv_heads * c->max_len; }
+
+// the caches' own pointers: scales with 8 and 4 bits, and only then
+int check_cache_pointers(const moe_cache_shape_t* c, const void* kc, const void* vc, const void* kx, const void* vx) {
+    if (!kc || !vc || !aligned16(kc) || !aligned16(vc)) return MOE_ERR_INVALID_ARG;
+    if (c->kind == MOE_CACHE_BF16) return kx || vx ? MOE_ERR_INVALID_ARG : MOE_OK;
+    return kx && vx && aligned16(kx) && aligned16(vx) ? MOE_OK : MOE_ERR_INVALID_ARG;
+}
+
+int check_cache_rows(const moe_cache_shape_t* c, int32_t n_rows, const void* k, int64_t k_stride, const void* v, int64_t v_stride,
+                     const int32_t* seq, const int32_t* pos, const void* kc, const void* vc, const void* kx, const void* vx) {
+    int rc = check_cache(c);
+    if (rc != MOE_OK) return rc;
+    if (n_rows < 1 || !k || !v || !seq || !pos || !aligned16(k) || !aligned16(v) || !aligned16(seq) || !aligned16(pos)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_cache_pointers(c, kc, vc, kx, vx)) != MOE_OK) return rc;
+    if (n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    const long long width = (long long)c->n_kv_heads * c->head_dim;
+    return row_stride_ok(k_stride, width, 8) && row_stride_ok(v_stride, width, 8) ? MOE_OK : MOE_ERR_INVALID_ARG;
+}
+
+constexpr int kMaxDraft = 256;
+int check_tree(const moe_cache_shape_t* c, int32_t n_draft) {
+    const int rc = check_cache(c);
+    if (rc != MOE_OK) return rc;
+    if (n_draft < 1) return MOE_ERR_INVALID_ARG;
+    if (n_draft > kMaxDraft || (long long)c->n_seq * n_draft * c->n_heads >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    return MOE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int moe_rope_frequencies(const moe_rope_t* rope, double* turns) {
+    const int rc = check_rope(rope);
+    if (rc != MOE_OK) return rc;
+    if (!turns) return MOE_ERR_INVALID_ARG;
+    for (int i = 0; i < rope->rot_dim / 2; ++i) {
+        double t = std::pow(rope->base, -2.0 * i / rope->rot_dim) / 6.283185307179586476925;
+        if (rope->scaling == MOE_ROPE_LINEAR) {
+            t /= rope->factor;
+        } else if (rope->scaling == MOE_ROPE_BY_PARTS) {
+            const double g = std::clamp((rope->original_len * t - rope->low) / (rope->high - rope->low), 0.0, 1.0);
+            t *= g + (1.0 - g) / rope->factor;
+        }
+        turns[i] = t;
+    }
+    return MOE_OK;
+}
+
+int moe_rope(const moe_rope_t* rope, int32_t n_rows, int32_t n_heads, const void* x, int64_t x_stride, const double* turns,
+             const int32_t* pos, void* out, int64_t out_stride, void* stream) {
+    const int rc = check_rope(rope);
+    if (rc != MOE_OK) return rc;
+    if (n_rows < 1 || n_heads < 1 || !x || !turns || !pos || !out) return MOE_ERR_INVALID_ARG;
+    if (!aligned16(x) || !aligned16(turns) || !aligned16(pos) || !aligned16(out)) return MOE_ERR_INVALID_ARG;
+    const long long width = (long long)n_heads * rope->head_dim;
+    const int mult = rope->dtype == MOE_F32 ? 4 : 8;
+    if (!row_stride_ok(x_stride, width, mult) || !row_stride_ok(out_stride, width, mult)) return MOE_ERR_INVALID_ARG;
+    if (x == out && x_stride != out_stride) return MOE_ERR_INVALID_ARG;
+    if (n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    return launch_rope(rope, n_rows, n_heads, x, x_stride, turns, pos, out, out_stride, static_cast<hipStream_t>(stream));
+}
+
+size_t moe_cache_bytes(const moe_cache_shape_t* cache) {
+    if (check_cache(cache) != MOE_OK) return 0;
+    const int bits = cache->kind == MOE_CACHE_BF16 ? 16 : cache->kind == MOE_CACHE_FP8 ? 8 : 4;
+    return cache_rows_total(cache) * (cache->head_dim * bits / 8);
+}
+
+size_t moe_cache_scale_bytes(const moe_cache_shape_t* cache) {
+    if (check_cache(cache) != MOE_OK || cache->kind == MOE_CACHE_BF16) return 0;
+    return cache_rows_total(cache) * (cache->head_dim / 32);
+}
+
+int moe_cache_write(const moe_cache_shape_t* cache, int32_t n_rows, const void* k, int64_t k_stride, const void* v,
+                    int64_t v_stride, const int32_t* seq, const int32_t* pos, void* k_cache, void* v_cache,
+                    uint8_t* k_scale, uint8_t* v_scale, void* stream) {
+    const int rc = check_cache_rows(cache, n_rows, k, k_stride, v, v_stride, seq, pos, k_cache, v_cache, k_scale, v_scale);
+    if (rc != MOE_OK) return rc;
+    return launch_cache_write(cache, n_rows, k, k_stride, v, v_stride, seq, pos, k_cache, v_cache, k_scale, v_scale,
+                              static_cast<hipStream_t>(stream));
+}
+
+int moe_cache_read(const moe_cache_shape_t* cache, int32_t n_rows, const void* k_cache, const void* v_cache,
+                   const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* seq, const int32_t* pos, void* k,
+                   int64_t k_stride, void* v, int64_t v_stride, void* stream) {
+    const int rc = check_cache_rows(cache, n_rows, k, k_stride, v, v_stride, seq, pos, k_cache, v_cache, k_scale, v_scale);
+    if (rc != MOE_OK) return rc;
+    return launch_cache_read(cache, n_rows, k_cache, v_cache, k_scale, v_scale, seq, pos, k, k_stride, v, v_stride,
+                             static_cast<hipStream_t>(stream));
+}
+
+size_t moe_tree_attention_workspace_bytes(const moe_cache_shape_t* cache, int32_t n_draft) {
+    if (check_tree(cache, n_draft) != MOE_OK) return 0;
+    return align_up(tree_attn_ws_bytes(cache, n_draft));
+}
+
+int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const void* q, int64_t q_stride, const void* k,
+                       int64_t k_stride, const void* v, int64_t v_stride, const void* k_cache, const void* v_cache,
+                       const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* lens, const int32_t* counts,
+                       const int32_t* tree, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_tree(cache, n_draft);
+    if (rc != MOE_OK) return rc;
+    if (!q || !k || !v || !lens || !out) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {q, k, v, static_cast<const void*>(lens), static_cast<const void*>(counts), static_cast<const void*>(tree),
+                          static_cast<const void*>(out)})
+        if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_cache_pointers(cache, k_cache, v_cache, k_scale, v_scale)) != MOE_OK) return rc;
+    const long long qw = (long long)cache->n_heads * cache->head_dim, kw = (long long)cache->n_kv_heads * cache->head_dim;
+    if (!row_stride_ok(q_stride, qw, 8) || !row_stride_ok(k_stride, kw, 8) || !row_stride_ok(v_stride, kw, 8) || !row_stride_ok(out_stride, qw, 8))
+        return MOE_ERR_INVALID_ARG;
+    if (!ws || !aligned16(ws) || ws_bytes < align_up(tree_attn_ws_bytes(cache, n_draft))) return MOE_ERR_WORKSPACE;
+    const TreeArgs a{u16(q), u16(k), u16(v), q_stride, k_stride, v_stride, out_stride, k_cache, v_cache, k_scale, v_scale,
+                     lens, counts, tree, u16(out), cache->n_seq, n_draft, cache->n_heads, cache->n_kv_heads, cache->max_len};
+    return launch_tree_attn(a, cache->kind, cache->head_dim, ws, static_cast<hipStream_t>(stream));
 }
 
 int moe_profile_enable(int max_calls) {

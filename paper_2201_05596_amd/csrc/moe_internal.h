@@ -341,4 +341,28 @@ size_t attn_partial_floats(int T, int H, int dh, int Lmax);
 int launch_attn_decode(const uint16_t* qkv, uint16_t* cache_k, uint16_t* cache_v, const int32_t* pos, float* partial,
                        uint16_t* attn, int T, int H, int dh, int Lmax, hipStream_t s);
 
+// ---- several new tokens per sequence ----------------------------------------------------------------------------
+// (rope.hip) out == x: in place
+int launch_rope(const moe_rope_t* rope, int n_rows, int n_heads, const void* x, long long x_stride, const double* turns,
+                const int32_t* pos, void* out, long long out_stride, hipStream_t s);
+// (kv_cache.hip)
+int launch_cache_write(const moe_cache_shape_t* c, int n_rows, const void* k, long long k_stride, const void* v, long long v_stride,
+                       const int32_t* seq, const int32_t* pos, void* k_cache, void* v_cache, uint8_t* k_scale, uint8_t* v_scale,
+                       hipStream_t s);
+int launch_cache_read(const moe_cache_shape_t* c, int n_rows, const void* k_cache, const void* v_cache, const uint8_t* k_scale,
+                      const uint8_t* v_scale, const int32_t* seq, const int32_t* pos, void* k, long long k_stride, void* v,
+                      long long v_stride, hipStream_t s);
+// (tree_attn.hip)
+struct TreeArgs {
+    const uint16_t *q, *k, *v;         // rows of the drafted tokens
+    long long q_stride, k_stride, v_stride, out_stride;
+    const void *k_cache, *v_cache;
+    const uint8_t *k_scale, *v_scale;
+    const int32_t *lens, *counts, *tree;
+    uint16_t* out;
+    int n_seq, N, H, G, max_len;       // N drafted tokens per sequence
+};
+size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft);
+int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s);
+
 }  // namespace moe
