@@ -278,7 +278,8 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
  *   moe_cache_write      of the rows that were accepted (and of a prompt's rows), quantised on the way if the cache is
  * moe_draft_block_forward is such a step of a whole decoder block.  Rows are given as a pointer and a distance between rows
  * in elements (so that heads may be columns of a wider projection); distances are at least the row's width, at most 2^24,
- * and multiples of 8 (float: 4).  Calls take up to 2^30 rows.  Outputs may overlap no input unless said otherwise. */
+ * and multiples of 8 (float: 4).  moe_rope, moe_cache_write and
+ * moe_cache_read take up to 2^24 rows.  Outputs may overlap no input unless said otherwise. */
 
 /* Rotary positions.  rot_dim dimensions of each head turn in rot_dim / 2 pairs, pair i of position p by the angle p f_i:
  *   (x, y) -> amplitude (x cos - y sin, y cos + x sin),      f_i = base^(-2 i / rot_dim) scaled as `scaling` says:

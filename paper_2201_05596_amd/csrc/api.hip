@@ -1144,7 +1144,7 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
 namespace {
 
 constexpr long long kMaxRowStride = 1ll << 24;
-constexpr int kMaxRows = 1 << 30;
+constexpr int kMaxRows = 1 << 24;
 
 // a distance between rows of `width` elements, pieces of `mult` elements
 bool row_stride_ok(long long stride, long long width, int mult) { return stride >= width && stride <= kMaxRowStride && stride % mult == 0; }

@@ -1,82 +1,112 @@
-// Attention of several new tokens per sequence over its cached positions and, through a bit mask, over each other.
-//   out[b, i, h] = sum_j p_j v_j / sum_j p_j,   p_j = exp(q . k_j / sqrt(DH) - max)     over what token i sees
-// One wave per row and head: 64 positions at a time, a score per lane, then DH / 64 dimensions of the values per lane.
-#include "cache_kind.h"
+// Attention for drafted tokens: the choice of an instance, its workspace, and the merge of items that lie in several shares.
+#include <algorithm>
+
+#include "tree_attn.h"
 
 namespace moe {
 
-template <int KIND, int DH>
-__device__ __forceinline__ float cached_element(const void* cache, const uint8_t* scale, long long row, int i) {
-    if constexpr (KIND == MOE_CACHE_BF16) {
-        return bf16_to_f32(static_cast<const uint16_t*>(cache)[row * DH + i]);
-    } else {
-        const float s = scale_value(scale[row * (DH / kScaleBlock) + i / kScaleBlock]);
-        uint32_t pair;
-        if constexpr (KIND == MOE_CACHE_FP8) pair = fp8_pair<false>(static_cast<const uint8_t*>(cache)[row * DH + i], s);
-        else pair = fp4_pair<0>((uint32_t)static_cast<const uint8_t*>(cache)[row * (DH / 2) + i / 2] >> (4 * (i & 1)), s);
-        return __uint_as_float(pair << 16);
+int launch_tree_bf16(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s);
+int launch_tree_fp8(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s);
+int launch_tree_fp4(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s);
+
+// out of the parts of every item that lies in more than one share.  A work-group takes `per` rows of an item; 16 threads share
+// a row (DH / 16 elements each), the other factor of 256 takes every so many parts and is added up in LDS.
+template <int DH>
+__global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a, const TreeParts parts, int ROWS, int wp, int per, int blocks_per_head) {
+    constexpr int NF = DH / 16;
+    __shared__ long long sh[8];
+    __shared__ float ml[16][16][2], o[16][16][NF];            // [part set][row] and, per thread, its sums
+    const int tid = threadIdx.x, R = a.H / a.G;
+    const int chunks = ROWS / per;
+    const Shares share = shares(a, ROWS, parts.groups, wp, sh, tid);
+    for (long long bx = blockIdx.x; bx < (long long)a.n_seq * a.G * blocks_per_head * chunks; bx += gridDim.x) {
+    const int chunk = (int)(bx % chunks), block = (int)(bx / chunks % blocks_per_head), g = (int)(bx / chunks / blocks_per_head % a.G);
+    const int b = (int)(bx / chunks / blocks_per_head / a.G);
+    const Sequence s = sequence(a, b, ROWS);
+    const int rows = s.count * R, row0 = block * ROWS + chunk * per;
+    if (row0 >= rows) continue;
+    long long before = 0;                                     // steps of the sequences before b
+    int unused = 0;
+    for (int i = tid; i < b; i += 256) { const Sequence t = sequence(a, i, ROWS); before += t.items * t.tiles; }
+    block_sum_max(before, unused, sh, tid);
+    const long long first = before + ((long long)g * (s.items / a.G) + block) * s.tiles, last = first + s.tiles - 1;
+    const long long w0 = first / share.size, w1 = last / share.size;
+    if (w0 == w1) continue;
+    const int piece = tid % 16, local = tid / 16 % per, set = tid / 16 / per, sets = 16 / per;
+    const int row = row0 + local, in_block = chunk * per + local;
+    float M = kLowest, L = 0.f, v[NF] = {};
+    for (long long w = w0 + set; w <= w1; w += sets) {
+        const size_t at = partial_slot(w, w > w0 || first == w0 * share.size) * ROWS + in_block;
+        const float2 x = *reinterpret_cast<const float2*>(parts.ml + at * 2);
+        float e[NF];
+#pragma unroll
+        for (int i = 0; i < NF; i += 4) *reinterpret_cast<float4*>(e + i) = *reinterpret_cast<const float4*>(parts.o + at * DH + piece * NF + i);
+        const float m = fmaxf(M, x.x), f = __builtin_amdgcn_exp2f(M - m), h = __builtin_amdgcn_exp2f(x.x - m);
+        M = m;
+        L = L * f + x.y * h;
+#pragma unroll
+        for (int i = 0; i < NF; ++i) v[i] = v[i] * f + e[i] * h;
+    }
+    if (sets > 1) {
+        if (piece == 0) { ml[set][local][0] = M; ml[set][local][1] = L; }
+#pragma unroll
+        for (int i = 0; i < NF; ++i) o[tid / 16][piece][i] = v[i];
+        __syncthreads();
+        const float own = M;
+        for (int i = 1; i < sets; ++i) M = fmaxf(M, ml[i][local][0]);
+        float f = __builtin_amdgcn_exp2f(own - M);
+        L *= f;
+#pragma unroll
+        for (int j = 0; j < NF; ++j) v[j] *= f;
+        for (int i = 1; i < sets; ++i) {
+            f = __builtin_amdgcn_exp2f(ml[i][local][0] - M);
+            L += ml[i][local][1] * f;
+#pragma unroll
+            for (int j = 0; j < NF; ++j) v[j] += o[i * per + local][piece][j] * f;
+        }
+    }
+    if (set || row >= rows) continue;
+    const int tok = row / R;
+    float none = 0.f;                                         // a row of sum 0: 0 if it sees nothing, NaN if all its scores are -inf
+    if (L == 0.f && sees_anything(a, s, b, tok)) none = __uint_as_float(0x7fc00000u);
+    const float f = 1.f / L;
+    uint32_t w[NF / 2];
+#pragma unroll
+    for (int i = 0; i < NF / 2; ++i) w[i] = L == 0.f ? pack_bf16x2(none, none) : pack_bf16x2(v[2 * i] * f, v[2 * i + 1] * f);
+    uint16_t* dst = a.out + ((long long)b * a.N + tok) * a.out_stride + (g * R + row - tok * R) * DH + piece * NF;
+    if constexpr (DH == 128) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+    else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
     }
 }
 
-template <int KIND, int DH>
-__global__ __launch_bounds__(64) void tree_attn_kernel(const TreeArgs a) {
-    __shared__ float q[DH], p_sh[64];
-    const int lane = threadIdx.x, h = blockIdx.x % a.H, row = blockIdx.x / a.H, b = row / a.N, i = row % a.N, g = h / (a.H / a.G);
-    const int len = min(max(a.lens[b], 0), a.max_len), count = a.counts ? min(max(a.counts[b], 0), a.N) : a.N;
-    if (i >= count) return;
-    for (int d = lane; d < DH; d += 64) q[d] = bf16_to_f32(a.q[row * a.q_stride + h * DH + d]) * rsqrtf((float)DH);
-    __syncthreads();
-    const long long base = ((long long)b * a.G + g) * a.max_len;
-    float m = -INFINITY, l = 0.f, o[DH / 64] = {};
-    for (int j0 = 0; j0 < len + count; j0 += 64) {
-        const int j = j0 + lane, t = j - len;                  // cached position j, or drafted token t
-        bool sees = j < len + count;
-        if (sees && t >= 0) sees = a.tree ? a.tree[(size_t)row * ((a.N + 31) / 32) + t / 32] >> (t % 32) & 1 : t <= i;
-        float s = -INFINITY;
-        if (sees) {
-            s = 0.f;
-            for (int d = 0; d < DH; ++d)
-                s = fmaf(q[d], t >= 0 ? bf16_to_f32(a.k[(b * (long long)a.N + t) * a.k_stride + g * DH + d])
-                                      : cached_element<KIND, DH>(a.k_cache, a.k_scale, base + j, d), s);
-        }
-        float mn = s;
-        for (int x = 32; x >= 1; x >>= 1) mn = fmaxf(mn, __shfl_xor(mn, x));
-        mn = fmaxf(m, mn);
-        const float zero = mn == -INFINITY ? 0.f : mn, c = expf(m - zero), p = sees ? expf(s - zero) : 0.f;
-        __syncthreads();
-        p_sh[lane] = p;
-        __syncthreads();
-        const uint64_t seen = __ballot(sees);
-        l *= c;
-        for (int e = 0; e < DH / 64; ++e) o[e] *= c;
-        for (int n = 0; n < 64; ++n) {
-            if (!(seen >> n & 1)) continue;
-            l += p_sh[n];
-            const int tn = j0 + n - len;
-            for (int e = 0; e < DH / 64; ++e)
-                o[e] = fmaf(p_sh[n], tn >= 0 ? bf16_to_f32(a.v[(b * (long long)a.N + tn) * a.v_stride + g * DH + e * 64 + lane])
-                                             : cached_element<KIND, DH>(a.v_cache, a.v_scale, base + j0 + n, e * 64 + lane), o[e]);
-        }
-        m = mn;
-    }
-    bool any = len > 0;
-    for (int t = 0; !any && t < count; ++t) any = a.tree ? a.tree[(size_t)row * ((a.N + 31) / 32) + t / 32] >> (t % 32) & 1 : t <= i;
-    for (int e = 0; e < DH / 64; ++e) a.out[row * a.out_stride + h * DH + e * 64 + lane] = any ? f32_to_bf16(o[e] / l) : 0;
+static TreePlan tree_plan(int n_seq, int G, int R, int N, int head_dim) {
+    const int rows = N * R;                                   // at most, per key/value head
+    TreePlan p;
+    p.mt = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
+    p.wr = rows <= 32 ? 1 : rows <= 128 ? 2 : 4;
+    p.groups = p.mt == 1 ? 768 : p.mt == 2 ? 512 : 256;
+    const int block = 16 * p.mt * p.wr;
+    p.row_blocks = (rows + block - 1) / block;
+    p.partial_bytes = (size_t)2 * p.groups * block * head_dim * sizeof(float);
+    return p;
+}
+size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft) {
+    const TreePlan p = tree_plan(c->n_seq, c->n_kv_heads, c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
+    return p.partial_bytes + (size_t)2 * p.groups * 16 * p.mt * p.wr * 2 * sizeof(float);
 }
 
-size_t tree_attn_ws_bytes(const moe_cache_shape_t*, int) { return 256; }
-
-int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void*, hipStream_t s) {
-    const dim3 grid((unsigned)(a.n_seq * a.N * a.H));
-#define MOE_TREE(KIND) \
-    do { \
-        if (head_dim == 128) hipLaunchKernelGGL((tree_attn_kernel<KIND, 128>), grid, dim3(64), 0, s, a); \
-        else hipLaunchKernelGGL((tree_attn_kernel<KIND, 64>), grid, dim3(64), 0, s, a); \
-    } while (0)
-    if (kind == MOE_CACHE_BF16) MOE_TREE(MOE_CACHE_BF16);
-    else if (kind == MOE_CACHE_FP8) MOE_TREE(MOE_CACHE_FP8);
-    else MOE_TREE(MOE_CACHE_FP4);
-#undef MOE_TREE
+int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s) {
+    const TreePlan p = tree_plan(a.n_seq, a.G, a.H / a.G, a.N, head_dim);
+    const TreeParts parts{static_cast<float*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + p.partial_bytes), p.groups};
+    const int rc = kind == MOE_CACHE_BF16 ? launch_tree_bf16(a, parts, head_dim, p.mt, p.wr, s)
+                   : kind == MOE_CACHE_FP8 ? launch_tree_fp8(a, parts, head_dim, p.mt, p.wr, s) : launch_tree_fp4(a, parts, head_dim, p.mt, p.wr, s);
+    if (rc != MOE_OK) return rc;
+    const int block = 16 * p.mt * p.wr;
+    const long long items = (long long)a.n_seq * a.G * p.row_blocks;
+    const int per = items <= 32 ? 1 : items <= 128 ? 4 : 16;  // few items: many parts each
+    const unsigned grid = (unsigned)std::min(items * (block / per), 8192ll);
+    if (head_dim == 128) hipLaunchKernelGGL((tree_merge_kernel<128>), dim3(grid), dim3(256), 0, s, a, parts, block, 4 / p.wr, per, p.row_blocks);
+    else hipLaunchKernelGGL((tree_merge_kernel<64>), dim3(grid), dim3(256), 0, s, a, parts, block, 4 / p.wr, per, p.row_blocks);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

@@ -1,0 +1,10 @@
+// Instances of the attention for drafted tokens on caches of kind MOE_CACHE_BF16.
+#include "tree_attn_kernel.h"
+
+namespace moe {
+
+int launch_tree_bf16(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s) {
+    return launch_tree_kind<MOE_CACHE_BF16>(a, p, head_dim, mt, wr, s);
+}
+
+}  // namespace moe

@@ -1,0 +1,10 @@
+// Instances of the attention for drafted tokens on caches of kind MOE_CACHE_FP4.
+#include "tree_attn_kernel.h"
+
+namespace moe {
+
+int launch_tree_fp4(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s) {
+    return launch_tree_kind<MOE_CACHE_FP4>(a, p, head_dim, mt, wr, s);
+}
+
+}  // namespace moe

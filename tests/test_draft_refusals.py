@@ -34,7 +34,7 @@ def test_rope_arguments():
     for bad in (dict(rows=0), dict(heads=0), dict(x=None), dict(turns=None), dict(pos=None), dict(out=None), dict(x=ODD), dict(turns=ODD), dict(pos=ODD),
                 dict(out=ODD), dict(xs=248), dict(os=248), dict(xs=260), dict(xs=(1 << 24) + 8), dict(xs=-256), dict(x=0x2000, xs=512)):
         assert rope_call(**bad) == -1, bad
-    assert rope_call(rows=(1 << 30) + 1) == -2
+    assert rope_call(rows=(1 << 24) + 1) == -2
     lib, r = B.load_library(), B.make_rope(128, 64, "half", "bf16")
     assert lib.moe_rope(None, 4, 2, FAKE, 256, FAKE, FAKE, FAKE, 256, None) == -1
     assert lib.moe_rope_frequencies(ctypes.byref(r), None) == -1 and lib.moe_rope_frequencies(None, (ctypes.c_double * 64)()) == -1
@@ -86,7 +86,7 @@ def test_cache_arguments():
         for bad in (dict(rows=0), dict(rows=-1), dict(k=None), dict(v=None), dict(seq=None), dict(pos=None), dict(kc=None), dict(vc=None), dict(k=ODD),
                     dict(v=ODD), dict(seq=ODD), dict(pos=ODD), dict(kc=ODD), dict(vc=ODD), dict(ks=248), dict(vs=252), dict(vs=260), dict(ks=0)):
             assert write_call(c, **{**scales, **bad}) == -1, bad
-        assert write_call(c, **{**scales, "rows": (1 << 30) + 1}) == -2
+        assert write_call(c, **{**scales, "rows": (1 << 24) + 1}) == -2
         wrong = [dict(kx=FAKE, vx=None), dict(kx=None, vx=FAKE), dict(kx=FAKE, vx=FAKE)] if kind == 0 else [dict(kx=None), dict(vx=None), dict(kx=ODD)]
         for bad in wrong:
             assert write_call(c, **bad) == -1 and tree_call(c, **bad) == -1, bad
