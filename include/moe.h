@@ -368,7 +368,8 @@ int moe_cache_read(const moe_cache_shape_t* cache, int32_t n_rows, const void* k
  *         sees nothing.  Rows from counts[b] on stay as they are.
  * Keys and values that a token does not see have no part in its result, whatever they hold.  Softmax statistics and sums
  * are in 32 bits; the probabilities are rounded to bf16 for the product with the values.  The caches are only read.
- * n_seq * n_draft * n_heads is below 2^31.  ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */
+ * n_seq * n_draft * n_heads is below 2^31, and 2^30 is above the steps of 32 positions that the longest lengths take: n_seq *
+ * n_kv_heads * ceil(max_len / 32 + n_draft / 32), times what 128 go into n_draft * n_heads / n_kv_heads.  ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */
 size_t moe_tree_attention_workspace_bytes(const moe_cache_shape_t* cache, int32_t n_draft);
 int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const void* q, int64_t q_stride, const void* k,
                        int64_t k_stride, const void* v, int64_t v_stride, const void* k_cache, const void* v_cache,

@@ -413,25 +413,41 @@ def moe_decode_block_forward(shape, block, weights: dict, x, k_cache, v_cache, p
 
 # ---- several new tokens per sequence ---------------------------------------------------------------------------
 
-def _here(*tensors) -> None:
-    """The launch goes to the current device: tensors of another one are refused."""
+# A step makes several of these calls for a few microseconds of kernels each, so a tensor is looked at once, and what is wrong
+# with it is worked out only for the error.
+
+def _refuse(t, dtype, numel, name: str):
     device = torch._C._cuda_getDevice()
-    for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != device:
-            raise ValueError(f"tensor on {t.device}, the current device is cuda:{device}")
-
-
-def _rows(t: torch.Tensor, dtype: torch.dtype, rows: int, cols: int, name: str):
-    """(address, distance between rows in elements) of [rows, cols], whose rows may be columns of wider ones."""
     if not t.is_cuda:
         raise ValueError(f"{name}: device tensor required")
-    if t.dtype != dtype:
+    if t.get_device() != device:
+        raise ValueError(f"{name}: on cuda:{t.get_device()}, the launch goes to the current device cuda:{device}")
+    if t.dtype is not dtype:
         raise ValueError(f"{name}: expected {dtype}, got {t.dtype}")
-    if tuple(t.shape) != (rows, cols):
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: contiguous tensor required")
+    raise ValueError(f"{name}: expected {numel} elements for this shape, got {t.numel()}")
+
+
+def _at(t, device: int, dtype, numel: int, name: str):
+    """Address of a contiguous tensor on the current device, or None."""
+    if t is None:
+        return None
+    if t.get_device() != device or t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+        _refuse(t, dtype, numel, name)
+    return t.data_ptr()
+
+
+def _rows(t, device: int, dtype, rows: int, cols: int, name: str):
+    """(address, distance between rows in elements) of [rows, cols], whose rows may be columns of wider ones."""
+    if t.get_device() != device or t.dtype is not dtype:
+        _refuse(t, dtype, rows * cols, name)
+    if t.shape != (rows, cols):
         raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
-    if t.stride(1) != 1 and cols > 1:
+    between, inside = t.stride()
+    if inside != 1 and cols > 1:
         raise ValueError(f"{name}: the elements of a row have to be adjacent")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), between if rows > 1 else cols
 
 
 def make_rope(head_dim: int, rot_dim: int, layout, dtype, base: float = 10000.0, amplitude: float = 1.0, scaling="plain",
@@ -463,11 +479,11 @@ def moe_rope(rope: MoeRope, x, turns, pos, out) -> None:
         return
     if cols == 0 or cols % rope.head_dim:
         raise ValueError(f"x: {cols} columns are no heads of {rope.head_dim}")
-    _here(x, turns, pos, out)
-    xp, xs = _rows(x, dtype, rows, cols, "x")
-    op, os_ = _rows(out, dtype, rows, cols, "out")
-    rc = load_library().moe_rope(ctypes.byref(rope), rows, cols // rope.head_dim, xp, xs, _ptr(turns, torch.float64, rope.rot_dim // 2, "turns"),
-                                 _ptr(pos, torch.int32, rows, "pos"), op, os_, _stream())
+    dev = torch._C._cuda_getDevice()
+    xp, xs = _rows(x, dev, dtype, rows, cols, "x")
+    op, os_ = _rows(out, dev, dtype, rows, cols, "out")
+    rc = load_library().moe_rope(ctypes.byref(rope), rows, cols // rope.head_dim, xp, xs, _at(turns, dev, torch.float64, rope.rot_dim // 2, "turns"),
+                                 _at(pos, dev, torch.int32, rows, "pos"), op, os_, torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_rope", rc)
 
 
@@ -498,15 +514,16 @@ def alloc_cache(cache: MoeCacheShape, device="cuda"):
         *(torch.zeros((B, G, L, dh // 32), dtype=torch.uint8, device=device) for _ in "kv")
 
 
-def _cache_args(cache, k_cache, v_cache, k_scale, v_scale):
+def _cache_args(cache, device: int, k_cache, v_cache, k_scale, v_scale):
+    kind, dh = cache.kind, cache.head_dim
     total = cache.n_seq * cache.n_kv_heads * cache.max_len
-    if cache.kind == MOE_CACHE_BF16:
-        el, n = torch.bfloat16, total * cache.head_dim
+    if kind == MOE_CACHE_BF16:
+        el, n = torch.bfloat16, total * dh
     else:
-        el, n = torch.uint8, total * cache.head_dim // (1 if cache.kind == MOE_CACHE_FP8 else 2)
-    x = total * (cache.head_dim // 32)
-    return (_ptr(k_cache, el, n, "k_cache"), _ptr(v_cache, el, n, "v_cache"), _ptr(k_scale, torch.uint8, x, "k_scale"),
-            _ptr(v_scale, torch.uint8, x, "v_scale"))
+        el, n = torch.uint8, total * dh // (1 if kind == MOE_CACHE_FP8 else 2)
+    x = total * (dh // 32)
+    return (_at(k_cache, device, el, n, "k_cache"), _at(v_cache, device, el, n, "v_cache"), _at(k_scale, device, torch.uint8, x, "k_scale"),
+            _at(v_scale, device, torch.uint8, x, "v_scale"))
 
 
 def moe_cache_write(cache, k, v, seq, pos, k_cache, v_cache, k_scale, v_scale) -> None:
@@ -514,10 +531,10 @@ def moe_cache_write(cache, k, v, seq, pos, k_cache, v_cache, k_scale, v_scale) -
     rows, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
     if rows == 0:
         return
-    _here(k, v, seq, pos, k_cache, v_cache, k_scale, v_scale)
+    dev, bf = torch._C._cuda_getDevice(), torch.bfloat16
     rc = load_library().moe_cache_write(
-        ctypes.byref(cache), rows, *_rows(k, torch.bfloat16, rows, cols, "k"), *_rows(v, torch.bfloat16, rows, cols, "v"),
-        _ptr(seq, torch.int32, rows, "seq"), _ptr(pos, torch.int32, rows, "pos"), *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _stream())
+        ctypes.byref(cache), rows, *_rows(k, dev, bf, rows, cols, "k"), *_rows(v, dev, bf, rows, cols, "v"), _at(seq, dev, torch.int32, rows, "seq"),
+        _at(pos, dev, torch.int32, rows, "pos"), *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_cache_write", rc)
 
 
@@ -526,10 +543,11 @@ def moe_cache_read(cache, k_cache, v_cache, k_scale, v_scale, seq, pos, k, v) ->
     rows, cols = k.shape[0], cache.n_kv_heads * cache.head_dim
     if rows == 0:
         return
-    _here(k, v, seq, pos, k_cache, v_cache, k_scale, v_scale)
+    dev, bf = torch._C._cuda_getDevice(), torch.bfloat16
     rc = load_library().moe_cache_read(
-        ctypes.byref(cache), rows, *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _ptr(seq, torch.int32, rows, "seq"),
-        _ptr(pos, torch.int32, rows, "pos"), *_rows(k, torch.bfloat16, rows, cols, "k"), *_rows(v, torch.bfloat16, rows, cols, "v"), _stream())
+        ctypes.byref(cache), rows, *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), _at(seq, dev, torch.int32, rows, "seq"),
+        _at(pos, dev, torch.int32, rows, "pos"), *_rows(k, dev, bf, rows, cols, "k"), *_rows(v, dev, bf, rows, cols, "v"),
+        torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_cache_read", rc)
 
 
@@ -545,14 +563,17 @@ def _tree_workspace_need(cache: bytes, n_draft: int) -> int:
 def moe_tree_attention(cache, n_draft: int, q, k, v, k_cache, v_cache, k_scale, v_scale, lens, counts, tree, out, ws) -> None:
     """q, out: [n_seq * n_draft, n_heads * head_dim], k, v: [n_seq * n_draft, n_kv_heads * head_dim] bf16, columns of wider rows if
     need be; counts and tree may be None."""
-    bf, i32 = torch.bfloat16, torch.int32
-    T, qw, kw = cache.n_seq * n_draft, cache.n_heads * cache.head_dim, cache.n_kv_heads * cache.head_dim
-    _here(q, k, v, k_cache, v_cache, k_scale, v_scale, lens, counts, tree, out, ws)
-    wsp, wsn = _ws(cache, ws, _tree_workspace_need(bytes(cache), n_draft))
+    bf, i32, dev = torch.bfloat16, torch.int32, torch._C._cuda_getDevice()
+    B, dh = cache.n_seq, cache.head_dim
+    T, qw, kw = B * n_draft, cache.n_heads * dh, cache.n_kv_heads * dh
+    need, nbytes = _tree_workspace_need(bytes(cache), n_draft), 0 if ws is None else ws.numel() * ws.element_size()
+    if nbytes < need:
+        raise ValueError(f"workspace: {nbytes} bytes, this shape needs {need}")
     rc = load_library().moe_tree_attention(
-        ctypes.byref(cache), n_draft, *_rows(q, bf, T, qw, "q"), *_rows(k, bf, T, kw, "k"), *_rows(v, bf, T, kw, "v"),
-        *_cache_args(cache, k_cache, v_cache, k_scale, v_scale), _ptr(lens, i32, cache.n_seq, "lens"), _ptr(counts, i32, cache.n_seq, "counts"),
-        _ptr(tree, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, bf, T, qw, "out"), wsp, wsn, _stream())
+        ctypes.byref(cache), n_draft, *_rows(q, dev, bf, T, qw, "q"), *_rows(k, dev, bf, T, kw, "k"), *_rows(v, dev, bf, T, kw, "v"),
+        *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), _at(lens, dev, i32, B, "lens"), _at(counts, dev, i32, B, "counts"),
+        _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, dev, bf, T, qw, "out"), _at(ws, dev, ws.dtype, ws.numel(), "ws"), nbytes,
+        torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_tree_attention", rc)
 
 

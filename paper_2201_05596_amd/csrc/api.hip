@@ -1199,6 +1199,7 @@ int check_tree(const moe_cache_shape_t* c, int32_t n_draft) {
     if (rc != MOE_OK) return rc;
     if (n_draft < 1) return MOE_ERR_INVALID_ARG;
     if (n_draft > kMaxDraft || (long long)c->n_seq * n_draft * c->n_heads >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
+    if (tree_attn_steps(c, n_draft) >= (1ll << 30)) return MOE_ERR_UNSUPPORTED;
     return MOE_OK;
 }
 

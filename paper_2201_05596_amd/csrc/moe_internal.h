@@ -363,6 +363,7 @@ struct TreeArgs {
     int n_seq, N, H, G, max_len;       // N drafted tokens per sequence
 };
 size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft);
+long long tree_attn_steps(const moe_cache_shape_t* c, int n_draft);     // work of the largest call of a shape; below 2^30
 int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s);
 
 }  // namespace moe

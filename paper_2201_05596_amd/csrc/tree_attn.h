@@ -14,22 +14,26 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;              // positions per step of a wave; one word of a row's mask
+constexpr int kItemSteps = 8;          // what an item's beginning and end take, in steps
+constexpr int kLeastSteps = 4;         // steps of a wave below which an item is not cut
 constexpr float kLowest = -3.40282347e38f;
 
 struct TreePlan {                      // how the host sets a call up
-    int mt, wr;                        // 16-row tiles per wave, waves with rows of their own (the other factor of 4 splits positions)
-    int groups;                        // work-groups
+    int mt, wr;                        // 16-row tiles per wave; waves with rows of their own, the other factor of 4 splits positions
+    int groups;                        // work-groups, a multiple of 8
     int row_blocks;                    // blocks of 16 mt wr rows per key/value head, at most
-    size_t partial_bytes;
+    size_t partial_bytes, ml_bytes;
 };
 
 // ---- the share of a work-group ----------------------------------------------------------------------------------
 // A sequence has G x (blocks of ROWS rows) items of `tiles` steps each: ceil(len / 32) over the cache, ceil(count / 32) over the
-// drafted tokens.  All items' steps in a row are cut into equal shares, so that work-groups take as long as each other whatever
-// the lengths are; an item that lies in several shares is merged from its parts by tree_merge_kernel.
+// drafted tokens; an item's beginning and end count as kItemSteps more, ahead of its own.  All items' steps in a row are cut into
+// equal shares, so that work-groups take as long as each other whatever the lengths are; an item that lies in several shares is
+// merged from its parts by tree_merge_kernel.  The host refuses shapes with 2^30 steps.
 struct Sequence {
     int len, count, cached, tiles;     // cached: steps over the cache
-    long long items;
+    int blocks, items;                 // blocks of rows per key/value head
+    __device__ __forceinline__ int item_steps() const { return tiles + kItemSteps; }
 };
 __device__ __forceinline__ Sequence sequence(const TreeArgs& a, int b, int ROWS) {
     Sequence s;
@@ -37,9 +41,19 @@ __device__ __forceinline__ Sequence sequence(const TreeArgs& a, int b, int ROWS)
     s.count = a.counts ? min(max(a.counts[b], 0), a.N) : a.N;
     s.cached = (s.len + kTile - 1) / kTile;
     s.tiles = s.cached + (s.count + kTile - 1) / kTile;
-    s.items = (long long)a.G * ((s.count * (a.H / a.G) + ROWS - 1) / ROWS);
+    s.blocks = (s.count * (a.H / a.G) + ROWS - 1) / ROWS;
+    s.items = a.G * s.blocks;
     return s;
 }
+
+struct TreeParts {                     // workspace: parts of items that lie in several shares
+    float* o;                          // [slot][ROWS][DH]
+    float* ml;                         // [slot][ROWS][2]: maximum (times c), sum
+    int4* split;                       // per share: the item that begins and does not end in it: sequence (-1: none), item, last share, slot
+    int groups;
+};
+// where share `w` puts its part of an item that is not all its own: its first part, or the last one
+__device__ __forceinline__ size_t partial_slot(int w, bool first) { return 2 * (size_t)w + (first ? 0 : 1); }
 
 // The drafted tokens j0 .. j0 + 31 that token `tok` sees, a bit each
 __device__ __forceinline__ uint32_t seen_word(const TreeArgs& a, const Sequence& s, int b, int tok, int j0) {
@@ -54,48 +68,52 @@ __device__ __forceinline__ bool sees_anything(const TreeArgs& a, const Sequence&
     return s.len > 0;
 }
 
-struct TreeParts {                     // workspace: parts of items that lie in several shares
-    float* o;                          // [slot][ROWS][DH]
-    float* ml;                         // [slot][ROWS][2]: maximum, sum
-    int groups;
+struct Share {
+    int begin, end, size;              // steps of all items in a row; size: of a whole share
+    int b, off;                        // the sequence that holds step `begin`, and that step in it
 };
 
-struct Shares { long long total, size; };
-
-// Sum and maximum over 256 threads; sh: 8 words of LDS
-__device__ __forceinline__ void block_sum_max(long long& sum, int& most, long long* sh, int tid) {
+// The share of work-group `w`, by each wave.  wp: positions are split over so many waves.
+__device__ __forceinline__ Share share_of(const TreeArgs& a, int ROWS, int groups, int wp, int w, int lane) {
+    auto steps = [&](int b, int& tiles) {
+        const Sequence s = sequence(a, min(b, a.n_seq - 1), ROWS);
+        tiles = b < a.n_seq && s.items ? s.item_steps() : 0;
+        return s.items * tiles;
+    };
+    int tiles, most, mine = steps(lane, most), total = mine;
+    for (int b = lane + kWave; b < a.n_seq; b += kWave) {
+        total += steps(b, tiles);
+        most = max(most, tiles);
+    }
 #pragma unroll
     for (int x = 32; x >= 1; x >>= 1) {
-        sum += __shfl_xor(sum, x);
+        total += __shfl_xor(total, x);
         most = max(most, __shfl_xor(most, x));
     }
-    if (tid % kWave == 0) { sh[tid / kWave] = sum; sh[4 + tid / kWave] = most; }
-    __syncthreads();
-    sum = sh[0] + sh[1] + sh[2] + sh[3];
-    most = max(max((int)sh[4], (int)sh[5]), max((int)sh[6], (int)sh[7]));
-    __syncthreads();
-}
-
-// least: steps below which a share is not worth a work-group of its own (an item that is shorter is not cut)
-__device__ __forceinline__ Shares shares(const TreeArgs& a, int ROWS, int groups, int wp, long long* sh, int tid) {
-    long long total = 0;
-    int most = 0;
-    for (int b = tid; b < a.n_seq; b += 256) {
-        const Sequence s = sequence(a, b, ROWS);
-        total += s.items * s.tiles;
-        if (s.items) most = max(most, s.tiles);
-    }
-    block_sum_max(total, most, sh, tid);
-    Shares r;
-    r.total = total;
+    total = __builtin_amdgcn_readfirstlane(total);
+    most = __builtin_amdgcn_readfirstlane(most);
+    Share r;
     r.size = (total + groups - 1) / groups;
     if (r.size > wp) r.size = (r.size + wp - 1) / wp * wp;
-    r.size = max(r.size, (long long)min(most, 4 * wp));
-    r.size = max(r.size, 1ll);
-    return r;
+    r.size = max(r.size, max(1, min(most, kLeastSteps * wp + kItemSteps)));     // shorter items are not cut
+    r.begin = (int)min((long long)w * r.size, (long long)total);
+    r.end = min(r.begin + r.size, total);
+    r.b = r.off = 0;
+    if (r.begin >= r.end) return r;
+    for (int base = 0, b0 = 0;; b0 += kWave) {
+        if (b0) mine = steps(b0 + lane, tiles);
+        int sum = mine;
+#pragma unroll
+        for (int d = 1; d < kWave; d <<= 1) { const int v = __shfl_up(sum, d); sum += lane >= d ? v : 0; }
+        const uint64_t behind = __ballot(r.begin < base + sum);        // the sequences that end behind it
+        if (behind) {
+            const int l = __ffsll((unsigned long long)behind) - 1;
+            r.b = b0 + l;
+            r.off = r.begin - base - __builtin_amdgcn_readlane(sum - mine, l);
+            return r;
+        }
+        base += __builtin_amdgcn_readlane(sum, kWave - 1);
+    }
 }
-
-// Where share `w` puts its part of an item that is not all its own: its first part, or the last one
-__device__ __forceinline__ size_t partial_slot(long long w, bool first) { return 2 * (size_t)w + (first ? 0 : 1); }
 
 }  // namespace moe

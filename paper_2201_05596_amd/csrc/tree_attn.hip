@@ -9,63 +9,70 @@ int launch_tree_bf16(const TreeArgs& a, const TreeParts& p, int head_dim, int mt
 int launch_tree_fp8(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s);
 int launch_tree_fp4(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s);
 
-// out of the parts of every item that lies in more than one share.  A work-group takes `per` rows of an item; 16 threads share
-// a row (DH / 16 elements each), the other factor of 256 takes every so many parts and is added up in LDS.
-template <int DH>
-__global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a, const TreeParts parts, int ROWS, int wp, int per, int blocks_per_head) {
+// out of the parts of every item that lies in more than one share; the share in which it begins says which.  A work-group takes
+// 16 rows of one share's item; 16 threads share a row (DH / 16 elements each), SETS such groups take every so many parts and are
+// added up in LDS.
+template <int DH, int SETS>
+__global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a, const TreeParts parts, int ROWS) {
     constexpr int NF = DH / 16;
-    __shared__ long long sh[8];
-    __shared__ float ml[16][16][2], o[16][16][NF];            // [part set][row] and, per thread, its sums
-    const int tid = threadIdx.x, R = a.H / a.G;
-    const int chunks = ROWS / per;
-    const Shares share = shares(a, ROWS, parts.groups, wp, sh, tid);
-    for (long long bx = blockIdx.x; bx < (long long)a.n_seq * a.G * blocks_per_head * chunks; bx += gridDim.x) {
-    const int chunk = (int)(bx % chunks), block = (int)(bx / chunks % blocks_per_head), g = (int)(bx / chunks / blocks_per_head % a.G);
-    const int b = (int)(bx / chunks / blocks_per_head / a.G);
+    __shared__ float ml[SETS][16][2], o[SETS][16][16][NF];
+    const int R = a.H / a.G, w0 = blockIdx.x;
+    const int4 split = parts.split[w0];
+    if (split.x < 0) return;
+    const int b = split.x, w1 = split.z;
     const Sequence s = sequence(a, b, ROWS);
-    const int rows = s.count * R, row0 = block * ROWS + chunk * per;
-    if (row0 >= rows) continue;
-    long long before = 0;                                     // steps of the sequences before b
-    int unused = 0;
-    for (int i = tid; i < b; i += 256) { const Sequence t = sequence(a, i, ROWS); before += t.items * t.tiles; }
-    block_sum_max(before, unused, sh, tid);
-    const long long first = before + ((long long)g * (s.items / a.G) + block) * s.tiles, last = first + s.tiles - 1;
-    const long long w0 = first / share.size, w1 = last / share.size;
-    if (w0 == w1) continue;
-    const int piece = tid % 16, local = tid / 16 % per, set = tid / 16 / per, sets = 16 / per;
-    const int row = row0 + local, in_block = chunk * per + local;
+    const int g = split.y / s.blocks, block = split.y - g * s.blocks, rows = s.count * R, row0 = block * ROWS + blockIdx.y * 16;
+    if (row0 >= rows) return;
+    const int tid = threadIdx.x, piece = tid % 16, local = tid / 16 % 16, set = tid / 256;
+    const int row = row0 + local, in_block = blockIdx.y * 16 + local;
     float M = kLowest, L = 0.f, v[NF] = {};
-    for (long long w = w0 + set; w <= w1; w += sets) {
-        const size_t at = partial_slot(w, w > w0 || first == w0 * share.size) * ROWS + in_block;
-        const float2 x = *reinterpret_cast<const float2*>(parts.ml + at * 2);
-        float e[NF];
+    for (int w = w0 + set; w <= w1; w += 4 * SETS) {          // four parts' loads at once; behind the last: the last, with no weight
+        float2 x[4];
+        float e[4][NF], m = M;
 #pragma unroll
-        for (int i = 0; i < NF; i += 4) *reinterpret_cast<float4*>(e + i) = *reinterpret_cast<const float4*>(parts.o + at * DH + piece * NF + i);
-        const float m = fmaxf(M, x.x), f = __builtin_amdgcn_exp2f(M - m), h = __builtin_amdgcn_exp2f(x.x - m);
+        for (int u = 0; u < 4; ++u) {
+            const int wu = min(w + u * SETS, w1);
+            const size_t at = (wu > w0 ? partial_slot(wu, true) : (size_t)split.w) * ROWS + in_block;
+            x[u] = *reinterpret_cast<const float2*>(parts.ml + at * 2);
+#pragma unroll
+            for (int i = 0; i < NF; i += 4) *reinterpret_cast<float4*>(e[u] + i) = *reinterpret_cast<const float4*>(parts.o + at * DH + piece * NF + i);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) m = w + u * SETS <= w1 ? fmaxf(m, x[u].x) : m;
+        const float f = __builtin_amdgcn_exp2f(M - m);
         M = m;
-        L = L * f + x.y * h;
+        L *= f;
 #pragma unroll
-        for (int i = 0; i < NF; ++i) v[i] = v[i] * f + e[i] * h;
+        for (int i = 0; i < NF; ++i) v[i] *= f;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (w + u * SETS > w1) break;
+            const float h = __builtin_amdgcn_exp2f(x[u].x - m);
+            L += x[u].y * h;
+#pragma unroll
+            for (int i = 0; i < NF; ++i) v[i] += e[u][i] * h;
+        }
     }
-    if (sets > 1) {
+    if constexpr (SETS > 1) {
         if (piece == 0) { ml[set][local][0] = M; ml[set][local][1] = L; }
 #pragma unroll
-        for (int i = 0; i < NF; ++i) o[tid / 16][piece][i] = v[i];
+        for (int i = 0; i < NF; ++i) o[set][local][piece][i] = v[i];
         __syncthreads();
+        if (set) return;
         const float own = M;
-        for (int i = 1; i < sets; ++i) M = fmaxf(M, ml[i][local][0]);
+        for (int i = 1; i < SETS; ++i) M = fmaxf(M, ml[i][local][0]);
         float f = __builtin_amdgcn_exp2f(own - M);
         L *= f;
 #pragma unroll
         for (int j = 0; j < NF; ++j) v[j] *= f;
-        for (int i = 1; i < sets; ++i) {
+        for (int i = 1; i < SETS; ++i) {
             f = __builtin_amdgcn_exp2f(ml[i][local][0] - M);
             L += ml[i][local][1] * f;
 #pragma unroll
-            for (int j = 0; j < NF; ++j) v[j] += o[i * per + local][piece][j] * f;
+            for (int j = 0; j < NF; ++j) v[j] += o[i][local][piece][j] * f;
         }
     }
-    if (set || row >= rows) continue;
+    if (row >= rows) return;
     const int tok = row / R;
     float none = 0.f;                                         // a row of sum 0: 0 if it sees nothing, NaN if all its scores are -inf
     if (L == 0.f && sees_anything(a, s, b, tok)) none = __uint_as_float(0x7fc00000u);
@@ -76,37 +83,50 @@ __global__ __launch_bounds__(256) void tree_merge_kernel(const TreeArgs a, const
     uint16_t* dst = a.out + ((long long)b * a.N + tok) * a.out_stride + (g * R + row - tok * R) * DH + piece * NF;
     if constexpr (DH == 128) *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
     else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
-    }
 }
 
-static TreePlan tree_plan(int n_seq, int G, int R, int N, int head_dim) {
+static TreePlan tree_plan(int R, int N, int head_dim) {
     const int rows = N * R;                                   // at most, per key/value head
     TreePlan p;
-    p.mt = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
-    p.wr = rows <= 32 ? 1 : rows <= 128 ? 2 : 4;
-    p.groups = p.mt == 1 ? 768 : p.mt == 2 ? 512 : 256;
+    p.mt = rows <= 16 ? 1 : 2;
+    p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    p.groups = 512;
     const int block = 16 * p.mt * p.wr;
     p.row_blocks = (rows + block - 1) / block;
     p.partial_bytes = (size_t)2 * p.groups * block * head_dim * sizeof(float);
+    p.ml_bytes = (size_t)2 * p.groups * block * 2 * sizeof(float);
     return p;
 }
 size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft) {
-    const TreePlan p = tree_plan(c->n_seq, c->n_kv_heads, c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
-    return p.partial_bytes + (size_t)2 * p.groups * 16 * p.mt * p.wr * 2 * sizeof(float);
+    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
+    return p.partial_bytes + p.ml_bytes + (size_t)p.groups * sizeof(int4);
+}
+// steps of all items together, at most
+long long tree_attn_steps(const moe_cache_shape_t* c, int n_draft) {
+    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
+    return (long long)c->n_seq * c->n_kv_heads * p.row_blocks * ((c->max_len + kTile - 1) / kTile + (n_draft + kTile - 1) / kTile + kItemSteps);
 }
 
 int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s) {
-    const TreePlan p = tree_plan(a.n_seq, a.G, a.H / a.G, a.N, head_dim);
-    const TreeParts parts{static_cast<float*>(ws), reinterpret_cast<float*>(static_cast<char*>(ws) + p.partial_bytes), p.groups};
+    const TreePlan p = tree_plan(a.H / a.G, a.N, head_dim);
+    char* at = static_cast<char*>(ws);
+    const TreeParts parts{reinterpret_cast<float*>(at), reinterpret_cast<float*>(at + p.partial_bytes),
+                          reinterpret_cast<int4*>(at + p.partial_bytes + p.ml_bytes), p.groups};
     const int rc = kind == MOE_CACHE_BF16 ? launch_tree_bf16(a, parts, head_dim, p.mt, p.wr, s)
                    : kind == MOE_CACHE_FP8 ? launch_tree_fp8(a, parts, head_dim, p.mt, p.wr, s) : launch_tree_fp4(a, parts, head_dim, p.mt, p.wr, s);
     if (rc != MOE_OK) return rc;
     const int block = 16 * p.mt * p.wr;
     const long long items = (long long)a.n_seq * a.G * p.row_blocks;
-    const int per = items <= 32 ? 1 : items <= 128 ? 4 : 16;  // few items: many parts each
-    const unsigned grid = (unsigned)std::min(items * (block / per), 8192ll);
-    if (head_dim == 128) hipLaunchKernelGGL((tree_merge_kernel<128>), dim3(grid), dim3(256), 0, s, a, parts, block, 4 / p.wr, per, p.row_blocks);
-    else hipLaunchKernelGGL((tree_merge_kernel<64>), dim3(grid), dim3(256), 0, s, a, parts, block, 4 / p.wr, per, p.row_blocks);
+    const dim3 grid((unsigned)p.groups, (unsigned)(std::min(block, a.N * (a.H / a.G) + 15) / 16));
+    const bool many = items * 8 <= p.groups;                  // parts per item
+#define MOE_MERGE(DH) \
+    do { \
+        if (many) hipLaunchKernelGGL((tree_merge_kernel<DH, 4>), grid, dim3(1024), 0, s, a, parts, block); \
+        else hipLaunchKernelGGL((tree_merge_kernel<DH, 1>), grid, dim3(256), 0, s, a, parts, block); \
+    } while (0)
+    if (head_dim == 128) MOE_MERGE(128);
+    else MOE_MERGE(64);
+#undef MOE_MERGE
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

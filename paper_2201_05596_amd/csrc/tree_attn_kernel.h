@@ -23,19 +23,22 @@ template <int KIND, int DH> struct Layout {
     }
 };
 
-template <int BYTES> __device__ __forceinline__ void load_raw(const uint8_t* p, uint32_t (&w)[(BYTES + 3) / 4]) {
-    typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-    typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+// Memory from p on, of which `bytes` may be read: loads behind them give 0
+typedef __amdgpu_buffer_rsrc_t Window;
+__device__ __forceinline__ Window window(const void* p, int bytes) {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+}
+template <int BYTES> __device__ __forceinline__ void load_raw(Window p, int at, int plus, uint32_t (&w)[(BYTES + 3) / 4]) {
     if constexpr (BYTES == 16) {
-        const u4 v = *reinterpret_cast<const u4*>(p);
-        w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(p, at, plus, 0);
+        w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3];
     } else if constexpr (BYTES == 8) {
-        const u2 v = *reinterpret_cast<const u2*>(p);
-        w[0] = v.x; w[1] = v.y;
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(p, at, plus, 0);
+        w[0] = v[0]; w[1] = v[1];
     } else if constexpr (BYTES == 4) {
-        w[0] = *reinterpret_cast<const uint32_t*>(p);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(p, at, plus, 0);
     } else {
-        w[0] = *reinterpret_cast<const uint16_t*>(p);
+        w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(p, at, plus, 0);
     }
 }
 
@@ -46,25 +49,27 @@ template <int KIND, int DH> struct CacheTile {
     uint32_t v[8][vw];
     uint32_t ks[2], vs[8];                                        // scale bytes of the rows
 
-    // whole: all 32 positions are there; else `left` of them (at least one): the others read the last one and are not used
-    __device__ __forceinline__ void load(const uint8_t* kc, const uint8_t* vc, const uint8_t* kx, const uint8_t* vx, int left, int lane) {
+    // kc, kx, vc, vx: the tile's positions that are there
+    __device__ __forceinline__ void load_keys(Window kc, Window kx, int lane) {
         const int r = lane & 15, g = lane >> 4;
-        const bool whole = left >= kTile;
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-            const int p = whole ? t * 16 + r : min(t * 16 + r, left - 1);
 #pragma unroll
-            for (int n = 0; n < L::nk; ++n) load_raw<L::kload>(kc + p * L::row + n * 4 * L::kload + g * L::kload, k[t][n]);
+            for (int n = 0; n < L::nk; ++n) load_raw<L::kload>(kc, r * L::row + g * L::kload, t * 16 * L::row + n * 4 * L::kload, k[t][n]);
             if constexpr (KIND != MOE_CACHE_BF16) {
-                if constexpr (L::srow == 4) ks[t] = *reinterpret_cast<const uint32_t*>(kx + p * 4);
-                else ks[t] = *reinterpret_cast<const uint16_t*>(kx + p * 2);
+                uint32_t w[1];
+                load_raw<L::srow>(kx, r * L::srow, t * 16 * L::srow, w);
+                ks[t] = w[0];
             }
         }
+    }
+    __device__ __forceinline__ void load_values(Window vc, Window vx, int lane) {
+        const int c = lane & 15, g = lane >> 4;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const int at = (j >> 2) * 16 + g * 4 + (j & 3), p = whole ? at : min(at, left - 1);
-            load_raw<L::vload>(vc + p * L::row + r * L::vload, v[j]);
-            if constexpr (KIND != MOE_CACHE_BF16) vs[j] = vx[p * L::srow + r * L::srow / 16];
+            const int at = (j >> 2) * 16 + (j & 3);
+            load_raw<L::vload>(vc, g * 4 * L::row + c * L::vload, at * L::row, v[j]);
+            if constexpr (KIND != MOE_CACHE_BF16) vs[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vx, g * 4 * L::srow + c * L::srow / 16, at * L::srow, 0);
         }
     }
 
@@ -86,36 +91,21 @@ template <int KIND, int DH> struct CacheTile {
             }
         }
     }
-    // the row's DH / 16 elements in bf16; `there`: 0 where the position is none
-    __device__ __forceinline__ void value(int j, bool there, uint32_t (&o)[DH / 32]) const {
-        const uint32_t none = there ? ~0u : 0u;
-        if constexpr (KIND == MOE_CACHE_BF16) {
-#pragma unroll
-            for (int i = 0; i < DH / 32; ++i) o[i] = v[j][i] & none;
-        } else {
-            const float f = scale_value(vs[j]);
-            if constexpr (KIND == MOE_CACHE_FP8) {
-#pragma unroll
-                for (int i = 0; i < DH / 64; ++i) { o[2 * i] = fp8_pair<false>(v[j][i], f) & none; o[2 * i + 1] = fp8_pair<true>(v[j][i], f) & none; }
-            } else {
-                o[0] = fp4_pair<0>(v[j][0], f) & none;
-                o[1] = fp4_pair<1>(v[j][0], f) & none;
-                if constexpr (DH == 128) { o[2] = fp4_pair<2>(v[j][0], f) & none; o[3] = fp4_pair<3>(v[j][0], f) & none; }
-            }
-        }
+    // elements 2 i and 2 i + 1 of the lane's DH / 16 of row j, in bf16
+    __device__ __forceinline__ uint32_t value(int j, int i) const {
+        if constexpr (KIND == MOE_CACHE_BF16) return v[j][i];
+        const float f = scale_value(vs[j]);
+        if constexpr (KIND == MOE_CACHE_FP8) return i & 1 ? fp8_pair<true>(v[j][i / 2], f) : fp8_pair<false>(v[j][i / 2], f);
+        return i == 0 ? fp4_pair<0>(v[j][0], f) : i == 1 ? fp4_pair<1>(v[j][0], f) : i == 2 ? fp4_pair<2>(v[j][0], f) : fp4_pair<3>(v[j][0], f);
     }
 };
 
-// rows[8][DH / 32]: DH / 16 elements of eight positions -> operands of V^T: fragment q is element q of each
-template <int DH> __device__ __forceinline__ void transpose(const uint32_t (&rows)[8][DH / 32], uint4 (&f)[DH / 16]) {
+// pairs[8]: two elements of eight positions each -> the operand of V^T for the first (HIGH: the second) of them
+template <bool HIGH> __device__ __forceinline__ uint4 gather(const uint32_t (&pairs)[8]) {
+    uint32_t w[4];
 #pragma unroll
-    for (int q = 0; q < DH / 16; ++q) {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)      // low or high halves of two positions' words
-            w[j] = __builtin_amdgcn_perm(rows[2 * j + 1][q / 2], rows[2 * j][q / 2], q & 1 ? 0x07060302u : 0x05040100u);
-        f[q] = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(pairs[2 * j + 1], pairs[2 * j], HIGH ? 0x07060302u : 0x05040100u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 __device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, f32x4 c) {
@@ -124,104 +114,147 @@ __device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, f32x4 c) {
 
 // over the four lanes that hold a row
 __device__ __forceinline__ float row_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
-__device__ __forceinline__ float row_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 
 template <int DH, int MT> struct Rows {          // a wave's rows: lane (n, g) holds row n of every 16, elements (4 g + i) DH / 16 + q in o[.][q][i]
     f32x4 o[MT][DH / 16];
-    float m[MT], l[MT];                          // l: of the lane's own positions
-    __device__ __forceinline__ void clear() {
+    f32x4 l[MT];                                 // sums, by a product with ones: the same in every element, the first one is kept
+    float m[MT], mc[MT];                         // maximum score, and c times it
+    __device__ __forceinline__ void clear(float c) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             m[t] = kLowest;
-            l[t] = 0.f;
+            mc[t] = kLowest * c;
+            l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int q = 0; q < DH / 16; ++q) o[t][q] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
 };
 
-// A tile's scores -> probabilities (as the second product's operand).  seen: bits of the row's 32 positions, only with MASKED.
-// The maximum moves only when a score exceeds it by 2^8: until then probabilities are at most 2^8, which sums in 32 bits and
-// bf16's range take, and neither the rows' lanes nor the sums have to be touched.
-template <int DH, int MT, bool MASKED>
-__device__ __forceinline__ uint4 probabilities(Rows<DH, MT>& r, int t, f32x4 (&s)[2], float c, uint32_t seen, int g) {
-    float x[8], top = -INFINITY;
+// A tile's scores -> probabilities (as the second product's operands).  The maximum moves only when a score exceeds it by 2^8:
+// until then probabilities are at most 2^8, which sums in 32 bits and bf16's range take, and neither the rows' lanes nor the
+// sums have to be touched.  ahead: 8 / c.
+template <int DH, int MT>
+__device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, float ahead, uint4 (&out)[MT]) {
+    bool grows = false;
+    float top[MT];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        x[i] = s[i / 4][i % 4] * c;
-        if (MASKED && !(seen >> ((i / 4) * 16 + g * 4 + i % 4) & 1u)) x[i] = -INFINITY;
-        top = fmaxf(top, x[i]);
-    }
-    if (__any(top > r.m[t] + 8.f)) {
-        const float m = fmaxf(r.m[t], row_max(top)), f = __builtin_amdgcn_exp2f(r.m[t] - m);
-        r.m[t] = m;
-        r.l[t] *= f;
+    for (int t = 0; t < MT; ++t) {
+        top[t] = s[t][0][0];
 #pragma unroll
-        for (int q = 0; q < DH / 16; ++q) r.o[t][q] *= f;
+        for (int i = 1; i < 8; ++i) top[t] = fmaxf(top[t], s[t][i / 4][i % 4]);
+        grows |= top[t] > r.m[t] + ahead;
     }
-    float p[8];
+    if (__any(grows)) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(x[i] - r.m[t]);
-        r.l[t] += p[i];
+        for (int t = 0; t < MT; ++t) {
+            const float m = fmaxf(r.m[t], row_max(top[t])), f = __builtin_amdgcn_exp2f((r.m[t] - m) * c);
+            r.m[t] = m;
+            r.mc[t] = m * c;
+            r.l[t][0] *= f;
+#pragma unroll
+            for (int q = 0; q < DH / 16; ++q) r.o[t][q] *= f;
+        }
     }
-    return make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+    const uint32_t one = 0x3f803f80u;
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        float p[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i / 4][i % 4], c, -r.mc[t]));
+        out[t] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+        r.l[t] = mfma(make_uint4(one, one, one, one), out[t], r.l[t]);
+    }
+}
+
+// bits of the row's 32 positions that it sees: the others have no score
+__device__ __forceinline__ void mask_scores(f32x4 (&s)[2], uint32_t seen, int g) {
+    seen >>= 4 * g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (!(seen & (1u << (i / 4 * 16 + i % 4)))) s[i / 4][i % 4] = -INFINITY;
 }
 
 template <int KIND, int DH, int MT, int WR>
-__global__ __launch_bounds__(256) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
+__global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
     typedef Layout<KIND, DH> L;
     constexpr int WP = 4 / WR, QT = 16 * MT, ROWS = QT * WR, KS = DH / 32, NF = DH / 16, OS = DH + 4;
-    __shared__ long long sh[8];
-    __shared__ long long found[2];
-    extern __shared__ float lds[];                    // WP > 1: [4][QT][OS] and [4][QT][2]
+    constexpr bool SHARED = WR > 1;                   // a tile is in operand order in LDS, for all waves; else in its own wave's registers
+    extern __shared__ uint4 lds16[];                  // SHARED: [4 tiles][2 KS + NF][64]; WP > 1, behind the steps: [4][QT][OS] and [4][QT][2] floats
+    float* lds = reinterpret_cast<float*>(lds16);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WP, wp = wave % WP, n = lane & 15, g4 = lane >> 4;
     const int R = a.H / a.G;
-    const float c = 1.44269504f * rsqrtf((float)DH);
+    const float c = 1.44269504f * rsqrtf((float)DH), ahead = 8.f / c;
 
-    const Shares share = shares(a, ROWS, parts.groups, WP, sh, tid);
     // consecutive shares on one XCD: they read the same keys and values where an item's rows take several blocks
-    const long long w = (blockIdx.x % 8) * (long long)(parts.groups / 8) + blockIdx.x / 8;
-    long long x = w * share.size;
-    const long long end = min(x + share.size, share.total), begin = x;
-    if (x >= end) return;
-
-    // the sequence that holds step x
-    int b = 0;
-    long long off = 0;                                // step x in the sequence
-    {
-        long long base = 0;
-        for (int b0 = 0;; b0 += 256) {
-            long long mine = 0;
-            if (b0 + tid < a.n_seq) { const Sequence s = sequence(a, b0 + tid, ROWS); mine = s.items * s.tiles; }
-            long long sum = mine;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) { const long long v = __shfl_up(sum, d); if (lane >= d) sum += v; }
-            if (lane == 63) sh[tid >> 6] = sum;
-            __syncthreads();
-            for (int i = 0; i < (tid >> 6); ++i) sum += sh[i];
-            const long long all = sh[0] + sh[1] + sh[2] + sh[3];
-            if (x < base + all) {
-                if (x >= base + sum - mine && x < base + sum) { found[0] = b0 + tid; found[1] = base + sum - mine; }
-                __syncthreads();
-                b = __builtin_amdgcn_readfirstlane((int)found[0]);
-                off = x - found[1];
-                break;
-            }
-            base += all;
-            __syncthreads();
-        }
+    const int w = (blockIdx.x % 8) * (parts.groups / 8) + blockIdx.x / 8;
+    const Share share = share_of(a, ROWS, parts.groups, WP, w, lane);
+    const int begin = share.begin, end = share.end;
+    int4 split = make_int4(-1, 0, 0, 0);
+    if (begin >= end) {
+        if (tid == 0) parts.split[w] = split;
+        return;
     }
+    struct Piece {                                    // a share's part of an item
+        Sequence s;
+        int b, off, t0, steps, g, row0, cached;       // off: the step behind it in the sequence
+        bool first;                                   // it begins where the share does
+        const uint8_t *kc, *vc, *kx, *vx;
+    };
+    // from p.s, p.b and p.off on, with `left` steps in the share; p.steps: 0 if there is none
+    auto piece = [&](Piece& p, int& left) {
+        p.steps = 0;
+        int item, ahead;
+        for (;; left -= ahead, p.off += ahead) {      // parts of an item's beginning alone are none
+            if (left <= 0) { left = 0; p.cached = p.t0 = 0; return; }
+            while (p.off >= p.s.items * p.s.item_steps()) { p.off = 0; p.s = sequence(a, ++p.b, ROWS); }
+            item = p.off / p.s.item_steps();
+            const int at = p.off - item * p.s.item_steps();
+            p.t0 = max(at - kItemSteps, 0);
+            ahead = min(max(kItemSteps - at, 0), left);
+            if (left > ahead) break;
+        }
+        p.first = left == end - begin;
+        left -= ahead;
+        p.off += ahead;
+        p.steps = min(p.s.tiles - p.t0, left);
+        left -= p.steps;
+        p.off += p.steps;
+        p.g = item / p.s.blocks;
+        p.row0 = (item - p.g * p.s.blocks) * ROWS + wr * QT;
+        p.cached = min(p.t0 + p.steps, p.s.cached);
+        const long long head = ((long long)p.b * a.G + p.g) * a.max_len;
+        p.kc = static_cast<const uint8_t*>(a.k_cache) + head * L::row;
+        p.vc = static_cast<const uint8_t*>(a.v_cache) + head * L::row;
+        p.kx = KIND == MOE_CACHE_BF16 ? nullptr : a.k_scale + head * L::srow;
+        p.vx = KIND == MOE_CACHE_BF16 ? nullptr : a.v_scale + head * L::srow;
+        // the share that holds the item's last step: as many steps behind this part as are left of it
+        if (p.t0 == 0 && p.steps < p.s.tiles)
+            split = make_int4(p.b, item, w + (p.s.tiles - p.steps + share.size - 1) / share.size, (int)partial_slot(w, p.first));
+    };
+    // Keys and values of the next step are loaded into the registers that a step is done with; behind the last step nothing is
+    // read (an empty window), so that loads are no branches and their waits are counted
+    CacheTile<KIND, DH> tile;
+    auto there = [&](const Piece& p, const uint8_t* at, int t, int row) {
+        return window(at + (long long)t * (kTile * row), t < p.cached ? min(p.s.len - t * kTile, kTile) * row : 0);
+    };
+    auto load_keys = [&](const Piece& p, int t) { tile.load_keys(there(p, p.kc, t, L::row), there(p, p.kx, t, L::srow), lane); };
+    auto load_values = [&](const Piece& p, int t) { tile.load_values(there(p, p.vc, t, L::row), there(p, p.vx, t, L::srow), lane); };
+    const int mine = SHARED ? wave : wp;              // the wave's tile of the first steps
 
-    Sequence s = sequence(a, b, ROWS);
-    while (x < end) {
-        while (off >= s.items * s.tiles) { off = 0; s = sequence(a, ++b, ROWS); }
-        const int item = (int)(off / s.tiles), t0 = (int)(off - (long long)item * s.tiles);
-        const int steps = (int)min((long long)(s.tiles - t0), end - x);
-        const int blocks = (int)(s.items / a.G), g = item / blocks, row0 = (item - g * blocks) * ROWS + wr * QT;
-        const int rows = s.count * R;
-
+    Piece next;
+    next.b = share.b;
+    next.off = share.off;
+    next.s = sequence(a, next.b, ROWS);
+    int left_steps = end - begin;
+    piece(next, left_steps);
+    load_keys(next, next.t0 + mine);
+    load_values(next, next.t0 + mine);
+    while (next.steps) {
+        const Piece now = next;
+        const Sequence& s = now.s;
+        const int b = now.b, g = now.g, row0 = now.row0, t0 = now.t0, steps = now.steps, cached = now.cached, rows = s.count * R;
         // queries, in the order that the cache's elements come in
         uint4 q[MT][KS];
         int token[MT];
@@ -234,135 +267,188 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeArgs a, const 
             for (int i = 0; i < KS; ++i) q[t][i] = *reinterpret_cast<const uint4*>(src + L::dim(i, g4));
         }
         Rows<DH, MT> r;
-        r.clear();
+        r.clear(c);
 
-        const long long head = ((long long)b * a.G + g) * a.max_len;
-        const uint8_t* kc = static_cast<const uint8_t*>(a.k_cache) + head * L::row;
-        const uint8_t* vc = static_cast<const uint8_t*>(a.v_cache) + head * L::row;
-        const uint8_t* kx = KIND == MOE_CACHE_BF16 ? nullptr : a.k_scale + head * L::srow;
-        const uint8_t* vx = KIND == MOE_CACHE_BF16 ? nullptr : a.v_scale + head * L::srow;
-        const int cached = min(t0 + steps, s.cached);
-        int t = t0 + wp;
-        CacheTile<KIND, DH> next;
-        auto load = [&](int at) {
-            const long long p = (long long)at * kTile;
-            next.load(kc + p * L::row, vc + p * L::row, kx + p * L::srow, vx + p * L::srow, s.len - (int)p, lane);
-        };
-        if (t < cached) load(t);
-        for (; t < cached; t += WP) {
-            const CacheTile<KIND, DH> tile = next;
-            if (t + WP < cached) load(t + WP);
-            const int left = s.len - t * kTile;
+        // The drafted tokens, dealt to the waves that split positions, come first: their loads are on their way together with the
+        // queries' and the first keys'.
+        for (int t = max(t0, s.cached) + wp; t < t0 + steps; t += WP) {
+            const int j0 = (t - s.cached) * kTile, left = s.count - j0;
+            const Window kd = window(a.k + ((long long)b * a.N + j0) * a.k_stride + g * DH, (int)((min(left, kTile) - 1) * a.k_stride + DH) * 2);
+            const Window vd = window(a.v + ((long long)b * a.N + j0) * a.v_stride + g * DH, (int)((min(left, kTile) - 1) * a.v_stride + DH) * 2);
             f32x4 sc[MT][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int i = 0; i < KS; ++i) {
-                    const uint4 k = tile.key(h, i, lane);
+                    uint32_t w4[4];
+                    load_raw<16>(kd, (h * 16 + n) * (int)a.k_stride * 2 + L::dim(0, g4) * 2, L::dim(i, 0) * 2, w4);
+                    const uint4 k = make_uint4(w4[0], w4[1], w4[2], w4[3]);
 #pragma unroll
                     for (int m = 0; m < MT; ++m) sc[m][h] = mfma(k, q[m][i], i ? sc[m][h] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
             uint32_t rowsv[8][DH / 32];
-            uint4 vt[NF];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) tile.value(j, (j >> 2) * 16 + g4 * 4 + (j & 3) < left, rowsv[j]);
-            transpose<DH>(rowsv, vt);
-            uint4 p[MT];
-            if (left >= kTile) {
-#pragma unroll
-                for (int m = 0; m < MT; ++m) p[m] = probabilities<DH, MT, false>(r, m, sc[m], c, 0, g4);
-            } else {
-#pragma unroll
-                for (int m = 0; m < MT; ++m) p[m] = probabilities<DH, MT, true>(r, m, sc[m], c, (1u << left) - 1, g4);
-            }
-#pragma unroll
-            for (int f = 0; f < NF; ++f)
-#pragma unroll
-                for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(vt[f], p[m], r.o[m][f]);
-        }
-        // the drafted tokens
-        for (; t < t0 + steps; t += WP) {
-            const int j0 = (t - s.cached) * kTile, left = s.count - j0;
-            const uint16_t* kd = a.k + ((long long)b * a.N + j0) * a.k_stride + g * DH;
-            const uint16_t* vd = a.v + ((long long)b * a.N + j0) * a.v_stride + g * DH;
-            f32x4 sc[MT][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint16_t* row = kd + min(h * 16 + n, left - 1) * a.k_stride;
-#pragma unroll
-                for (int i = 0; i < KS; ++i) {
-                    const uint4 k = *reinterpret_cast<const uint4*>(row + L::dim(i, g4));
-#pragma unroll
-                    for (int m = 0; m < MT; ++m) sc[m][h] = mfma(k, q[m][i], i ? sc[m][h] : f32x4{0.f, 0.f, 0.f, 0.f});
-                }
-            }
-            uint32_t rowsv[8][DH / 32];
-            uint4 vt[NF];
-            bool odd = false;                          // infinities and NaN among the values
+            uint32_t largest = 0;                      // magnitude bits of the values: infinities and NaN from 0x7f80 on
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int at = (j >> 2) * 16 + g4 * 4 + (j & 3);
-                load_raw<DH / 8>(reinterpret_cast<const uint8_t*>(vd + min(at, left - 1) * a.v_stride + n * (DH / 16)), rowsv[j]);
+                load_raw<DH / 8>(vd, ((j >> 2) * 16 + g4 * 4 + (j & 3)) * (int)a.v_stride * 2 + n * (DH / 8), 0, rowsv[j]);
 #pragma unroll
-                for (int i = 0; i < DH / 32; ++i) {
-                    rowsv[j][i] = at < left ? rowsv[j][i] : 0u;
-                    odd = odd || (rowsv[j][i] & 0x7f80u) == 0x7f80u || (rowsv[j][i] & 0x7f800000u) == 0x7f800000u;
-                }
+                for (int i = 0; i < DH / 32; ++i) largest = max(largest, max(rowsv[j][i] & 0x7fffu, (rowsv[j][i] >> 16) & 0x7fffu));
             }
-            transpose<DH>(rowsv, vt);
             uint4 p[MT];
             uint32_t seen[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
                 seen[m] = seen_word(a, s, b, token[m], j0);
-                p[m] = probabilities<DH, MT, true>(r, m, sc[m], c, seen[m], g4);
+                mask_scores(sc[m], seen[m], g4);
             }
-            if (__any(odd)) {
-                // Such a value is for the rows that see it: products with 0 would give it to all.  It counts as an infinity of either
-                // sign, NaN as both, in products of their own with the masks; the values proper have 0 in its place.
-                const uint32_t one = 0x3f80u;
+            probabilities<DH, MT>(r, sc, c, ahead, p);
+            auto operand = [&](int f) {
+                uint32_t pairs[8];
 #pragma unroll
-                for (int f = 0; f < NF; ++f) {
-                    uint32_t up[4], down[4], w4[4] = {vt[f].x, vt[f].y, vt[f].z, vt[f].w};
+                for (int j = 0; j < 8; ++j) pairs[j] = rowsv[j][f / 2];
+                return f % 2 ? gather<true>(pairs) : gather<false>(pairs);
+            };
+            if (__any(largest >= 0x7f80u)) {
+                // Infinities and NaN among the values are for the rows that see them, products with 0 would give them to all: added
+                // here, a position at a time, and 0 in the product
+#pragma unroll 1
+                for (int j = 0; j < min(left, kTile); ++j)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        up[i] = down[i] = 0;
+                        uint32_t w[DH / 32];
+                        load_raw<DH / 8>(vd, j * (int)a.v_stride * 2 + (g4 * 4 + i) * (DH / 8), 0, w);
 #pragma unroll
-                        for (int h = 0; h < 32; h += 16) {
-                            const uint32_t e = (w4[i] >> h) & 0xffffu;
-                            if ((e & 0x7f80u) != 0x7f80u) continue;
-                            if ((e & 0x7fu) || !(e & 0x8000u)) up[i] |= one << h;
-                            if ((e & 0x7fu) || (e & 0x8000u)) down[i] |= one << h;
-                            w4[i] &= ~(0xffffu << h);
+                        for (int f = 0; f < NF; ++f) {
+                            const float e = __uint_as_float(f & 1 ? w[f / 2] & 0xffff0000u : w[f / 2] << 16);
+                            const float add = fabsf(e) < INFINITY ? 0.f : e;
+#pragma unroll
+                            for (int m = 0; m < MT; ++m) r.o[m][f][i] += seen[m] >> j & 1u ? add : 0.f;
                         }
                     }
-                    vt[f] = make_uint4(w4[0], w4[1], w4[2], w4[3]);
 #pragma unroll
-                    for (int m = 0; m < MT; ++m) {
-                        uint32_t v4[4];
+                for (int j = 0; j < 8; ++j)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t two = seen[m] >> ((i / 2) * 16 + g4 * 4 + (i % 2) * 2);
-                            v4[i] = (two & 1u ? one : 0u) | (two & 2u ? one << 16 : 0u);
-                        }
-                        const uint4 vis = make_uint4(v4[0], v4[1], v4[2], v4[3]);
-                        const f32x4 zero{0.f, 0.f, 0.f, 0.f};
-                        const f32x4 ups = mfma(make_uint4(up[0], up[1], up[2], up[3]), vis, zero);
-                        const f32x4 downs = mfma(make_uint4(down[0], down[1], down[2], down[3]), vis, zero);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) r.o[m][f][i] += (ups[i] > 0.f ? INFINITY : 0.f) + (downs[i] > 0.f ? -INFINITY : 0.f);
+                    for (int i = 0; i < DH / 32; ++i) {
+                        if ((rowsv[j][i] & 0x7f80u) == 0x7f80u) rowsv[j][i] &= 0xffff0000u;
+                        if ((rowsv[j][i] & 0x7f800000u) == 0x7f800000u) rowsv[j][i] &= 0xffffu;
                     }
-                }
             }
 #pragma unroll
-            for (int f = 0; f < NF; ++f)
+            for (int f = 0; f < NF; ++f) {
+                const uint4 v = operand(f);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(vt[f], p[m], r.o[m][f]);
+                for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(v, p[m], r.o[m][f]);
+            }
         }
+
+        if constexpr (SHARED) {
+            for (int first = t0; first < cached; first += 4) {
+                uint4* own = lds16 + wave * (2 * KS + NF) * 64 + lane;
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) own[(h * KS + i) * 64] = tile.key(h, i, lane);
+                load_keys(now, first + 4 + wave);
+#pragma unroll
+                for (int f = 0; f < NF; f += 2) {
+                    uint32_t pairs[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) pairs[j] = tile.value(j, f / 2);
+                    own[(2 * KS + f) * 64] = gather<false>(pairs);
+                    own[(2 * KS + f + 1) * 64] = gather<true>(pairs);
+                }
+                load_values(now, first + 4 + wave);
+                lds_barrier();
+                // operands are read a group ahead of the products that take them: a wave has one tile's latency to itself
+                constexpr int half = NF / 2;
+                uint4 k0[KS], k1[KS], v0[half], v1[half];
+                const uint4* from = lds16 + wp * (2 * KS + NF) * 64 + lane;
+#pragma unroll
+                for (int i = 0; i < KS; ++i) k0[i] = from[i * 64];
+                for (int u = wp; u < 4 && first + u < cached; u += WP) {
+                    f32x4 sc[MT][2];
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) k1[i] = from[(KS + i) * 64];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < KS; ++i)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) sc[m][0] = mfma(k0[i], q[m][i], i ? sc[m][0] : f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+                    for (int f = 0; f < half; ++f) v0[f] = from[(2 * KS + f) * 64];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int i = 0; i < KS; ++i)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) sc[m][1] = mfma(k1[i], q[m][i], i ? sc[m][1] : f32x4{0.f, 0.f, 0.f, 0.f});
+                    const int left = s.len - (first + u) * kTile;
+                    if (left < kTile) {
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
+                    }
+                    uint4 p[MT];
+                    probabilities<DH, MT>(r, sc, c, ahead, p);
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int f = 0; f < half; ++f) v1[f] = from[(2 * KS + half + f) * 64];
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int f = 0; f < half; ++f)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(v0[f], p[m], r.o[m][f]);
+                    if (u + WP < 4) from += WP * (2 * KS + NF) * 64;
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) k0[i] = from[i * 64];         // the next tile's, or some again
+                    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                    for (int f = 0; f < half; ++f)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) r.o[m][half + f] = mfma(v1[f], p[m], r.o[m][half + f]);
+                }
+                lds_barrier();
+            }
+        } else {
+            for (int t = t0 + wp; t < cached; t += WP) {
+                const int left = s.len - t * kTile;
+                f32x4 sc[MT][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int i = 0; i < KS; ++i) {
+                        const uint4 k = tile.key(h, i, lane);
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) sc[m][h] = mfma(k, q[m][i], i ? sc[m][h] : f32x4{0.f, 0.f, 0.f, 0.f});
+                    }
+                load_keys(now, t + WP);
+                if (left < kTile) {
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
+                }
+                uint4 p[MT];
+                probabilities<DH, MT>(r, sc, c, ahead, p);
+#pragma unroll
+                for (int f = 0; f < NF; f += 2) {
+                    uint32_t pairs[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) pairs[j] = tile.value(j, f / 2);
+                    const uint4 lo = gather<false>(pairs), hi = gather<true>(pairs);
+#pragma unroll
+                    for (int m = 0; m < MT; ++m) {
+                        r.o[m][f] = mfma(lo, p[m], r.o[m][f]);
+                        r.o[m][f + 1] = mfma(hi, p[m], r.o[m][f + 1]);
+                    }
+                }
+                load_values(now, t + WP);
+            }
+        }
+        // the next part's first keys and values are on their way while this one's rows are finished
+        piece(next, left_steps);
+        load_keys(next, next.t0 + mine);
+        load_values(next, next.t0 + mine);
 
         // ---- the rows' results: to out if the item is all this share's, else into its part
         const bool whole = steps == s.tiles;
-        const size_t slot = partial_slot(w, x == begin);
+        const size_t slot = partial_slot(w, now.first);
         auto put = [&](int row, int first, const float* v, int count, float m, float l) {      // elements first.. of a row of the block
             if (row >= rows) return;
             const int local = row % ROWS;
@@ -387,29 +473,29 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeArgs a, const 
         if constexpr (WP == 1) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const float l = row_sum(r.l[m]);
+                const float l = r.l[m][0];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[8];
 #pragma unroll
                     for (int f = 0; f < NF; ++f) v[f] = r.o[m][f][i];
-                    put(row0 + m * 16 + n, (g4 * 4 + i) * NF, v, NF, r.m[m], l);
+                    put(row0 + m * 16 + n, (g4 * 4 + i) * NF, v, NF, r.mc[m], l);
                 }
             }
         } else {
             float* ml = lds + 4 * QT * OS;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const float l = row_sum(r.l[m]);
+                const float l = r.l[m][0];
                 float* o = lds + (wave * QT + m * 16 + n) * OS;
-                if (g4 == 0) { ml[(wave * QT + m * 16 + n) * 2] = r.m[m]; ml[(wave * QT + m * 16 + n) * 2 + 1] = l; }
+                if (g4 == 0) { ml[(wave * QT + m * 16 + n) * 2] = r.mc[m]; ml[(wave * QT + m * 16 + n) * 2 + 1] = l; }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int f = 0; f < NF; f += 4)
                         *reinterpret_cast<float4*>(o + (g4 * 4 + i) * NF + f) = make_float4(r.o[m][f][i], r.o[m][f + 1][i], r.o[m][f + 2][i], r.o[m][f + 3][i]);
             }
-            __syncthreads();
+            lds_barrier();
             for (int e = tid; e < ROWS * 16; e += 256) {           // 16 pieces of NF elements per row
                 const int row = e / 16, first = e % 16 * NF, set = row / QT;
                 float M = kLowest, l = 0.f, v[8] = {};
@@ -425,16 +511,16 @@ __global__ __launch_bounds__(256) void tree_attn_kernel(const TreeArgs a, const 
                 }
                 put(row0 - wr * QT + row, first, v, NF, M, l);
             }
-            __syncthreads();
+            lds_barrier();
         }
-        x += steps;
-        off += steps;
     }
+    if (tid == 0) parts.split[w] = split;
 }
 
 template <int KIND, int DH, int MT, int WR> int launch_tree_instance(const TreeArgs& a, const TreeParts& parts, hipStream_t s) {
     static OncePerDevice asked;
-    const int lds = WR == 4 ? 0 : 4 * 16 * MT * (DH + 4 + 2) * (int)sizeof(float);
+    constexpr int tiles = WR > 1 ? 4 * (DH / 32 * 2 + DH / 16) * 1024 : 0, merge = WR < 4 ? 4 * 16 * MT * (DH + 4 + 2) * (int)sizeof(float) : 0;
+    const int lds = tiles > merge ? tiles : merge;
     const int rc = ask_lds(reinterpret_cast<const void*>(&tree_attn_kernel<KIND, DH, MT, WR>), lds, asked);
     if (rc != MOE_OK) return rc;
     hipLaunchKernelGGL((tree_attn_kernel<KIND, DH, MT, WR>), dim3((unsigned)parts.groups), dim3(256), lds, s, a, parts);
@@ -443,9 +529,8 @@ template <int KIND, int DH, int MT, int WR> int launch_tree_instance(const TreeA
 
 template <int KIND> int launch_tree_kind(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s) {
 #define MOE_TREE(DH) \
-    (mt == 1 ? launch_tree_instance<KIND, DH, 1, 1>(a, p, s) : mt == 2 && wr == 1 ? launch_tree_instance<KIND, DH, 2, 1>(a, p, s) \
-     : mt == 2 ? launch_tree_instance<KIND, DH, 2, 2>(a, p, s) : wr == 2 ? launch_tree_instance<KIND, DH, 4, 2>(a, p, s) \
-                                                                         : launch_tree_instance<KIND, DH, 4, 4>(a, p, s))
+    (mt == 1 ? launch_tree_instance<KIND, DH, 1, 1>(a, p, s) : wr == 1 ? launch_tree_instance<KIND, DH, 2, 1>(a, p, s) \
+     : wr == 2 ? launch_tree_instance<KIND, DH, 2, 2>(a, p, s) : launch_tree_instance<KIND, DH, 2, 4>(a, p, s))
     const int rc = head_dim == 128 ? MOE_TREE(128) : MOE_TREE(64);
 #undef MOE_TREE
     return rc != MOE_OK ? rc : hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;

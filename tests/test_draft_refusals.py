@@ -117,8 +117,11 @@ class FakeDevice:
         self._s = strides or torch.empty(shape, device="meta").stride()
         self.device = torch.device("cuda", index)
 
-    def stride(self, i):
-        return self._s[i]
+    def stride(self):
+        return self._s
+
+    def get_device(self):
+        return self.device.index
 
     def is_contiguous(self):
         return tuple(self._s) == torch.empty(self.shape, device="meta").stride()
