@@ -16,14 +16,29 @@ template <int DH, int SETS>
 __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a, const TreeParts parts, int ROWS) {
     constexpr int NF = DH / 16;
     __shared__ float ml[SETS][16][2], o[SETS][16][16][NF];
-    const int R = a.H / a.G, w0 = blockIdx.x;
+    const int R = a.H / a.G, tid = threadIdx.x;
+    int w0 = blockIdx.x;
+    if constexpr (SETS > 1) {                                 // few items: the blockIdx.x-th share that has one, not a work-group for each
+        __shared__ int some[4 * SETS], found;
+        const bool here = tid < parts.groups && parts.split[tid].x >= 0;
+        const uint64_t m = __ballot(here);
+        if (tid % kWave == 0) some[tid / kWave] = __popcll(m);
+        if (tid == 0) found = -1;
+        __syncthreads();
+        int before = __popcll(m & ((1ull << (tid % kWave)) - 1));
+        for (int i = 0; i < tid / kWave; ++i) before += some[i];
+        if (here && before == (int)blockIdx.x) found = tid;
+        __syncthreads();
+        w0 = found;
+        if (w0 < 0) return;
+    }
     const int4 split = parts.split[w0];
     if (split.x < 0) return;
     const int b = split.x, w1 = split.z;
     const Sequence s = sequence(a, b, ROWS);
     const int g = split.y / s.blocks, block = split.y - g * s.blocks, rows = s.count * R, row0 = block * ROWS + blockIdx.y * 16;
     if (row0 >= rows) return;
-    const int tid = threadIdx.x, piece = tid % 16, local = tid / 16 % 16, set = tid / 256;
+    const int piece = tid % 16, local = tid / 16 % 16, set = tid / 256;
     const int row = row0 + local, in_block = blockIdx.y * 16 + local;
     float M = kLowest, L = 0.f, v[NF] = {};
     for (int w = w0 + set; w <= w1; w += 4 * SETS) {          // four parts' loads at once; behind the last: the last, with no weight
@@ -90,7 +105,7 @@ static TreePlan tree_plan(int R, int N, int head_dim) {
     TreePlan p;
     p.mt = rows <= 16 ? 1 : 2;
     p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
-    p.groups = 512;
+    p.groups = kMaxGroups;
     const int block = 16 * p.mt * p.wr;
     p.row_blocks = (rows + block - 1) / block;
     p.partial_bytes = (size_t)2 * p.groups * block * head_dim * sizeof(float);
@@ -117,8 +132,9 @@ int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStr
     if (rc != MOE_OK) return rc;
     const int block = 16 * p.mt * p.wr;
     const long long items = (long long)a.n_seq * a.G * p.row_blocks;
-    const dim3 grid((unsigned)p.groups, (unsigned)(std::min(block, a.N * (a.H / a.G) + 15) / 16));
     const bool many = items * 8 <= p.groups;                  // parts per item
+    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * (a.H / a.G) + 15) / 16));
+    static_assert(kMaxGroups <= 1024, "a thread per share");
 #define MOE_MERGE(DH) \
     do { \
         if (many) hipLaunchKernelGGL((tree_merge_kernel<DH, 4>), grid, dim3(1024), 0, s, a, parts, block); \
