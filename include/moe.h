@@ -376,6 +376,26 @@ int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const vo
                        const uint8_t* k_scale, const uint8_t* v_scale, const int32_t* lens, const int32_t* counts,
                        const int32_t* tree, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
+/* moe_draft_block_forward -- a decoder block (moe_decode_block_forward) over n_draft new tokens per sequence, bf16, with
+ * rotary positions, shared key/value heads and a cache of any kind.  With T = shape.T = n_seq * n_draft rows, d = d_model =
+ * n_heads * head_dim and G = n_kv_heads:
+ *   a      = LayerNorm(x; ln1_gamma, ln1_beta)
+ *   qkv    = a Wqkv + bqkv                    Wqkv [d, d + 2 G head_dim], columns q | k | v; q and k then turned by moe_rope
+ *   o      = moe_tree_attention(q, k, v; cache, lens, tree)
+ *   x1     = x + o Wo + bo
+ *   out    = x1 + moe_layer_forward(LayerNorm(x1; ln2_gamma, ln2_beta))
+ * rope may be NULL (no rotary positions; turns and pos are NULL then), else pos [T] are the rows' positions, whose q and k
+ * stay as they are where pos is negative.  lens, tree and the caches are those of moe_tree_attention; a sequence with fewer
+ * tokens has rows that no other token sees (the MoE layer routes them as it does every row).  The caches are not written: qkv [T, d + 2 G head_dim] is an output, of which the
+ * caller hands the accepted rows' k and v columns to moe_cache_write.  Weights, exports and flags are those of
+ * moe_decode_block_forward.  ws >= moe_draft_block_workspace_bytes(shape, cache, n_draft). */
+size_t moe_draft_block_workspace_bytes(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft);
+int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft, const moe_rope_t* rope,
+                            const moe_block_weights_t* weights, const void* x, const double* turns, const int32_t* pos,
+                            const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                            const int32_t* lens, const int32_t* tree, void* qkv, void* out, void* x1_out, void* moe_in_out,
+                            float* logits_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Stage timing of moe_layer_forward, for benchmarks (the paper reports the MoE
  * kernels' latency as a whole, Sec. 5.4; this splits it per kernel).
  * moe_profile_enable(n > 0) creates events for the next n calls (the one place

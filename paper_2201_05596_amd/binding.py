@@ -31,7 +31,8 @@ ENTRY_POINTS = ("moe_workspace_bytes", "moe_status_string", "moe_version", "moe_
                 "moe_gate_noalloc_bytes", "moe_gate_noalloc_max_bytes", "moe_dispatch",
                 "moe_expert_ffn", "moe_expert_ffn_slice", "moe_expert_ffn_slice_reduce", "moe_combine", "moe_layer_forward", "moe_decode_block_workspace_bytes",
                 "moe_decode_block_forward", "moe_rope_frequencies", "moe_rope", "moe_cache_bytes", "moe_cache_scale_bytes",
-                "moe_cache_write", "moe_cache_read", "moe_tree_attention_workspace_bytes", "moe_tree_attention", "moe_profile_enable", "moe_profile_select",
+                "moe_cache_write", "moe_cache_read", "moe_tree_attention_workspace_bytes", "moe_tree_attention",
+                "moe_draft_block_workspace_bytes", "moe_draft_block_forward", "moe_profile_enable", "moe_profile_select",
                 "moe_profile_stride", "moe_profile_calls",
                 "moe_profile_stage_count", "moe_profile_stage_name", "moe_profile_elapsed")
 
@@ -137,6 +138,10 @@ def load_library() -> ctypes.CDLL:
     lib.moe_tree_attention_workspace_bytes.argtypes = [cp, i32]
     lib.moe_tree_attention.restype = i32
     lib.moe_tree_attention.argtypes = [cp, i32] + [vp, i64] * 3 + [vp] * 7 + [vp, i64, vp, st, vp]
+    lib.moe_draft_block_workspace_bytes.restype = st
+    lib.moe_draft_block_workspace_bytes.argtypes = [sp, cp, i32]
+    lib.moe_draft_block_forward.restype = i32
+    lib.moe_draft_block_forward.argtypes = [sp, cp, i32, rp, ctypes.POINTER(MoeBlockWeights)] + [vp] * 14 + [vp, st, vp]
     lib.moe_profile_enable.restype = i32
     lib.moe_profile_enable.argtypes = [i32]
     lib.moe_profile_select.restype = i32
@@ -390,18 +395,25 @@ def moe_decode_block_workspace_bytes(shape: MoeShape, block: MoeBlockShape) -> i
     return int(load_library().moe_decode_block_workspace_bytes(ctypes.byref(shape), ctypes.byref(block)))
 
 
+def _block_weights(shape, weights: dict, width: int) -> MoeBlockWeights:
+    """width: columns of Wqkv."""
+    el, f32 = _elem(shape), torch.float32
+    d, f, E = shape.d_model, shape.d_ffn, shape.E
+    sizes = {"ln1_gamma": (f32, d), "ln1_beta": (f32, d), "ln2_gamma": (f32, d), "ln2_beta": (f32, d),
+             "Wqkv": (el, d * width), "bqkv": (el, width), "Wo": (el, d * d), "bo": (el, d),
+             "Wg": (f32, _wg(shape)), "bg": (f32, E), "W1": (el, _w(shape, E, d, f)), "b1": (el, E * f),
+             "W2": (el, _w(shape, E, f, d)), "b2": (el, E * d), "Wd1": (el, _w(shape, 1, d, f)), "bd1": (el, f),
+             "Wd2": (el, _w(shape, 1, f, d)), "bd2": (el, d)}
+    return MoeBlockWeights(**{n: _ptr(weights.get(n), sizes[n][0], sizes[n][1], n) for n in BLOCK_WEIGHT_FIELDS})
+
+
 def moe_decode_block_forward(shape, block, weights: dict, x, k_cache, v_cache, pos, out, x1_out, moe_in_out, logits_out,
                              ws) -> None:
     """`weights`: name -> tensor (or None) for the fields of moe_block_weights_t."""
     el, f32 = _elem(shape), torch.float32
-    T, d, f, E = shape.T, shape.d_model, shape.d_ffn, shape.E
+    T, d, E = shape.T, shape.d_model, shape.E
     cache = T * d * block.max_len                      # [T, H, max_len, d/H]
-    sizes = {"ln1_gamma": (f32, d), "ln1_beta": (f32, d), "ln2_gamma": (f32, d), "ln2_beta": (f32, d),
-             "Wqkv": (el, 3 * d * d), "bqkv": (el, 3 * d), "Wo": (el, d * d), "bo": (el, d),
-             "Wg": (f32, _wg(shape)), "bg": (f32, E), "W1": (el, _w(shape, E, d, f)), "b1": (el, E * f),
-             "W2": (el, _w(shape, E, f, d)), "b2": (el, E * d), "Wd1": (el, _w(shape, 1, d, f)), "bd1": (el, f),
-             "Wd2": (el, _w(shape, 1, f, d)), "bd2": (el, d)}
-    w = MoeBlockWeights(**{n: _ptr(weights.get(n), sizes[n][0], sizes[n][1], n) for n in BLOCK_WEIGHT_FIELDS})
+    w = _block_weights(shape, weights, 3 * d)
     wsp, wsn = _ws(shape, ws, _block_workspace_need(bytes(shape), bytes(block)))
     rc = load_library().moe_decode_block_forward(
         ctypes.byref(shape), ctypes.byref(block), ctypes.byref(w), _ptr(x, el, T * d, "x"),
@@ -575,6 +587,35 @@ def moe_tree_attention(cache, n_draft: int, q, k, v, k_cache, v_cache, k_scale, 
         _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, dev, bf, T, qw, "out"), _at(ws, dev, ws.dtype, ws.numel(), "ws"), nbytes,
         torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_tree_attention", rc)
+
+
+def moe_draft_block_workspace_bytes(shape: MoeShape, cache: MoeCacheShape, n_draft: int) -> int:
+    return int(load_library().moe_draft_block_workspace_bytes(ctypes.byref(shape), ctypes.byref(cache), int(n_draft)))
+
+
+@functools.lru_cache(maxsize=256)
+def _draft_workspace_need(shape: bytes, cache: bytes, n_draft: int) -> int:
+    return moe_draft_block_workspace_bytes(MoeShape.from_buffer_copy(shape), MoeCacheShape.from_buffer_copy(cache), n_draft)
+
+
+def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, turns, pos, k_cache, v_cache, k_scale, v_scale, lens, tree, qkv, out,
+                            x1_out, moe_in_out, logits_out, ws) -> None:
+    """`weights` as in moe_decode_block_forward, with Wqkv [d, d + 2 n_kv_heads head_dim]; rope, turns and pos may be None."""
+    el, f32, i32, dev = torch.bfloat16, torch.float32, torch.int32, torch._C._cuda_getDevice()
+    T, d, E = shape.T, shape.d_model, shape.E
+    width = d + 2 * cache.n_kv_heads * cache.head_dim
+    w = _block_weights(shape, weights, width)
+    need, nbytes = _draft_workspace_need(bytes(shape), bytes(cache), n_draft), 0 if ws is None else ws.numel() * ws.element_size()
+    if nbytes < need:
+        raise ValueError(f"workspace: {nbytes} bytes, this shape needs {need}")
+    rc = load_library().moe_draft_block_forward(
+        ctypes.byref(shape), ctypes.byref(cache), n_draft, None if rope is None else ctypes.byref(rope), ctypes.byref(w), _at(x, dev, el, T * d, "x"),
+        _at(turns, dev, torch.float64, 0 if rope is None else rope.rot_dim // 2, "turns"), _at(pos, dev, i32, T, "pos"),
+        *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), _at(lens, dev, i32, cache.n_seq, "lens"),
+        _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), _at(qkv, dev, el, T * width, "qkv"), _at(out, dev, el, T * d, "out"),
+        _at(x1_out, dev, el, T * d, "x1_out"), _at(moe_in_out, dev, el, T * d, "moe_in_out"), _at(logits_out, dev, f32, T * E, "logits_out"),
+        _at(ws, dev, ws.dtype, ws.numel(), "ws"), nbytes, torch._C._cuda_getCurrentRawStream(dev))
+    _check("moe_draft_block_forward", rc)
 
 
 def moe_profile_enable(max_calls: int) -> None:

@@ -1037,6 +1037,16 @@ int check_block_shape(const moe_shape_t* s, const moe_block_shape_t* b) {
     return MOE_OK;
 }
 
+// Parts that K of such a product is split into, and its tile
+int linear_split(int T, int K, int N, int* MT, int* NW) {
+    wsgemm_pick_tile(T, 1, N, MT, NW);
+    const long long waves = (long long)((N + 127) / 128) * ((T + *MT - 1) / *MT);
+    const int chunks = (K + wsgemm_chunk_k(*MT) - 1) / wsgemm_chunk_k(*MT);
+    long long ks = waves < 1024 ? (2048 + waves - 1) / waves : 1;
+    if (ks > kLinearMaxSplit) ks = kLinearMaxSplit;
+    if (ks > chunks) ks = chunks;
+    return (int)ks;
+}
 // out[T, N] = x[T, K] W[K, N] + bias on the weight-streaming kernel (a decode step has few rows: the product is a
 // read of W); with few output columns the inner dimension is split over more waves and summed in a fixed order: here, or
 // (split_out given and more than 1) by whoever reads `partial` next
@@ -1048,22 +1058,17 @@ int run_linear(const uint16_t* x, const uint16_t* W, const uint16_t* bias, uint1
     a.o_group_stride = T; a.a_group_stride = T; a.ksplit = 1;
     if (T <= 32) return launch_rows(a, nullptr, EPI_STORE, 2, st);   // 64 rows: two launches 151 us, one 158 (d = 1024)
     int MT, NW;
-    wsgemm_pick_tile(T, 1, N, &MT, &NW);
-    const long long waves = (long long)((N + 127) / 128) * ((T + MT - 1) / MT);
-    const int chunks = (K + wsgemm_chunk_k(MT) - 1) / wsgemm_chunk_k(MT);
-    long long ks = waves < 1024 ? (2048 + waves - 1) / waves : 1;
-    if (ks > kLinearMaxSplit) ks = kLinearMaxSplit;
-    if (ks > chunks) ks = chunks;
+    const int ks = linear_split(T, K, N, &MT, &NW);
     if (ks <= 1) return launch_wsgemm(a, EPI_STORE, MT, NW, 2, st);
-    a.ksplit = (int)ks; a.partial = partial; a.partial_rows = T;
+    a.ksplit = ks; a.partial = partial; a.partial_rows = T;
     int rc = launch_wsgemm(a, EPI_PARTIAL, MT, NW, 2, st);
     if (rc != MOE_OK) return rc;
     if (split_out) {
-        *split_out = (int)ks;
+        *split_out = ks;
         return MOE_OK;
     }
     SplitKReduceArgs r{};
-    r.partial = partial; r.ksplit = (int)ks; r.G = 1; r.N = N; r.group_stride = T; r.rows = nullptr; r.max_rows = T;
+    r.partial = partial; r.ksplit = ks; r.G = 1; r.N = N; r.group_stride = T; r.rows = nullptr; r.max_rows = T;
     r.bias = bias; r.out = out; r.top_k = 1; r.T = T;
     return launch_splitk_reduce(r, st);
 }
@@ -1075,27 +1080,72 @@ size_t moe_decode_block_workspace_bytes(const moe_shape_t* shape, const moe_bloc
     return block_layout(shape, block).total;
 }
 
+}  // extern "C"
+
+namespace {
+
+// what both blocks ask of their weights
+int check_block_weights(const moe_shape_t* shape, const moe_block_weights_t* w) {
+    if (!w || !w->ln1_gamma || !w->ln1_beta || !w->Wqkv || !w->Wo || !w->ln2_gamma || !w->ln2_beta || !w->Wg || !w->W1 || !w->W2)
+        return MOE_ERR_INVALID_ARG;
+    if (shape->residual && (!w->Wd1 || !w->Wd2)) return MOE_ERR_INVALID_ARG;
+    if (!shape->residual && (w->Wd1 || w->Wd2 || w->bd1 || w->bd2)) return MOE_ERR_INVALID_ARG;
+    const void* ptrs[] = {w->ln1_gamma, w->ln1_beta, w->Wqkv, w->bqkv, w->Wo, w->bo, w->ln2_gamma, w->ln2_beta, w->Wg,
+                          w->bg, w->W1, w->b1, w->W2, w->b2, w->Wd1, w->bd1, w->Wd2, w->bd2};
+    for (const void* p : ptrs)
+        if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+constexpr float kLayerNormEps = 1e-5f;
+
+// A block from its attention's rows on: projection, residual add, LayerNorm, MoE layer, residual add
+int block_tail(const moe_shape_t* shape, const moe_block_weights_t* w, const void* x, const uint16_t* attn, uint16_t* proj, uint16_t* x1,
+               uint16_t* moe_in, uint16_t* moe_out, float* lin_partial, void* moe_ws, void* out, float* logits_out, void* stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int T = shape->T, d = shape->d_model;
+    int split = 1;
+    int rc = run_linear(attn, u16(w->Wo), u16(w->bo), proj, T, d, d, lin_partial, add_layernorm_sums(d) ? &split : nullptr, st);
+    if (rc != MOE_OK) return rc;
+    // x1 = x + attention; the MoE layer sees LayerNorm(x1)
+    const AddedRows projected = split > 1 ? AddedRows{nullptr, PartSums{lin_partial, split, u16(w->bo)}} : AddedRows{proj, PartSums{}};
+    rc = launch_add_layernorm(u16(x), projected, w->ln2_gamma, w->ln2_beta, x1, moe_in, T, d, kLayerNormEps, st);
+    if (rc != MOE_OK) return rc;
+    // out = x1 + MoE: in the layer's last kernel or behind it
+    if (!layer_adds(shape, plan_ffn(shape))) {
+        rc = layer_forward_checked(shape, moe_in, w->Wg, w->bg, w->W1, w->b1, w->W2, w->b2, w->Wd1, w->bd1, w->Wd2, w->bd2,
+                                   moe_out, logits_out, nullptr, nullptr, nullptr, nullptr, nullptr,
+                                   moe_ws, ws_layout(shape).total, nullptr, stream);
+        g_prof.cur = -1;
+        if (rc != MOE_OK) return rc;
+        return launch_add_rows(x1, moe_out, u16(out), (long long)T * d, st);
+    }
+    rc = layer_forward_checked(shape, moe_in, w->Wg, w->bg, w->W1, w->b1, w->W2, w->b2, w->Wd1, w->bd1, w->Wd2, w->bd2,
+                               out, logits_out, nullptr, nullptr, nullptr, nullptr, nullptr,
+                               moe_ws, ws_layout(shape).total, x1, stream);
+    g_prof.cur = -1;
+    return rc;
+}
+
+}  // namespace
+
+extern "C" {
+
 int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* block, const moe_block_weights_t* w,
                              const void* x, void* k_cache, void* v_cache, const int32_t* pos, void* out, void* x1_out,
                              void* moe_in_out, float* logits_out, void* ws, size_t ws_bytes, void* stream) {
     int rc = check_block_shape(shape, block);
     if (rc != MOE_OK) return rc;
-    if (!w || !x || !k_cache || !v_cache || !pos || !out) return MOE_ERR_INVALID_ARG;
-    if (!w->ln1_gamma || !w->ln1_beta || !w->Wqkv || !w->Wo || !w->ln2_gamma || !w->ln2_beta || !w->Wg || !w->W1 || !w->W2)
-        return MOE_ERR_INVALID_ARG;
-    if (shape->residual && (!w->Wd1 || !w->Wd2)) return MOE_ERR_INVALID_ARG;
-    if (!shape->residual && (w->Wd1 || w->Wd2 || w->bd1 || w->bd2)) return MOE_ERR_INVALID_ARG;
-    const void* ptrs[] = {x, k_cache, v_cache, pos, out, x1_out, moe_in_out, logits_out, w->ln1_gamma, w->ln1_beta, w->Wqkv,
-                          w->bqkv, w->Wo, w->bo, w->ln2_gamma, w->ln2_beta, w->Wg, w->bg, w->W1, w->b1, w->W2, w->b2,
-                          w->Wd1, w->bd1, w->Wd2, w->bd2};
-    for (const void* p : ptrs)
+    if ((rc = check_block_weights(shape, w)) != MOE_OK) return rc;
+    if (!x || !k_cache || !v_cache || !pos || !out) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, static_cast<const void*>(k_cache), static_cast<const void*>(v_cache), static_cast<const void*>(pos), static_cast<const void*>(out),
+                          static_cast<const void*>(x1_out), static_cast<const void*>(moe_in_out), static_cast<const void*>(logits_out)})
         if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
     const BlockLayout L = block_layout(shape, block);
     if (!ws || !aligned16(ws) || ws_bytes < L.total) return MOE_ERR_WORKSPACE;
 
     hipStream_t st = static_cast<hipStream_t>(stream);
     const int T = shape->T, d = shape->d_model, H = block->n_heads, dh = d / H;
-    const float eps = 1e-5f;
     uint16_t* qkv = at<uint16_t>(ws, L.qkv);
     uint16_t* attn = at<uint16_t>(ws, L.attn);
     uint16_t* proj = at<uint16_t>(ws, L.proj);
@@ -1106,7 +1156,7 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
     float* lin_partial = at<float>(ws, L.lin_partial);
 
     // a = LayerNorm(x); qkv = a Wqkv + bqkv
-    rc = launch_add_layernorm(u16(x), AddedRows{}, w->ln1_gamma, w->ln1_beta, nullptr, xn, T, d, eps, st);
+    rc = launch_add_layernorm(u16(x), AddedRows{}, w->ln1_gamma, w->ln1_beta, nullptr, xn, T, d, kLayerNormEps, st);
     if (rc != MOE_OK) return rc;
     rc = run_linear(xn, u16(w->Wqkv), u16(w->bqkv), qkv, T, d, 3 * d, lin_partial, nullptr, st);
     if (rc != MOE_OK) return rc;
@@ -1114,27 +1164,7 @@ int moe_decode_block_forward(const moe_shape_t* shape, const moe_block_shape_t* 
     rc = launch_attn_decode(qkv, u16(k_cache), u16(v_cache), pos, at<float>(ws, L.attn_partial), attn, T, H, dh,
                             block->max_len, st);
     if (rc != MOE_OK) return rc;
-    int split = 1;
-    rc = run_linear(attn, u16(w->Wo), u16(w->bo), proj, T, d, d, lin_partial, add_layernorm_sums(d) ? &split : nullptr, st);
-    if (rc != MOE_OK) return rc;
-    // x1 = x + attention; the MoE layer sees LayerNorm(x1)
-    const AddedRows projected = split > 1 ? AddedRows{nullptr, PartSums{lin_partial, split, u16(w->bo)}} : AddedRows{proj, PartSums{}};
-    rc = launch_add_layernorm(u16(x), projected, w->ln2_gamma, w->ln2_beta, x1, moe_in, T, d, eps, st);
-    if (rc != MOE_OK) return rc;
-    // out = x1 + MoE: in the layer's last kernel or behind it
-    if (!layer_adds(shape, plan_ffn(shape))) {
-        rc = layer_forward_checked(shape, moe_in, w->Wg, w->bg, w->W1, w->b1, w->W2, w->b2, w->Wd1, w->bd1, w->Wd2, w->bd2,
-                                   moe_out, logits_out, nullptr, nullptr, nullptr, nullptr, nullptr,
-                                   at<void>(ws, L.moe_ws), ws_layout(shape).total, nullptr, stream);
-        g_prof.cur = -1;
-        if (rc != MOE_OK) return rc;
-        return launch_add_rows(x1, moe_out, u16(out), (long long)T * d, st);
-    }
-    rc = layer_forward_checked(shape, moe_in, w->Wg, w->bg, w->W1, w->b1, w->W2, w->b2, w->Wd1, w->bd1, w->Wd2, w->bd2,
-                               out, logits_out, nullptr, nullptr, nullptr, nullptr, nullptr,
-                               at<void>(ws, L.moe_ws), ws_layout(shape).total, x1, stream);
-    g_prof.cur = -1;
-    return rc;
+    return block_tail(shape, w, x, attn, proj, x1, moe_in, moe_out, lin_partial, at<void>(ws, L.moe_ws), out, logits_out, stream);
 }
 
 // ---- several new tokens per sequence ------------------------------------------------------------------------------
@@ -1290,6 +1320,95 @@ int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const vo
     const TreeArgs a{u16(q), u16(k), u16(v), q_stride, k_stride, v_stride, out_stride, k_cache, v_cache, k_scale, v_scale,
                      lens, counts, tree, u16(out), cache->n_seq, n_draft, cache->n_heads, cache->n_kv_heads, cache->max_len};
     return launch_tree_attn(a, cache->kind, cache->head_dim, ws, static_cast<hipStream_t>(stream));
+}
+
+// ---- a decoder block over drafted tokens -------------------------------------------------------------------------
+
+}  // extern "C"
+
+namespace {
+
+struct DraftLayout {
+    size_t attn, proj, x1, xn, moe_out, tree_ws, lin_partial, moe_ws, total;
+};
+
+DraftLayout draft_layout(const moe_shape_t* s, const moe_cache_shape_t* c, int n_draft) {
+    DraftLayout L{};
+    const size_t T = s->T, d = s->d_model;
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+    auto sums = [&](int K, int N) {
+        int MT, NW;
+        const int ks = s->T > 32 ? linear_split(s->T, K, N, &MT, &NW) : 1;
+        return ks > 1 ? (size_t)ks * T * N * 4 : 0;
+    };
+    L.attn = take(T * d * 2);
+    L.proj = take(T * d * 2);
+    L.x1 = take(T * d * 2);
+    L.xn = take(T * d * 2);
+    L.moe_out = take(T * d * 2);
+    L.tree_ws = take(tree_attn_ws_bytes(c, n_draft));
+    L.lin_partial = take(std::max(sums(s->d_model, (c->n_heads + 2 * c->n_kv_heads) * c->head_dim), sums(s->d_model, s->d_model)));
+    L.moe_ws = take(ws_layout(s).total);
+    L.total = off;
+    return L;
+}
+
+int check_draft_block(const moe_shape_t* s, const moe_cache_shape_t* c, int32_t n_draft) {
+    int rc = check_shape(s);
+    if (rc == MOE_OK) rc = check_tree(c, n_draft);
+    if (rc != MOE_OK) return rc;
+    if ((long long)c->n_seq * n_draft != s->T || c->n_heads * c->head_dim != s->d_model) return MOE_ERR_INVALID_ARG;
+    return s->dtype == MOE_BF16 ? MOE_OK : MOE_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_draft_block_workspace_bytes(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft) {
+    if (check_draft_block(shape, cache, n_draft) != MOE_OK) return 0;
+    return draft_layout(shape, cache, n_draft).total;
+}
+
+int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft, const moe_rope_t* rope,
+                            const moe_block_weights_t* w, const void* x, const double* turns, const int32_t* pos,
+                            const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                            const int32_t* lens, const int32_t* tree, void* qkv, void* out, void* x1_out, void* moe_in_out,
+                            float* logits_out, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_draft_block(shape, cache, n_draft);
+    if (rc == MOE_OK && rope) rc = check_rope(rope);
+    if (rc == MOE_OK) rc = check_block_weights(shape, w);
+    if (rc == MOE_OK) rc = check_cache_pointers(cache, k_cache, v_cache, k_scale, v_scale);
+    if (rc != MOE_OK) return rc;
+    if (!x || !lens || !qkv || !out) return MOE_ERR_INVALID_ARG;
+    if (rope ? rope->head_dim != cache->head_dim || rope->dtype != MOE_BF16 || !turns || !pos : turns || pos) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, static_cast<const void*>(turns), static_cast<const void*>(pos), static_cast<const void*>(lens), static_cast<const void*>(tree),
+                          static_cast<const void*>(qkv), static_cast<const void*>(out), static_cast<const void*>(x1_out),
+                          static_cast<const void*>(moe_in_out), static_cast<const void*>(logits_out)})
+        if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    const int T = shape->T, d = shape->d_model, H = cache->n_heads, G = cache->n_kv_heads, dh = cache->head_dim, width = (H + 2 * G) * dh;
+    if (T > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    const DraftLayout L = draft_layout(shape, cache, n_draft);
+    if (!ws || !aligned16(ws) || ws_bytes < L.total) return MOE_ERR_WORKSPACE;
+
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    uint16_t* rows = u16(qkv);
+    uint16_t* attn = at<uint16_t>(ws, L.attn);
+    uint16_t* xn = at<uint16_t>(ws, L.xn);
+    float* lin_partial = at<float>(ws, L.lin_partial);
+    rc = launch_add_layernorm(u16(x), AddedRows{}, w->ln1_gamma, w->ln1_beta, nullptr, xn, T, d, kLayerNormEps, st);
+    if (rc != MOE_OK) return rc;
+    rc = run_linear(xn, u16(w->Wqkv), u16(w->bqkv), rows, T, d, width, lin_partial, nullptr, st);
+    if (rc != MOE_OK) return rc;
+    if (rope) rc = launch_rope(rope, T, H + G, rows, width, turns, pos, rows, width, st);
+    if (rc != MOE_OK) return rc;
+    const TreeArgs a{rows, rows + H * dh, rows + (H + G) * dh, width, width, width, d, k_cache, v_cache, k_scale, v_scale,
+                     lens, nullptr, tree, attn, cache->n_seq, n_draft, H, G, cache->max_len};
+    rc = launch_tree_attn(a, cache->kind, dh, at<void>(ws, L.tree_ws), st);
+    if (rc != MOE_OK) return rc;
+    return block_tail(shape, w, x, attn, at<uint16_t>(ws, L.proj), x1_out ? u16(x1_out) : at<uint16_t>(ws, L.x1),
+                      moe_in_out ? u16(moe_in_out) : xn, at<uint16_t>(ws, L.moe_out), lin_partial, at<void>(ws, L.moe_ws), out, logits_out, stream);
 }
 
 int moe_profile_enable(int max_calls) {

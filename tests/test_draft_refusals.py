@@ -181,3 +181,33 @@ def test_names_of_choices():
         B.make_rope(64, 64, "other", "bf16")
     with pytest.raises(KeyError):
         B.make_cache_shape(1, 1, 1, 64, 1, "int8")
+
+
+def block_call(shape=None, c=None, n=4, rope="own", weights=None, x=FAKE, turns=FAKE, pos=FAKE, kc=FAKE, vc=FAKE, kx=FAKE, vx=FAKE, lens=FAKE, tree=FAKE,
+               qkv=FAKE, out=FAKE, x1=None, moe_in=None, logits=None, ws=FAKE, wsn=BIG):
+    s = B.MoeShape(**{**dict(T=8, d_model=512, d_ffn=1024, E=4, top_k=1, capacity=8, dtype=1, residual=0, flags=0), **(shape or {})})
+    c = cache_shape(**(c or {}))
+    r = B.make_rope(64, 64, "half", "bf16") if rope == "own" else rope
+    w = {n: FAKE for n in B.BLOCK_WEIGHT_FIELDS if not n.endswith(("d1", "d2"))}
+    w.update(weights or {})
+    return B.load_library().moe_draft_block_forward(ctypes.byref(s), ctypes.byref(c), n, None if r is None else ctypes.byref(r),
+                                                    ctypes.byref(B.MoeBlockWeights(**w)), x, turns, pos, kc, vc, kx, vx, lens, tree, qkv, out, x1, moe_in,
+                                                    logits, ws, wsn, None)
+
+
+def test_draft_block_arguments():
+    for patch, code in BAD_CACHES:
+        assert block_call(c=patch) == code, patch
+    for bad in (dict(shape=dict(T=7)), dict(shape=dict(T=12)), dict(shape=dict(d_model=256)), dict(n=3), dict(n=0), dict(x=None), dict(lens=None),
+                dict(qkv=None), dict(out=None), dict(kc=None), dict(vx=None), dict(turns=None), dict(pos=None), dict(x=ODD), dict(qkv=ODD), dict(tree=ODD),
+                dict(logits=ODD), dict(x1=ODD), dict(moe_in=ODD), dict(rope=None), dict(rope=None, pos=None), dict(rope=B.make_rope(128, 64, "half", "bf16")),
+                dict(rope=B.make_rope(64, 64, "half", "f32")), dict(weights=dict(Wqkv=None)), dict(weights=dict(ln2_beta=None)), dict(weights=dict(W1=ODD)),
+                dict(weights=dict(Wd1=FAKE)), dict(shape=dict(residual=1))):
+        assert block_call(**bad) == -1, bad
+    assert block_call(shape=dict(dtype=0)) == -2
+    assert block_call(ws=None) == -3
+    s, c = B.make_shape(8, 512, 1024, 4, 1, 8, "bf16"), cache_shape()
+    need = B.moe_draft_block_workspace_bytes(s, c, 4)
+    assert need > 0 and block_call(wsn=need - 1) == -3
+    assert B.moe_draft_block_workspace_bytes(s, c, 3) == 0
+    assert B.moe_draft_block_workspace_bytes(B.make_shape(8, 512, 1024, 4, 1, 8, "f32"), c, 4) == 0
