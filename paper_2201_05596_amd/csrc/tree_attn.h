@@ -26,6 +26,10 @@ struct TreePlan {                      // how the host sets a call up
     size_t partial_bytes, ml_bytes;
 };
 
+// Quotient of values that are the same in every lane.  Divisions (and clamps) are done by the vector unit; what depends on them
+// has to come back into scalar registers, or every load through a window becomes a loop over the lanes' different windows.
+__device__ __forceinline__ int quotient(int a, int b) { return __builtin_amdgcn_readfirstlane(a / b); }
+
 // ---- the share of a work-group ----------------------------------------------------------------------------------
 // A sequence has G x (blocks of ROWS rows) items of `tiles` steps each: ceil(len / 32) over the cache, ceil(count / 32) over the
 // drafted tokens; an item's beginning and end count as kItemSteps more, ahead of its own.  All items' steps in a row are cut into
@@ -36,13 +40,17 @@ struct Sequence {
     int blocks, items;                 // blocks of rows per key/value head
     __device__ __forceinline__ int item_steps() const { return tiles + kItemSteps; }
 };
-__device__ __forceinline__ Sequence sequence(const TreeArgs& a, int b, int ROWS) {
+// SAME: b is the same in every lane, and so is what is read (which the compiler does not know)
+template <bool SAME> __device__ __forceinline__ Sequence sequence(const TreeArgs& a, int b, int ROWS) {
     Sequence s;
-    s.len = min(max(a.lens[b], 0), a.max_len);
-    s.count = a.counts ? min(max(a.counts[b], 0), a.N) : a.N;
+    s.len = a.lens[b];
+    s.count = a.counts ? a.counts[b] : a.N;
+    s.len = min(max(s.len, 0), a.max_len);
+    s.count = min(max(s.count, 0), a.N);
+    if (SAME) { s.len = __builtin_amdgcn_readfirstlane(s.len); s.count = __builtin_amdgcn_readfirstlane(s.count); }
     s.cached = (s.len + kTile - 1) / kTile;
     s.tiles = s.cached + (s.count + kTile - 1) / kTile;
-    s.blocks = (s.count * (a.H / a.G) + ROWS - 1) / ROWS;
+    s.blocks = (s.count * a.R + ROWS - 1) / ROWS;
     s.items = a.G * s.blocks;
     return s;
 }
@@ -77,7 +85,7 @@ struct Share {
 // The share of work-group `w`, by each wave.  wp: positions are split over so many waves.
 __device__ __forceinline__ Share share_of(const TreeArgs& a, int ROWS, int groups, int wp, int w, int lane) {
     auto steps = [&](int b, int& tiles) {
-        const Sequence s = sequence(a, min(b, a.n_seq - 1), ROWS);
+        const Sequence s = sequence<false>(a, min(b, a.n_seq - 1), ROWS);
         tiles = b < a.n_seq && s.items ? s.item_steps() : 0;
         return s.items * tiles;
     };
@@ -94,7 +102,7 @@ __device__ __forceinline__ Share share_of(const TreeArgs& a, int ROWS, int group
     total = __builtin_amdgcn_readfirstlane(total);
     most = __builtin_amdgcn_readfirstlane(most);
     Share r;
-    r.size = (total + groups - 1) / groups;
+    r.size = quotient(total + groups - 1, groups);
     if (r.size > wp) r.size = (r.size + wp - 1) / wp * wp;
     r.size = max(r.size, max(1, min(most, kLeastSteps * wp + kItemSteps)));     // shorter items are not cut
     r.begin = (int)min((long long)w * r.size, (long long)total);

@@ -16,7 +16,7 @@ template <int DH, int SETS>
 __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a, const TreeParts parts, int ROWS) {
     constexpr int NF = DH / 16;
     __shared__ float ml[SETS][16][2], o[SETS][16][16][NF];
-    const int R = a.H / a.G, tid = threadIdx.x;
+    const int R = a.R, tid = threadIdx.x;
     int w0 = blockIdx.x;
     if constexpr (SETS > 1) {                                 // few items: the blockIdx.x-th share that has one, not a work-group for each
         __shared__ int some[4 * SETS], found;
@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
     const int4 split = parts.split[w0];
     if (split.x < 0) return;
     const int b = split.x, w1 = split.z;
-    const Sequence s = sequence(a, b, ROWS);
+    const Sequence s = sequence<true>(a, b, ROWS);
     const int g = split.y / s.blocks, block = split.y - g * s.blocks, rows = s.count * R, row0 = block * ROWS + blockIdx.y * 16;
     if (row0 >= rows) return;
     const int piece = tid % 16, local = tid / 16 % 16, set = tid / 256;
@@ -103,8 +103,8 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
 static TreePlan tree_plan(int R, int N, int head_dim) {
     const int rows = N * R;                                   // at most, per key/value head
     TreePlan p;
-    p.mt = rows <= 16 ? 1 : 2;
-    p.wr = rows <= 32 ? 1 : rows <= 64 ? 2 : 4;
+    p.mt = rows <= 32 ? 1 : 2;
+    p.wr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
     p.groups = kMaxGroups;
     const int block = 16 * p.mt * p.wr;
     p.row_blocks = (rows + block - 1) / block;
@@ -123,7 +123,7 @@ long long tree_attn_steps(const moe_cache_shape_t* c, int n_draft) {
 }
 
 int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s) {
-    const TreePlan p = tree_plan(a.H / a.G, a.N, head_dim);
+    const TreePlan p = tree_plan(a.R, a.N, head_dim);
     char* at = static_cast<char*>(ws);
     const TreeParts parts{reinterpret_cast<float*>(at), reinterpret_cast<float*>(at + p.partial_bytes),
                           reinterpret_cast<int4*>(at + p.partial_bytes + p.ml_bytes), p.groups};
@@ -133,7 +133,7 @@ int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStr
     const int block = 16 * p.mt * p.wr;
     const long long items = (long long)a.n_seq * a.G * p.row_blocks;
     const bool many = items * 8 <= p.groups;                  // parts per item
-    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * (a.H / a.G) + 15) / 16));
+    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * (a.R) + 15) / 16));
     static_assert(kMaxGroups <= 1024, "a thread per share");
 #define MOE_MERGE(DH) \
     do { \

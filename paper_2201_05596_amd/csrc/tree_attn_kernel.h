@@ -23,10 +23,10 @@ template <int KIND, int DH> struct Layout {
     }
 };
 
-// Memory from p on, of which `bytes` may be read: loads behind them give 0
+// Memory from p on, of which `bytes` may be read (the same in every lane): loads behind them give 0
 typedef __amdgpu_buffer_rsrc_t Window;
 __device__ __forceinline__ Window window(const void* p, int bytes) {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, bytes, 0x00027000);
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
 template <int BYTES> __device__ __forceinline__ void load_raw(Window p, int at, int plus, uint32_t (&w)[(BYTES + 3) / 4]) {
     if constexpr (BYTES == 16) {
@@ -42,18 +42,18 @@ template <int BYTES> __device__ __forceinline__ void load_raw(Window p, int at, 
     }
 }
 
-template <int KIND, int DH> struct CacheTile {
+template <int KIND, int DH, int HALVES> struct CacheTile {        // 16 HALVES positions
     typedef Layout<KIND, DH> L;
     static constexpr int kw = L::kload / 4, vw = (L::vload + 3) / 4;
-    uint32_t k[2][L::nk][kw];
-    uint32_t v[8][vw];
-    uint32_t ks[2], vs[8];                                        // scale bytes of the rows
+    uint32_t k[HALVES][L::nk][kw];
+    uint32_t v[4 * HALVES][vw];
+    uint32_t ks[HALVES], vs[4 * HALVES];                          // scale bytes of the rows
 
-    // kc, kx, vc, vx: the tile's positions that are there
+    // kc, kx, vc, vx: the positions that are there
     __device__ __forceinline__ void load_keys(Window kc, Window kx, int lane) {
         const int r = lane & 15, g = lane >> 4;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
+        for (int t = 0; t < HALVES; ++t) {
 #pragma unroll
             for (int n = 0; n < L::nk; ++n) load_raw<L::kload>(kc, r * L::row + g * L::kload, t * 16 * L::row + n * 4 * L::kload, k[t][n]);
             if constexpr (KIND != MOE_CACHE_BF16) {
@@ -66,14 +66,14 @@ template <int KIND, int DH> struct CacheTile {
     __device__ __forceinline__ void load_values(Window vc, Window vx, int lane) {
         const int c = lane & 15, g = lane >> 4;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < 4 * HALVES; ++j) {
             const int at = (j >> 2) * 16 + (j & 3);
             load_raw<L::vload>(vc, g * 4 * L::row + c * L::vload, at * L::row, v[j]);
             if constexpr (KIND != MOE_CACHE_BF16) vs[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vx, g * 4 * L::srow + c * L::srow / 16, at * L::srow, 0);
         }
     }
 
-    // step s of the product over the head dimension: 8 elements of row r of half tile t
+    // step s of the product over the head dimension: 8 elements of row r of half t
     __device__ __forceinline__ uint4 key(int t, int s, int lane) const {
         if constexpr (KIND == MOE_CACHE_BF16) {
             return make_uint4(k[t][s][0], k[t][s][1], k[t][s][2], k[t][s][3]);
@@ -100,12 +100,21 @@ template <int KIND, int DH> struct CacheTile {
     }
 };
 
-// pairs[8]: two elements of eight positions each -> the operand of V^T for the first (HIGH: the second) of them
+// pairs: two elements of N positions each -> their words of the operand of V^T for the first (HIGH: the second) of them
+template <bool HIGH, int N> __device__ __forceinline__ void gather(const uint32_t (&pairs)[N], uint32_t (&w)[N / 2]) {
+#pragma unroll
+    for (int j = 0; j < N / 2; ++j) w[j] = __builtin_amdgcn_perm(pairs[2 * j + 1], pairs[2 * j], HIGH ? 0x07060302u : 0x05040100u);
+}
 template <bool HIGH> __device__ __forceinline__ uint4 gather(const uint32_t (&pairs)[8]) {
     uint32_t w[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = __builtin_amdgcn_perm(pairs[2 * j + 1], pairs[2 * j], HIGH ? 0x07060302u : 0x05040100u);
+    gather<HIGH, 8>(pairs, w);
     return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// the same number, worked out anew from here on: what depends on it takes no registers elsewhere
+__device__ __forceinline__ int anew(int v) {
+    asm volatile("" : "+v"(v));
+    return v;
 }
 
 __device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, f32x4 c) {
@@ -113,29 +122,28 @@ __device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, f32x4 c) {
 }
 
 // over the four lanes that hold a row
+__device__ __forceinline__ float row_sum(float v) { v += __shfl_xor(v, 16); return v + __shfl_xor(v, 32); }
 __device__ __forceinline__ float row_max(float v) { v = fmaxf(v, __shfl_xor(v, 16)); return fmaxf(v, __shfl_xor(v, 32)); }
 
 template <int DH, int MT> struct Rows {          // a wave's rows: lane (n, g) holds row n of every 16, elements (4 g + i) DH / 16 + q in o[.][q][i]
     f32x4 o[MT][DH / 16];
-    f32x4 l[MT];                                 // sums, by a product with ones: the same in every element, the first one is kept
+    float l[MT];                                 // sums of the lane's own positions
     float m[MT], mc[MT];                         // maximum score, and c times it
     __device__ __forceinline__ void clear(float c) {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             m[t] = kLowest;
             mc[t] = kLowest * c;
-            l[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            l[t] = 0.f;
 #pragma unroll
             for (int q = 0; q < DH / 16; ++q) o[t][q] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
     }
 };
 
-// A tile's scores -> probabilities (as the second product's operands).  The maximum moves only when a score exceeds it by 2^8:
-// until then probabilities are at most 2^8, which sums in 32 bits and bf16's range take, and neither the rows' lanes nor the
-// sums have to be touched.  ahead: 8 / c.
-template <int DH, int MT>
-__device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, float ahead, uint4 (&out)[MT]) {
+// The maximum moves only when a score exceeds it by 2^8: until then probabilities are at most 2^8, which sums in 32 bits and
+// bf16's range take, and neither the rows' lanes nor the sums have to be touched.  ahead: 8 / c.
+template <int DH, int MT> __device__ __forceinline__ void raise_maximum(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, float ahead) {
     bool grows = false;
     float top[MT];
 #pragma unroll
@@ -151,19 +159,21 @@ __device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[
             const float m = fmaxf(r.m[t], row_max(top[t])), f = __builtin_amdgcn_exp2f((r.m[t] - m) * c);
             r.m[t] = m;
             r.mc[t] = m * c;
-            r.l[t][0] *= f;
+            r.l[t] *= f;
 #pragma unroll
             for (int q = 0; q < DH / 16; ++q) r.o[t][q] *= f;
         }
     }
-    const uint32_t one = 0x3f803f80u;
+}
+// A tile's scores -> probabilities, as the second product's operands
+template <int DH, int MT> __device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, uint4 (&out)[MT]) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         float p[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i / 4][i % 4], c, -r.mc[t]));
+        r.l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         out[t] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-        r.l[t] = mfma(make_uint4(one, one, one, one), out[t], r.l[t]);
     }
 }
 
@@ -178,13 +188,13 @@ __device__ __forceinline__ void mask_scores(f32x4 (&s)[2], uint32_t seen, int g)
 template <int KIND, int DH, int MT, int WR>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
     typedef Layout<KIND, DH> L;
-    constexpr int WP = 4 / WR, QT = 16 * MT, ROWS = QT * WR, KS = DH / 32, NF = DH / 16, OS = DH + 4;
+    constexpr int WP = 4 / WR, QT = 16 * MT, ROWS = QT * WR, KS = DH / 32, NF = DH / 16, OS = DH + 4, FRAGS = 2 * KS + NF;
     constexpr bool SHARED = WR > 1;                   // a tile is in operand order in LDS, for all waves; else in its own wave's registers
-    extern __shared__ uint4 lds16[];                  // SHARED: [4 tiles][2 KS + NF][64]; WP > 1, behind the steps: [4][QT][OS] and [4][QT][2] floats
+    extern __shared__ uint4 lds16[];                  // SHARED: [2 rounds][2 tiles][FRAGS][64]; WP > 1, behind the steps: [4][QT][OS] and [4][QT][2] floats
     float* lds = reinterpret_cast<float*>(lds16);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WP, wp = wave % WP, n = lane & 15, g4 = lane >> 4;
-    const int R = a.H / a.G;
+    const int R = a.R;
     const float c = 1.44269504f * rsqrtf((float)DH), ahead = 8.f / c;
 
     // consecutive shares on one XCD: they read the same keys and values where an item's rows take several blocks
@@ -208,8 +218,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         int item, ahead;
         for (;; left -= ahead, p.off += ahead) {      // parts of an item's beginning alone are none
             if (left <= 0) { left = 0; p.cached = p.t0 = 0; return; }
-            while (p.off >= p.s.items * p.s.item_steps()) { p.off = 0; p.s = sequence(a, ++p.b, ROWS); }
-            item = p.off / p.s.item_steps();
+            while (p.off >= p.s.items * p.s.item_steps()) { p.off = 0; p.s = sequence<true>(a, ++p.b, ROWS); }
+            item = quotient(p.off, p.s.item_steps());
             const int at = p.off - item * p.s.item_steps();
             p.t0 = max(at - kItemSteps, 0);
             ahead = min(max(kItemSteps - at, 0), left);
@@ -221,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         p.steps = min(p.s.tiles - p.t0, left);
         left -= p.steps;
         p.off += p.steps;
-        p.g = item / p.s.blocks;
+        p.g = quotient(item, p.s.blocks);
         p.row0 = (item - p.g * p.s.blocks) * ROWS + wr * QT;
         p.cached = min(p.t0 + p.steps, p.s.cached);
         const long long head = ((long long)p.b * a.G + p.g) * a.max_len;
@@ -231,26 +241,35 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         p.vx = KIND == MOE_CACHE_BF16 ? nullptr : a.v_scale + head * L::srow;
         // the share that holds the item's last step: as many steps behind this part as are left of it
         if (p.t0 == 0 && p.steps < p.s.tiles)
-            split = make_int4(p.b, item, w + (p.s.tiles - p.steps + share.size - 1) / share.size, (int)partial_slot(w, p.first));
+            split = make_int4(p.b, item, w + quotient(p.s.tiles - p.steps + share.size - 1, share.size), (int)partial_slot(w, p.first));
     };
     // Keys and values of the next step are loaded into the registers that a step is done with; behind the last step nothing is
     // read (an empty window), so that loads are no branches and their waits are counted
-    CacheTile<KIND, DH> tile;
-    auto there = [&](const Piece& p, const uint8_t* at, int t, int row) {
-        return window(at + (long long)t * (kTile * row), t < p.cached ? min(p.s.len - t * kTile, kTile) * row : 0);
+    constexpr int HALVES = SHARED ? 1 : 2;
+    CacheTile<KIND, DH, HALVES> tile, later;          // SHARED: of two rounds
+    // the 16 HALVES positions from `at` half tiles on
+    auto there = [&](const Piece& p, const uint8_t* from, int at, int row) {
+        return window(from + (long long)at * (16 * row), at < 2 * p.cached ? max(min(p.s.len - at * 16, 16 * HALVES), 0) * row : 0);
     };
-    auto load_keys = [&](const Piece& p, int t) { tile.load_keys(there(p, p.kc, t, L::row), there(p, p.kx, t, L::srow), lane); };
-    auto load_values = [&](const Piece& p, int t) { tile.load_values(there(p, p.vc, t, L::row), there(p, p.vx, t, L::srow), lane); };
-    const int mine = SHARED ? wave : wp;              // the wave's tile of the first steps
+    auto load_keys = [&](const Piece& p, CacheTile<KIND, DH, HALVES>& x, int at) { x.load_keys(there(p, p.kc, at, L::row), there(p, p.kx, at, L::srow), lane); };
+    auto load_values = [&](const Piece& p, CacheTile<KIND, DH, HALVES>& x, int at) { x.load_values(there(p, p.vc, at, L::row), there(p, p.vx, at, L::srow), lane); };
+    auto load_first = [&](const Piece& p) {
+        if constexpr (SHARED) {
+            load_keys(p, tile, 2 * p.t0 + wave);
+            load_values(p, tile, 2 * p.t0 + wave);
+        } else {
+            load_keys(p, tile, 2 * (p.t0 + wp));
+            load_values(p, tile, 2 * (p.t0 + wp));
+        }
+    };
 
     Piece next;
     next.b = share.b;
     next.off = share.off;
-    next.s = sequence(a, next.b, ROWS);
+    next.s = sequence<true>(a, next.b, ROWS);
     int left_steps = end - begin;
     piece(next, left_steps);
-    load_keys(next, next.t0 + mine);
-    load_values(next, next.t0 + mine);
+    load_first(next);
     while (next.steps) {
         const Piece now = next;
         const Sequence& s = now.s;
@@ -272,7 +291,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         // The drafted tokens, dealt to the waves that split positions, come first: their loads are on their way together with the
         // queries' and the first keys'.
         for (int t = max(t0, s.cached) + wp; t < t0 + steps; t += WP) {
-            const int j0 = (t - s.cached) * kTile, left = s.count - j0;
+            const int j0 = (t - s.cached) * kTile, left = s.count - j0, lane = anew(tid) & 63, n = lane & 15, g4 = lane >> 4;
             const Window kd = window(a.k + ((long long)b * a.N + j0) * a.k_stride + g * DH, (int)((min(left, kTile) - 1) * a.k_stride + DH) * 2);
             const Window vd = window(a.v + ((long long)b * a.N + j0) * a.v_stride + g * DH, (int)((min(left, kTile) - 1) * a.v_stride + DH) * 2);
             f32x4 sc[MT][2];
@@ -286,6 +305,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                     for (int m = 0; m < MT; ++m) sc[m][h] = mfma(k, q[m][i], i ? sc[m][h] : f32x4{0.f, 0.f, 0.f, 0.f});
                 }
+            __builtin_amdgcn_sched_barrier(0);         // the keys' registers are the values'
             uint32_t rowsv[8][DH / 32];
             uint32_t largest = 0;                      // magnitude bits of the values: infinities and NaN from 0x7f80 on
 #pragma unroll
@@ -301,7 +321,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                 seen[m] = seen_word(a, s, b, token[m], j0);
                 mask_scores(sc[m], seen[m], g4);
             }
-            probabilities<DH, MT>(r, sc, c, ahead, p);
+            raise_maximum<DH, MT>(r, sc, c, ahead);
+                probabilities<DH, MT>(r, sc, c, p);
             auto operand = [&](int f) {
                 uint32_t pairs[8];
 #pragma unroll
@@ -342,38 +363,49 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         }
 
         if constexpr (SHARED) {
-            for (int first = t0; first < cached; first += 4) {
-                uint4* own = lds16 + wave * (2 * KS + NF) * 64 + lane;
+            // A round is two tiles, of which every wave brings 16 positions into operand order; while one round is multiplied the
+            // next one is written beside it and the one after that is on its way from memory.
+            auto write = [&](const CacheTile<KIND, DH, 1>& x, int buffer) {
+                uint4* to = lds16 + (buffer * 2 + wave / 2) * FRAGS * 64 + lane;
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < KS; ++i) own[(h * KS + i) * 64] = tile.key(h, i, lane);
-                load_keys(now, first + 4 + wave);
+                for (int i = 0; i < KS; ++i) to[(wave % 2 * KS + i) * 64] = x.key(0, i, lane);
+                uint2* to8 = reinterpret_cast<uint2*>(to + 2 * KS * 64) + wave % 2;
 #pragma unroll
                 for (int f = 0; f < NF; f += 2) {
-                    uint32_t pairs[8];
+                    uint32_t pairs[4], w[2];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) pairs[j] = tile.value(j, f / 2);
-                    own[(2 * KS + f) * 64] = gather<false>(pairs);
-                    own[(2 * KS + f + 1) * 64] = gather<true>(pairs);
+                    for (int j = 0; j < 4; ++j) pairs[j] = x.value(j, f / 2);
+                    gather<false, 4>(pairs, w);
+                    to8[f * 128] = make_uint2(w[0], w[1]);
+                    gather<true, 4>(pairs, w);
+                    to8[(f + 1) * 128] = make_uint2(w[0], w[1]);
                 }
-                load_values(now, first + 4 + wave);
-                lds_barrier();
-                // operands are read a group ahead of the products that take them: a wave has one tile's latency to itself
+            };
+            // the round of tiles `first` and first + 1 in `buffer`; x: the next round's part
+            auto round = [&](int first, int buffer, CacheTile<KIND, DH, 1>& x) {
                 constexpr int half = NF / 2;
-                uint4 k0[KS], k1[KS], v0[half], v1[half];
-                const uint4* from = lds16 + wp * (2 * KS + NF) * 64 + lane;
+                constexpr bool EARLY = KIND != MOE_CACHE_BF16;         // registers: two rounds in flight take 64 in bf16
 #pragma unroll
-                for (int i = 0; i < KS; ++i) k0[i] = from[i * 64];
-                for (int u = wp; u < 4 && first + u < cached; u += WP) {
+                for (int u = wp; u < 2; u += WP) {
+                    const uint4* from = lds16 + (buffer * 2 + u) * FRAGS * 64 + lane;
+                    uint4 k0[KS], k1[KS], v0[half], v1[half];
                     f32x4 sc[MT][2];
 #pragma unroll
-                    for (int i = 0; i < KS; ++i) k1[i] = from[(KS + i) * 64];
+                    for (int i = 0; i < KS; ++i) k0[i] = from[i * 64];
+                    if (EARLY) {
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) k1[i] = from[(KS + i) * 64];
+                    }
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int i = 0; i < KS; ++i)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) sc[m][0] = mfma(k0[i], q[m][i], i ? sc[m][0] : f32x4{0.f, 0.f, 0.f, 0.f});
+                    if (!EARLY) {
+                        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                        for (int i = 0; i < KS; ++i) k1[i] = from[(KS + i) * 64];
+                    }
 #pragma unroll
                     for (int f = 0; f < half; ++f) v0[f] = from[(2 * KS + f) * 64];
                     __builtin_amdgcn_sched_barrier(0);
@@ -381,13 +413,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                     for (int i = 0; i < KS; ++i)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) sc[m][1] = mfma(k1[i], q[m][i], i ? sc[m][1] : f32x4{0.f, 0.f, 0.f, 0.f});
-                    const int left = s.len - (first + u) * kTile;
+                    const int left = first + u < cached ? s.len - (first + u) * kTile : 0;      // 0: the last round's second tile is none
                     if (left < kTile) {
 #pragma unroll
                         for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
                     }
+                    raise_maximum<DH, MT>(r, sc, c, ahead);
                     uint4 p[MT];
-                    probabilities<DH, MT>(r, sc, c, ahead, p);
+                    probabilities<DH, MT>(r, sc, c, p);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int f = 0; f < half; ++f) v1[f] = from[(2 * KS + half + f) * 64];
@@ -396,14 +429,30 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                     for (int f = 0; f < half; ++f)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(v0[f], p[m], r.o[m][f]);
-                    if (u + WP < 4) from += WP * (2 * KS + NF) * 64;
-#pragma unroll
-                    for (int i = 0; i < KS; ++i) k0[i] = from[i * 64];         // the next tile's, or some again
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int f = 0; f < half; ++f)
 #pragma unroll
                         for (int m = 0; m < MT; ++m) r.o[m][half + f] = mfma(v1[f], p[m], r.o[m][half + f]);
+                    if (u == wp) write(x, buffer ^ 1);         // in the shadow of the products
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (u == wp) {
+                        load_keys(now, x, 2 * first + 12 + wave);
+                        load_values(now, x, 2 * first + 12 + wave);
+                    }
+                }
+                lds_barrier();
+            };
+            if (t0 < cached) {
+                load_keys(now, later, 2 * t0 + 4 + wave);
+                load_values(now, later, 2 * t0 + 4 + wave);
+                write(tile, 0);
+                load_keys(now, tile, 2 * t0 + 8 + wave);
+                load_values(now, tile, 2 * t0 + 8 + wave);
+                lds_barrier();
+                for (int first = t0; first < cached; first += 4) {
+                    round(first, 0, later);
+                    if (first + 2 < cached) round(first + 2, 1, tile);
                 }
                 lds_barrier();
             }
@@ -419,13 +468,14 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                         for (int m = 0; m < MT; ++m) sc[m][h] = mfma(k, q[m][i], i ? sc[m][h] : f32x4{0.f, 0.f, 0.f, 0.f});
                     }
-                load_keys(now, t + WP);
+                load_keys(now, tile, 2 * (t + WP));
                 if (left < kTile) {
 #pragma unroll
                     for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
                 }
                 uint4 p[MT];
-                probabilities<DH, MT>(r, sc, c, ahead, p);
+                raise_maximum<DH, MT>(r, sc, c, ahead);
+                probabilities<DH, MT>(r, sc, c, p);
 #pragma unroll
                 for (int f = 0; f < NF; f += 2) {
                     uint32_t pairs[8];
@@ -438,15 +488,15 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                         r.o[m][f + 1] = mfma(hi, p[m], r.o[m][f + 1]);
                     }
                 }
-                load_values(now, t + WP);
+                load_values(now, tile, 2 * (t + WP));
             }
         }
         // the next part's first keys and values are on their way while this one's rows are finished
         piece(next, left_steps);
-        load_keys(next, next.t0 + mine);
-        load_values(next, next.t0 + mine);
+        load_first(next);
 
         // ---- the rows' results: to out if the item is all this share's, else into its part
+        const int lane = anew(tid) & 63, n = lane & 15, g4 = lane >> 4;
         const bool whole = steps == s.tiles;
         const size_t slot = partial_slot(w, now.first);
         auto put = [&](int row, int first, const float* v, int count, float m, float l) {      // elements first.. of a row of the block
@@ -473,7 +523,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         if constexpr (WP == 1) {
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const float l = r.l[m][0];
+                const float l = row_sum(r.l[m]);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     float v[8];
@@ -486,7 +536,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
             float* ml = lds + 4 * QT * OS;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-                const float l = r.l[m][0];
+                const float l = row_sum(r.l[m]);
                 float* o = lds + (wave * QT + m * 16 + n) * OS;
                 if (g4 == 0) { ml[(wave * QT + m * 16 + n) * 2] = r.mc[m]; ml[(wave * QT + m * 16 + n) * 2 + 1] = l; }
 #pragma unroll
@@ -529,7 +579,7 @@ template <int KIND, int DH, int MT, int WR> int launch_tree_instance(const TreeA
 
 template <int KIND> int launch_tree_kind(const TreeArgs& a, const TreeParts& p, int head_dim, int mt, int wr, hipStream_t s) {
 #define MOE_TREE(DH) \
-    (mt == 1 ? launch_tree_instance<KIND, DH, 1, 1>(a, p, s) : wr == 1 ? launch_tree_instance<KIND, DH, 2, 1>(a, p, s) \
+    (wr == 1 ? launch_tree_instance<KIND, DH, 1, 1>(a, p, s) : mt == 1 ? launch_tree_instance<KIND, DH, 1, 2>(a, p, s) \
      : wr == 2 ? launch_tree_instance<KIND, DH, 2, 2>(a, p, s) : launch_tree_instance<KIND, DH, 2, 4>(a, p, s))
     const int rc = head_dim == 128 ? MOE_TREE(128) : MOE_TREE(64);
 #undef MOE_TREE
