@@ -14,7 +14,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;              // positions per step of a wave; one word of a row's mask
-constexpr int kMaxGroups = 512;        // shares: two work-groups per CU
+constexpr int kMaxGroups = 768;
 constexpr int kItemSteps = 8;          // what an item's beginning and end take, in steps
 constexpr int kLeastSteps = 4;         // steps of a wave below which an item is not cut
 constexpr float kLowest = -3.40282347e38f;

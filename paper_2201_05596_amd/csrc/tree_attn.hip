@@ -100,12 +100,16 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
     else *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
 }
 
-static TreePlan tree_plan(int R, int N, int head_dim) {
+static TreePlan tree_plan(int R, int N, int head_dim, int kind) {
     const int rows = N * R;                                   // at most, per key/value head
     TreePlan p;
     p.mt = rows <= 32 ? 1 : 2;
     p.wr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
-    p.groups = kMaxGroups;
+    // Shares are as many as work-groups run at once.  Two per CU have enough of the cache on its way, and a third only adds ends of
+    // items (64 sequences of 1024 positions, 16 heads of 128 in bf16: 99 us with 512, 112 with 768), unless a wave's tile is
+    // small: 4096 positions in 4 bits 128 / 111 us, heads of 64 in 8 bits 117 / 103, in 4 bits 77 / 69.
+    const int tile = 2 * kTile * head_dim * (kind == MOE_CACHE_BF16 ? 16 : kind == MOE_CACHE_FP8 ? 8 : 4) / 8;
+    p.groups = p.wr == 1 && tile <= 4096 ? kMaxGroups : 512;
     const int block = 16 * p.mt * p.wr;
     p.row_blocks = (rows + block - 1) / block;
     p.partial_bytes = (size_t)2 * p.groups * block * head_dim * sizeof(float);
@@ -113,17 +117,17 @@ static TreePlan tree_plan(int R, int N, int head_dim) {
     return p;
 }
 size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft) {
-    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
+    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim, c->kind);
     return p.partial_bytes + p.ml_bytes + (size_t)p.groups * sizeof(int4);
 }
 // steps of all items together, at most
 long long tree_attn_steps(const moe_cache_shape_t* c, int n_draft) {
-    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim);
+    const TreePlan p = tree_plan(c->n_heads / c->n_kv_heads, n_draft, c->head_dim, c->kind);
     return (long long)c->n_seq * c->n_kv_heads * p.row_blocks * ((c->max_len + kTile - 1) / kTile + (n_draft + kTile - 1) / kTile + kItemSteps);
 }
 
 int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStream_t s) {
-    const TreePlan p = tree_plan(a.R, a.N, head_dim);
+    const TreePlan p = tree_plan(a.R, a.N, head_dim, kind);
     char* at = static_cast<char*>(ws);
     const TreeParts parts{reinterpret_cast<float*>(at), reinterpret_cast<float*>(at + p.partial_bytes),
                           reinterpret_cast<int4*>(at + p.partial_bytes + p.ml_bytes), p.groups};

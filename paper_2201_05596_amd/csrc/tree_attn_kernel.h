@@ -165,16 +165,33 @@ template <int DH, int MT> __device__ __forceinline__ void raise_maximum(Rows<DH,
         }
     }
 }
-// A tile's scores -> probabilities, as the second product's operands
-template <int DH, int MT> __device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, uint4 (&out)[MT]) {
+// A tile's scores -> probabilities, as the second product's operands.  Rounded to bf16 they add as much to the result's error as
+// its own rounding does (1.3 to 1.4 times the error without); PARTS = 2 keeps what is left in a second number, for a product more.
+template <int DH, int MT, int PARTS>
+__device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, uint4 (&out)[MT][PARTS]) {
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         float p[8];
+        uint32_t w[PARTS][4];
 #pragma unroll
         for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i / 4][i % 4], c, -r.mc[t]));
         r.l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        out[t] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+#pragma unroll
+        for (int n = 0; n < PARTS; ++n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[n][i] = pack_bf16x2(p[2 * i], p[2 * i + 1]);
+                p[2 * i] -= __uint_as_float(w[n][i] << 16);
+                p[2 * i + 1] -= __uint_as_float(w[n][i] & 0xffff0000u);
+            }
+            out[t][n] = make_uint4(w[n][0], w[n][1], w[n][2], w[n][3]);
+        }
     }
+}
+template <int PARTS> __device__ __forceinline__ f32x4 add_values(const uint4& v, const uint4 (&p)[PARTS], f32x4 o) {
+#pragma unroll
+    for (int n = PARTS - 1; n >= 0; --n) o = mfma(v, p[n], o);
+    return o;
 }
 
 // bits of the row's 32 positions that it sees: the others have no score
@@ -189,6 +206,7 @@ template <int KIND, int DH, int MT, int WR>
 __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
     typedef Layout<KIND, DH> L;
     constexpr int WP = 4 / WR, QT = 16 * MT, ROWS = QT * WR, KS = DH / 32, NF = DH / 16, OS = DH + 4, FRAGS = 2 * KS + NF;
+    constexpr int PARTS = MT == 1 ? 2 : 1;            // up to 32 rows per key/value head the reading of the cache is what takes the time
     constexpr bool SHARED = WR > 1;                   // a tile is in operand order in LDS, for all waves; else in its own wave's registers
     extern __shared__ uint4 lds16[];                  // SHARED: [2 rounds][2 tiles][FRAGS][64]; WP > 1, behind the steps: [4][QT][OS] and [4][QT][2] floats
     float* lds = reinterpret_cast<float*>(lds16);
@@ -314,7 +332,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                 for (int i = 0; i < DH / 32; ++i) largest = max(largest, max(rowsv[j][i] & 0x7fffu, (rowsv[j][i] >> 16) & 0x7fffu));
             }
-            uint4 p[MT];
+            uint4 p[MT][PARTS];
             uint32_t seen[MT];
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -322,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                 mask_scores(sc[m], seen[m], g4);
             }
             raise_maximum<DH, MT>(r, sc, c, ahead);
-                probabilities<DH, MT>(r, sc, c, p);
+                probabilities<DH, MT, PARTS>(r, sc, c, p);
             auto operand = [&](int f) {
                 uint32_t pairs[8];
 #pragma unroll
@@ -358,7 +376,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
             for (int f = 0; f < NF; ++f) {
                 const uint4 v = operand(f);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(v, p[m], r.o[m][f]);
+                for (int m = 0; m < MT; ++m) r.o[m][f] = add_values<PARTS>(v, p[m], r.o[m][f]);
             }
         }
 
@@ -419,8 +437,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                         for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
                     }
                     raise_maximum<DH, MT>(r, sc, c, ahead);
-                    uint4 p[MT];
-                    probabilities<DH, MT>(r, sc, c, p);
+                    uint4 p[MT][PARTS];
+                    probabilities<DH, MT, PARTS>(r, sc, c, p);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int f = 0; f < half; ++f) v1[f] = from[(2 * KS + half + f) * 64];
@@ -428,12 +446,12 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                     for (int f = 0; f < half; ++f)
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) r.o[m][f] = mfma(v0[f], p[m], r.o[m][f]);
+                        for (int m = 0; m < MT; ++m) r.o[m][f] = add_values<PARTS>(v0[f], p[m], r.o[m][f]);
                     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
                     for (int f = 0; f < half; ++f)
 #pragma unroll
-                        for (int m = 0; m < MT; ++m) r.o[m][half + f] = mfma(v1[f], p[m], r.o[m][half + f]);
+                        for (int m = 0; m < MT; ++m) r.o[m][half + f] = add_values<PARTS>(v1[f], p[m], r.o[m][half + f]);
                     if (u == wp) write(x, buffer ^ 1);         // in the shadow of the products
                     __builtin_amdgcn_sched_barrier(0);
                     if (u == wp) {
@@ -473,9 +491,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                     for (int m = 0; m < MT; ++m) mask_scores(sc[m], (1u << left) - 1, g4);
                 }
-                uint4 p[MT];
+                uint4 p[MT][PARTS];
                 raise_maximum<DH, MT>(r, sc, c, ahead);
-                probabilities<DH, MT>(r, sc, c, p);
+                probabilities<DH, MT, PARTS>(r, sc, c, p);
 #pragma unroll
                 for (int f = 0; f < NF; f += 2) {
                     uint32_t pairs[8];
@@ -484,8 +502,8 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                     const uint4 lo = gather<false>(pairs), hi = gather<true>(pairs);
 #pragma unroll
                     for (int m = 0; m < MT; ++m) {
-                        r.o[m][f] = mfma(lo, p[m], r.o[m][f]);
-                        r.o[m][f + 1] = mfma(hi, p[m], r.o[m][f + 1]);
+                        r.o[m][f] = add_values<PARTS>(lo, p[m], r.o[m][f]);
+                        r.o[m][f + 1] = add_values<PARTS>(hi, p[m], r.o[m][f + 1]);
                     }
                 }
                 load_values(now, tile, 2 * (t + WP));
