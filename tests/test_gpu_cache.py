@@ -144,3 +144,34 @@ def test_cache_behind_32_bits(kind, L):
     want = to_f32_numpy(x) if kind == "bf16" else drf.dequantise(*drf.quantise(to_f32_numpy(x), kind), kind)
     assert np.array_equal(to_f32_numpy(k), want) and torch.equal(k, v)
     assert bool((kc[0, 0, :4] == 3).all()) and bool((kc[0, 0, L - 4:] == 3).all())
+
+
+@pytest.mark.parametrize("kind,dh", [("bf16", 64), ("fp8", 128), ("fp4", 64), ("fp4", 128), ("fp8", 64)])
+def test_cache_many_rows(kind, dh):
+    """Rows enough for two units per thread, an odd number of them, some left out; what is read equals what a few rows at a time give."""
+    m = U.amd()
+    gen = torch.Generator(device=DEV).manual_seed(8)
+    B, G, L = 3, 4, 11003
+    n = B * L - 2
+    assert n * G * dh >= 1 << 23
+    print("case cache many", kind, dh, flush=True)
+    cache = m.make_cache_shape(B, G, G, dh, L, kind)
+    x, y = (torch.randn((n, G * dh), generator=gen, device=DEV).to(torch.bfloat16) for _ in "kv")
+    order = torch.randperm(B * L, generator=gen, device=DEV)[:n]
+    seq, pos = (order // L).to(torch.int32), (order % L).to(torch.int32)
+    pos[7::13] = -1
+    one, few = m.alloc_cache(cache, DEV), m.alloc_cache(cache, DEV)
+    m.moe_cache_write(cache, x, y, seq, pos, *one)
+    for a in range(0, n, 4096 // 16 * 16):
+        b = min(n, a + 4096 // 16 * 16)
+        m.moe_cache_write(cache, x[a:b], y[a:b], seq[a:b].clone(), pos[a:b].clone(), *few)
+    assert all(s is None or torch.equal(s, t) for s, t in zip(one, few))
+    k, v = torch.full_like(x, 5.0), torch.full_like(y, 5.0)
+    m.moe_cache_read(cache, *one, seq, pos, k, v)
+    some = torch.arange(0, n, 997, device=DEV)
+    for rows, back in ((x, k), (y, v)):
+        want = to_f32_numpy(rows[some]).reshape(-1, G, dh)
+        if kind != "bf16":
+            want = drf.dequantise(*drf.quantise(want, kind), kind)
+        want[(pos[some] < 0).cpu().numpy()] = 5.0
+        assert np.array_equal(to_f32_numpy(back[some]).reshape(-1, G, dh), want)

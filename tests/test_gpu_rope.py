@@ -98,3 +98,31 @@ def test_rope_nonfinite_stays_in_its_pair():
     m.moe_rope(rope, x, m.moe_rope_frequencies(rope, DEV), torch.tensor([3, 9], dtype=torch.int32, device=DEV), out)
     bad = ~torch.isfinite(out)
     assert sorted(map(tuple, bad.nonzero().tolist())) == [(0, 3), (0, 19), (1, 64 + 4), (1, 64 + 20)]
+
+
+@pytest.mark.parametrize("heads,dh", [(1, 64), (3, 128), (2, 8)])
+def test_rope_several_rows_per_work_group(heads, dh):
+    pos = torch.randint(-3, 9000, (16387,), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV, dtype=torch.int32)
+    print("case rope rows", heads, dh, flush=True)
+    _check(16387, heads, dh, dh, "half", pos=pos, before=8)
+    _check(16387, heads, dh, 8, "interleaved", dtype="f32", pos=pos, in_place=True, behind=4)
+
+
+def test_rope_captured():
+    m = U.amd()
+    rope = m.make_rope(64, 64, "half", "bf16", scaling="linear", factor=3.0)
+    turns, pos = m.moe_rope_frequencies(rope, DEV), torch.arange(9, dtype=torch.int32, device=DEV)
+    x = torch.randn((9, 256), device=DEV).to(torch.bfloat16)
+    out = torch.zeros_like(x)
+    m.moe_rope(rope, x, turns, pos, out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.moe_rope(rope, x, turns, pos, out)
+    for _ in range(3):
+        pos.add_(1000)
+        x.mul_(-1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        m.moe_rope(rope, x, turns, pos, out)
+        assert torch.equal(got, out)

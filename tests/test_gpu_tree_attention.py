@@ -264,3 +264,77 @@ def test_tree_cache_behind_32_bits():
     small.qkv.zero_()
     got = small.run()[4 * N:].float()
     assert (got - 1.0).abs().max() <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("kind,dh", [("bf16", 128), ("fp8", 64)])
+def test_tree_many_sequences(kind, dh):
+    """More sequences than a wave has lanes, ragged, with empty ones and such without drafted tokens among them, at both ends too."""
+    rng = np.random.default_rng(4)
+    for B, N in ((65, 3), (203, 5)):
+        lens, counts = rng.integers(0, 120, B), rng.integers(0, N + 1, B)
+        lens[::7], counts[::5] = 0, 0
+        lens[3] = 1200                                  # one that takes as long as many others
+        print("case tree many sequences", kind, B, flush=True)
+        s = Step(kind, B, N, 2, 1, dh, 1200, [int(v) for v in lens], [int(v) for v in counts], seed=B)
+        s.run()
+        s.check()
+
+
+def test_tree_nothing_to_do():
+    """No drafted token anywhere: out stays as it is."""
+    s = Step("bf16", 3, 4, 2, 1, 64, 50, [50, 0, 7], [0, 0, 0])
+    s.run()
+    s.check()
+
+
+@pytest.mark.parametrize("N,H,G", [(8, 2, 1), (16, 2, 1), (17, 2, 1), (32, 2, 1), (33, 2, 1), (64, 2, 1), (65, 2, 1), (100, 6, 2)])
+def test_tree_rows_at_the_edges_of_the_blocks(N, H, G):
+    """Rows per key/value head on both sides of every choice of tile, and blocks of rows beyond 128, over shares that end inside an item."""
+    for kind, dh, L in (("fp8", 128, 700), ("bf16", 128, 333), ("fp4", 64, 500)):
+        print("case tree rows", N, H, G, kind, flush=True)
+        s = Step(kind, 2, N, H, G, dh, L, [L, L // 3], seed=N)
+        s.run()
+        s.check()
+
+
+def test_tree_rows_with_distances_of_their_own():
+    s = Step("bf16", 2, 5, 4, 2, 64, 90, [90, 44], seed=3)
+    want = s.run().clone()
+    q, k, v = (s.qkv[:, a:b] for a, b in ((0, 256), (256, 384), (384, 512)))
+    far = torch.zeros((10, 4096), dtype=torch.bfloat16, device=DEV)
+    far[:, 1024:1152] = k
+    apart = torch.zeros((10, 136), dtype=torch.bfloat16, device=DEV)
+    apart[:, 8:] = v
+    s.out.fill_(9.0)
+    U.amd().moe_tree_attention(s.shape, 5, q.contiguous(), far[:, 1024:1152], apart[:, 8:], *s.caches, s.lens, s.counts, s.tree, s.out, s.ws)
+    assert torch.equal(s.out, want)
+
+
+def test_tree_seen_nonfinite():
+    """NaN in a cached key or value is for all that see it; keys of minus infinity alone leave no probability (NaN), one among others none of it."""
+    s = Step("bf16", 3, 4, 2, 2, 64, 40, [40, 40, 1], tree=np.zeros((3, 4, 1), np.int32), seed=6)
+    ks, vs = s.caches[0], s.caches[1]
+    ks[0, 0, 5, 3] = float("nan")
+    vs[1, 1, 39, 7] = float("nan")
+    s.qkv[:, :64] = s.qkv[:, :64].abs()
+    ks[2, 0, 0] = float("-inf")
+    got, ref = (s.run(), s.check())[1]
+    assert np.isnan(got[0, :, 0]).all() and np.isfinite(got[0, :, 1]).all()
+    assert np.isnan(got[1, :, 1, 7]).all() and np.isfinite(got[1, :, 1, :7]).all() and np.isfinite(got[1, :, 0]).all()
+    assert np.isnan(got[2, :, 0]).all() and np.isfinite(got[2, :, 1]).all()
+
+
+def test_tree_two_calls_at_once():
+    """Two streams, a workspace each."""
+    a, b = Step("fp8", 4, 8, 8, 2, 128, 2000, [2000, 5, 999, 1500], seed=1), Step("bf16", 2, 40, 4, 1, 64, 900, [900, 33], seed=2)
+    wants = [s.run().clone() for s in (a, b)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for s in (a, b):
+        s.out.fill_(9.0)
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, st in zip((a, b), streams):
+            with torch.cuda.stream(st):
+                s.run()
+    torch.cuda.synchronize()
+    assert torch.equal(a.out, wants[0]) and torch.equal(b.out, wants[1])
