@@ -366,11 +366,13 @@ int moe_cache_read(const moe_cache_shape_t* cache, int32_t n_rows, const void* k
  *         row is set; NULL: token i sees tokens 0..i.  Bits from counts[b] on are ignored.
  *   out   [T, n_heads * head_dim]: out[b, i, h] = softmax(q . K^T / sqrt(head_dim)) V over what it sees; exactly 0 if it
  *         sees nothing.  Rows from counts[b] on stay as they are.
- * Keys and values that a token does not see have no part in its result, whatever they hold.  Softmax statistics and sums
+ * Keys and values that a token does not see have no part in its result, whatever they hold.  (An infinite element of a
+ * cached value that is seen gives an infinity or NaN; drafted tokens' infinities add up as they are.)  Softmax statistics and sums
  * are in 32 bits; for the product with the values the probabilities are rounded to two bf16 numbers each (16 bits), and to
  * one where more than 32 rows (n_draft * n_heads / n_kv_heads) share a key/value head.  The caches are only read.
  * n_seq * n_draft * n_heads is below 2^31, and 2^30 is above the steps of 32 positions that the longest lengths take: n_seq *
- * n_kv_heads * ceil(max_len / 32 + n_draft / 32), times what 128 go into n_draft * n_heads / n_kv_heads.  ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */
+ * n_kv_heads * (ceil(max_len / 32) + ceil(n_draft / 32) + 8) * ceil(n_draft * n_heads / n_kv_heads / 128).
+ * ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */
 size_t moe_tree_attention_workspace_bytes(const moe_cache_shape_t* cache, int32_t n_draft);
 int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const void* q, int64_t q_stride, const void* k,
                        int64_t k_stride, const void* v, int64_t v_stride, const void* k_cache, const void* v_cache,

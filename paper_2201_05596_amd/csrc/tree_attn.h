@@ -4,6 +4,11 @@
 // scores K Q^T in tiles of 16 positions x 16 rows, then O^T += V^T P^T, with one pass over the positions and a running maximum
 // and sum per row.  The first product's result is laid out as the second one's operand has to be, so probabilities stay in
 // their lanes; keys go from memory into operand order by the choice of addresses, values by a transposition in registers.
+// Up to about 64 rows per key/value head the reading of the cache bounds it, beyond that the matrix unit, which the rounds of two
+// tiles keep busy for about 0.6 of their time (the rest are the softmax, the change of order and the rounds' barriers).  us without
+// the merge (5 to 11): 64 sequences of 64 to 2040 positions, 16 heads of 128 in bf16, 8 tokens each: 107 (5.2 TB/s); 128 of 1 to
+// 4095, 8 heads in 8 bits, 4 rows each: 104 (5.3 TB/s); 16 of 2000 to 16001, 8 heads in 8 bits, 128 rows each: 102 (590 TFLOP/s); 8 of
+// 3000 to 8100, 4 heads in bf16, 512 rows each: 62 (600 TFLOP/s); at lengths where the items' ends vanish 6.2 TB/s, 600 to 880 TFLOP/s.
 #pragma once
 
 #include "cache_kind.h"
@@ -15,8 +20,13 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;              // positions per step of a wave; one word of a row's mask
 constexpr int kMaxGroups = 768;
-constexpr int kItemSteps = 8;          // what an item's beginning and end take, in steps
-constexpr int kLeastSteps = 4;         // steps of a wave below which an item is not cut
+// What an item's beginning and end take, in steps.  us of the kernel with 0 / 4 / 8 / 12: 64 sequences of 50 to 1024 positions, 16
+// heads of 128 in bf16 136 / 107 / 102 / 105; 64 of 100 to 8192, 8 heads in 8 bits 132 / 120 / 107 / 105
+constexpr int kItemSteps = 8;
+// Steps of a wave below which an item is not cut: smaller shares end sooner, but leave more to merge.  us of both kernels with
+// 1 / 2 / 4 / 8, one sequence of 8 heads of 128 in 8 bits: 256 positions 14 / 15 / 11 / 11, 2048 19 / 21 / 19 / 23, 16384
+// 28 / 29 / 31 / 42; four of 16384 23 / 23 / 25 / 30
+constexpr int kLeastSteps = 4;
 constexpr float kLowest = -3.40282347e38f;
 
 struct TreePlan {                      // how the host sets a call up

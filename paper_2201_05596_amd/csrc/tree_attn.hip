@@ -145,7 +145,7 @@ int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStr
     const int block = 16 * p.mt * p.wr;
     const long long items = (long long)a.n_seq * a.G * p.row_blocks;
     const bool many = items * 8 <= p.groups;                  // parts per item
-    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * (a.R) + 15) / 16));
+    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * a.R + 15) / 16));
     static_assert(kMaxGroups <= 1024, "a thread per share");
 #define MOE_MERGE(DH) \
     do { \

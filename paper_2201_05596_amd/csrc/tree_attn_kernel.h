@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                 mask_scores(sc[m], seen[m], g4);
             }
             raise_maximum<DH, MT>(r, sc, c, ahead);
-                probabilities<DH, MT, PARTS>(r, sc, c, p);
+            probabilities<DH, MT, PARTS>(r, sc, c, p);
             auto operand = [&](int f) {
                 uint32_t pairs[8];
 #pragma unroll

@@ -338,3 +338,19 @@ def test_tree_two_calls_at_once():
                 s.run()
     torch.cuda.synchronize()
     assert torch.equal(a.out, wants[0]) and torch.equal(b.out, wants[1])
+
+
+@pytest.mark.parametrize("kind,dh,N", [("bf16", 64, 4), ("bf16", 128, 70), ("fp8", 128, 16), ("fp4", 64, 3), ("fp4", 128, 33), ("fp8", 64, 20)])
+def test_tree_every_length(kind, dh, N):
+    """Lengths that leave every number of positions in a tile, with NaN right behind each."""
+    lens = list(range(70))
+    print("case tree every length", kind, dh, N, flush=True)
+    s = Step(kind, len(lens), N, 2, 1, dh, 70, lens, [1 + b % N for b in lens], seed=N)
+    for b, n in enumerate(lens):
+        for cache, scale in zip(s.caches[:2], s.caches[2:]):
+            if kind == "bf16":
+                cache[b, :, n:] = float("nan")
+            else:
+                scale[b, :, n:] = 255
+    s.run()
+    s.check()
