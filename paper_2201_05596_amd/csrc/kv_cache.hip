@@ -1,8 +1,10 @@
 // Rows of keys and values into the caches, quantised as they are written, and back.
 // Bound by traffic.  A unit of work is 8 elements: 16 bytes of a row, and 16, 8 or 4 bytes of the cache.  A work-group takes
 // some rows of one head's keys or values: rows that follow each other in a sequence (a prefill, a prefix) are consecutive in
-// the cache, and so are their scales.  Reading 65536 positions of 8 heads of 128 from 8 bits takes 80 us, 5.1 TB/s, where a large
-// copy reaches 5.2; writing 64000 such rows 94 us, 3.9 TB/s (rows of other heads lie between a head's, 256 bytes each).
+// the cache, and so are their scales.  Reading 65536 positions of 8 heads of 128 from 8 bits takes 78 us, 5.2 TB/s, as a large
+// copy; writing and reading them 144 us, 5.6 TB/s.
+#include <algorithm>
+
 #include "cache_kind.h"
 
 namespace moe {
@@ -25,26 +27,39 @@ __device__ __forceinline__ long long cache_row(const CacheRows& a, int r, int g)
     return ((long long)b * a.G + g) * a.max_len + p;
 }
 
-// A thread has IT units of rows STEP apart, all their loads on the way before the first is used.
-template <int KIND, int DH, int IT>
+// The heads of the same rows follow each other, keys and values in turn: so a row's pieces are read (written, in the reverse) at
+// about the same time, whatever the number of heads.  us for 65536 rows of 8 heads of 128 with the rows of one head following each
+// other / so: written to bf16 104 / 88, 8 bits 97 / 81, 4 bits 90 / 74, read from 8 bits 82 / 80; heads of 64 the same either way.
+constexpr int kGridY = 32768;
+__device__ __forceinline__ int first_row(int rows_per_block) { return (blockIdx.z * kGridY + blockIdx.y) * rows_per_block; }
+// BIG: a call of so many rows that what it stores is out of the caches before anybody can read it: stores that leave no trace there,
+// and two units per thread, all their loads on the way before the first is used (bf16 rows, which are only moved: one).
+template <bool BIG, typename T> __device__ __forceinline__ void store(void* at, T v) {
+    if constexpr (BIG) __builtin_nontemporal_store(v, static_cast<T*>(at));
+    else *static_cast<T*>(at) = v;
+}
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <int KIND, bool BIG> constexpr int units() { return BIG && KIND != MOE_CACHE_BF16 ? 2 : 1; }
+template <int KIND, int DH, bool BIG>
 __global__ __launch_bounds__(256) void cache_write_kernel(const CacheRows a) {
-    constexpr int PPR = DH / 8, STEP = 256 / PPR;             // pieces per row, rows per round of the work-group
-    const int tid = threadIdx.x, g = blockIdx.y >> 1, which = blockIdx.y & 1, piece = tid % PPR;
+    constexpr int PPR = DH / 8, STEP = 256 / PPR, IT = units<KIND, BIG>();       // pieces per row; rows of the work-group's first units
+    const int tid = threadIdx.x, g = blockIdx.x >> 1, which = blockIdx.x & 1, piece = tid % PPR, first = first_row(IT * STEP) + tid / PPR;
     const uint16_t* rows = static_cast<const uint16_t*>(a.rows[which]);
     uint8_t* cache = static_cast<uint8_t*>(a.cache[which]);
     long long at[IT];
     uint4 w[IT];
 #pragma unroll
-    for (int n = 0; n < IT; ++n) at[n] = cache_row(a, (blockIdx.x * IT + n) * STEP + tid / PPR, g);
+    for (int n = 0; n < IT; ++n) at[n] = cache_row(a, first + n * STEP, g);
 #pragma unroll
     for (int n = 0; n < IT; ++n) {
-        const int r = (blockIdx.x * IT + n) * STEP + tid / PPR;
+        const int r = first + n * STEP;
         w[n] = at[n] >= 0 ? *reinterpret_cast<const uint4*>(rows + r * a.stride[which] + g * DH + piece * 8) : make_uint4(0, 0, 0, 0);
     }
 #pragma unroll
     for (int n = 0; n < IT; ++n) {
         if constexpr (KIND == MOE_CACHE_BF16) {
-            if (at[n] >= 0) *reinterpret_cast<uint4*>(cache + (at[n] * DH + piece * 8) * 2) = w[n];
+            if (at[n] >= 0) store<BIG>(cache + (at[n] * DH + piece * 8) * 2, u32x4{w[n].x, w[n].y, w[n].z, w[n].w});
         } else {
             uint32_t v[4] = {w[n].x, w[n].y, w[n].z, w[n].w};
             uint32_t top = 0;                                 // magnitudes of bf16 numbers are ordered as their bits are
@@ -80,15 +95,15 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheRows a) {
                 }
             }
             if (at[n] >= 0) {
-                if constexpr (KIND == MOE_CACHE_FP8) *reinterpret_cast<uint2*>(cache + at[n] * DH + piece * 8) = make_uint2(code[0], code[1]);
-                else *reinterpret_cast<uint32_t*>(cache + at[n] * (DH / 2) + piece * 4) = code[0];
+                if constexpr (KIND == MOE_CACHE_FP8) store<BIG>(cache + at[n] * DH + piece * 8, u32x2{code[0], code[1]});
+                else store<BIG>(cache + at[n] * (DH / 2) + piece * 4, code[0]);
             }
             // the row's scale bytes by one lane
             constexpr int blocks = DH / kScaleBlock;
             uint32_t bytes = 0;
-            const int first = (threadIdx.x & 63) - piece;
+            const int lane0 = (tid & 63) - piece;
 #pragma unroll
-            for (int j = 0; j < blocks; ++j) bytes |= (uint32_t)__shfl((int)byte, first + 4 * j) << (8 * j);
+            for (int j = 0; j < blocks; ++j) bytes |= (uint32_t)__shfl((int)byte, lane0 + 4 * j) << (8 * j);
             if (at[n] >= 0 && piece == 0) {
                 if constexpr (blocks == 4) *reinterpret_cast<uint32_t*>(a.scale[which] + at[n] * 4) = bytes;
                 else *reinterpret_cast<uint16_t*>(a.scale[which] + at[n] * 2) = (uint16_t)bytes;
@@ -97,27 +112,36 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheRows a) {
     }
 }
 
-template <int KIND, int DH>
+template <int KIND, int DH, bool BIG>
 __global__ __launch_bounds__(256) void cache_read_kernel(const CacheRows a) {
-    constexpr int PPR = DH / 8;
-    const int tid = threadIdx.x, g = blockIdx.y >> 1, which = blockIdx.y & 1, piece = tid % PPR, r = blockIdx.x * (256 / PPR) + tid / PPR;
+    constexpr int PPR = DH / 8, STEP = 256 / PPR, IT = units<KIND, BIG>();
+    const int tid = threadIdx.x, g = blockIdx.x >> 1, which = blockIdx.x & 1, piece = tid % PPR, first = first_row(IT * STEP) + tid / PPR;
     const uint8_t* cache = static_cast<const uint8_t*>(a.cache[which]);
-    const long long at = cache_row(a, r, g);
-    if (at < 0) return;
-    uint4 w;
-    if constexpr (KIND == MOE_CACHE_BF16) {
-        w = *reinterpret_cast<const uint4*>(cache + (at * DH + piece * 8) * 2);
-    } else {
-        const float scale = scale_value(a.scale[which][at * (DH / kScaleBlock) + piece / 4]);
-        if constexpr (KIND == MOE_CACHE_FP8) {
-            const uint2 c = *reinterpret_cast<const uint2*>(cache + at * DH + piece * 8);
-            w = make_uint4(fp8_pair<false>(c.x, scale), fp8_pair<true>(c.x, scale), fp8_pair<false>(c.y, scale), fp8_pair<true>(c.y, scale));
-        } else {
-            const uint32_t c = *reinterpret_cast<const uint32_t*>(cache + at * (DH / 2) + piece * 4);
-            w = make_uint4(fp4_pair<0>(c, scale), fp4_pair<1>(c, scale), fp4_pair<2>(c, scale), fp4_pair<3>(c, scale));
-        }
+    long long at[IT];
+    uint4 w[IT];                                              // as the cache holds it, then in bf16
+    uint8_t byte[IT];
+#pragma unroll
+    for (int n = 0; n < IT; ++n) at[n] = cache_row(a, first + n * STEP, g);
+#pragma unroll
+    for (int n = 0; n < IT; ++n) {
+        w[n] = make_uint4(0, 0, 0, 0);
+        byte[n] = 0;
+        if (at[n] < 0) continue;
+        if constexpr (KIND == MOE_CACHE_BF16) w[n] = *reinterpret_cast<const uint4*>(cache + (at[n] * DH + piece * 8) * 2);
+        else if constexpr (KIND == MOE_CACHE_FP8) { const uint2 c = *reinterpret_cast<const uint2*>(cache + at[n] * DH + piece * 8); w[n].x = c.x; w[n].y = c.y; }
+        else w[n].x = *reinterpret_cast<const uint32_t*>(cache + at[n] * (DH / 2) + piece * 4);
+        if constexpr (KIND != MOE_CACHE_BF16) byte[n] = a.scale[which][at[n] * (DH / kScaleBlock) + piece / 4];
     }
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(const_cast<void*>(a.rows[which])) + r * a.stride[which] + g * DH + piece * 8) = w;
+#pragma unroll
+    for (int n = 0; n < IT; ++n) {
+        if (at[n] < 0) continue;
+        const uint32_t x = w[n].x, y = w[n].y;
+        const float f = scale_value(byte[n]);
+        if constexpr (KIND == MOE_CACHE_FP8) w[n] = make_uint4(fp8_pair<false>(x, f), fp8_pair<true>(x, f), fp8_pair<false>(y, f), fp8_pair<true>(y, f));
+        if constexpr (KIND == MOE_CACHE_FP4) w[n] = make_uint4(fp4_pair<0>(x, f), fp4_pair<1>(x, f), fp4_pair<2>(x, f), fp4_pair<3>(x, f));
+        const int r = first + n * STEP;
+        store<BIG>(static_cast<uint16_t*>(const_cast<void*>(a.rows[which])) + r * a.stride[which] + g * DH + piece * 8, u32x4{w[n].x, w[n].y, w[n].z, w[n].w});
+    }
 }
 
 static CacheRows cache_rows(const moe_cache_shape_t* c, int n_rows, const void* k, long long ks, const void* v, long long vs, const int32_t* seq,
@@ -127,31 +151,39 @@ static CacheRows cache_rows(const moe_cache_shape_t* c, int n_rows, const void* 
 }
 
 static dim3 cache_grid(const CacheRows& a, int rows_per_block) {
-    return dim3((unsigned)((a.n_rows + rows_per_block - 1) / rows_per_block), (unsigned)(2 * a.G));
+    const int blocks = (a.n_rows + rows_per_block - 1) / rows_per_block;
+    return dim3((unsigned)(2 * a.G), (unsigned)std::min(blocks, kGridY), (unsigned)((blocks + kGridY - 1) / kGridY));
 }
-template <int KIND, int DH> void write_rows(const CacheRows& a, hipStream_t s) {
-    constexpr int step = 256 / (DH / 8);
-    // Two units per thread hide more of the memory's latency where there are work-groups enough: 64000 rows of 8 heads of 128 to
-    // 8 bits 105 / 94 us, of 64 to 4 bits 43 / 36, 8192 rows of 8 heads 11.1 / 10.4, but 64 rows 2.6 / 3.1; bf16 rows, which are only
-    // moved, 103 / 103.
-    if constexpr (KIND != MOE_CACHE_BF16) {
-        if ((long long)a.n_rows * a.G * DH >= 1 << 23) {
-            hipLaunchKernelGGL((cache_write_kernel<KIND, DH, 2>), cache_grid(a, 2 * step), dim3(256), 0, s, a);
-            return;
-        }
-    }
-    hipLaunchKernelGGL((cache_write_kernel<KIND, DH, 1>), cache_grid(a, step), dim3(256), 0, s, a);
+// us of a call for 65536 rows of 8 heads (keys and values), with ordinary stores and one unit / with these and one / with these and two:
+//                            written and read               read
+//     bf16, heads of 128     241 / 164 / 164            131 / 89 / 91
+//     8 bits                 174 / 163 / 144             91 / 82 / 78
+//     4 bits                 170 / 153 / 141             91 / 80 / 82
+//     bf16, heads of 64      118 /  90 /  93             58 / 47 / 50
+//     8 bits                  94 /  85 /  79             47 / 45 / 43
+//     4 bits                  78 /  81 /  76             47 / 27 / 27
+// (two units with ordinary stores: no faster than one).  Both sides of the border, 8000 rows of 8 heads of 128 read from 8 bits 11.1 / 9.0
+// us, of 64 from 4 bits 5.5 / 4.6; with fewer rows the next kernel may find them in the caches, and two units leave too few work-groups
+// (960 rows written to 8 bits 3.2 / 3.5).
+static bool many_rows(const CacheRows& a, int head_dim) { return (long long)a.n_rows * a.G * head_dim >= 1 << 22; }
+template <int KIND, int DH, bool BIG> void write_rows(const CacheRows& a, hipStream_t s) {
+    hipLaunchKernelGGL((cache_write_kernel<KIND, DH, BIG>), cache_grid(a, units<KIND, BIG>() * (256 / (DH / 8))), dim3(256), 0, s, a);
 }
-template <int KIND, int DH> void read_rows(const CacheRows& a, hipStream_t s) {
-    hipLaunchKernelGGL((cache_read_kernel<KIND, DH>), cache_grid(a, 256 / (DH / 8)), dim3(256), 0, s, a);
+template <int KIND, int DH, bool BIG> void read_rows(const CacheRows& a, hipStream_t s) {
+    hipLaunchKernelGGL((cache_read_kernel<KIND, DH, BIG>), cache_grid(a, units<KIND, BIG>() * (256 / (DH / 8))), dim3(256), 0, s, a);
 }
 
+#define MOE_CACHE_KIND(CALL, KIND) \
+    do { \
+        const bool big = many_rows(a, c->head_dim); \
+        if (c->head_dim == 128) big ? CALL<KIND, 128, true>(a, s) : CALL<KIND, 128, false>(a, s); \
+        else big ? CALL<KIND, 64, true>(a, s) : CALL<KIND, 64, false>(a, s); \
+    } while (0)
 #define MOE_CACHE_ROWS(CALL) \
     do { \
-        const bool wide = c->head_dim == 128; \
-        if (c->kind == MOE_CACHE_BF16) wide ? CALL<MOE_CACHE_BF16, 128>(a, s) : CALL<MOE_CACHE_BF16, 64>(a, s); \
-        else if (c->kind == MOE_CACHE_FP8) wide ? CALL<MOE_CACHE_FP8, 128>(a, s) : CALL<MOE_CACHE_FP8, 64>(a, s); \
-        else wide ? CALL<MOE_CACHE_FP4, 128>(a, s) : CALL<MOE_CACHE_FP4, 64>(a, s); \
+        if (c->kind == MOE_CACHE_BF16) MOE_CACHE_KIND(CALL, MOE_CACHE_BF16); \
+        else if (c->kind == MOE_CACHE_FP8) MOE_CACHE_KIND(CALL, MOE_CACHE_FP8); \
+        else MOE_CACHE_KIND(CALL, MOE_CACHE_FP4); \
     } while (0)
 
 int launch_cache_write(const moe_cache_shape_t* c, int n_rows, const void* k, long long k_stride, const void* v, long long v_stride,
@@ -167,5 +199,6 @@ int launch_cache_read(const moe_cache_shape_t* c, int n_rows, const void* kc, co
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 #undef MOE_CACHE_ROWS
+#undef MOE_CACHE_KIND
 
 }  // namespace moe

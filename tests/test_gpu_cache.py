@@ -175,3 +175,22 @@ def test_cache_many_rows(kind, dh):
             want = drf.dequantise(*drf.quantise(want, kind), kind)
         want[(pos[some] < 0).cpu().numpy()] = 5.0
         assert np.array_equal(to_f32_numpy(back[some]).reshape(-1, G, dh), want)
+
+
+def test_cache_more_rows_than_one_grid_dimension():
+    m = U.amd()
+    gen = torch.Generator(device=DEV).manual_seed(9)
+    n = (1 << 20) + 4099
+    print("case cache grid", flush=True)
+    cache = m.make_cache_shape(1, 1, 1, 128, n, "fp8")
+    x, y = (torch.randn((n, 128), generator=gen, device=DEV).to(torch.bfloat16) for _ in "kv")
+    seq, pos = torch.zeros(n, dtype=torch.int32, device=DEV), torch.arange(n, dtype=torch.int32, device=DEV).flip(0).contiguous()
+    held = m.alloc_cache(cache, DEV)
+    m.moe_cache_write(cache, x, y, seq, pos, *held)
+    k, v = torch.zeros_like(x), torch.zeros_like(y)
+    m.moe_cache_read(cache, *held, seq, pos, k, v)
+    some = torch.cat((torch.arange(0, n, 9973, device=DEV), torch.arange(n - 40, n, device=DEV)))
+    for rows, back in ((x, k), (y, v)):
+        want = drf.dequantise(*drf.quantise(to_f32_numpy(rows[some]), "fp8"), "fp8")
+        assert np.array_equal(to_f32_numpy(back[some]), want)
+    assert bool((k.float() - x.float()).abs().max() < 0.5) and bool((v.float() - y.float()).abs().max() < 0.5)
