@@ -126,3 +126,24 @@ def test_rope_captured():
         got = out.clone()
         m.moe_rope(rope, x, turns, pos, out)
         assert torch.equal(got, out)
+
+
+@pytest.mark.parametrize("layout,dh,rot,dtype", [("half", 128, 128, "bf16"), ("half", 64, 24, "bf16"), ("interleaved", 64, 16, "bf16"), ("half", 64, 64, "f32")])
+def test_rope_many_rows(layout, dh, rot, dtype):
+    """Rows enough for the stores of large calls: the same bits as in small calls, in place and into another tensor."""
+    m = U.amd()
+    n, heads = (1 << 24) // (8 * dh) + 5, 8
+    rope = m.make_rope(dh, rot, layout, dtype)
+    turns = m.moe_rope_frequencies(rope, DEV)
+    gen = torch.Generator(device=DEV).manual_seed(2)
+    x = torch.randn((n, heads * dh), generator=gen, device=DEV).to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    pos = torch.randint(-2, 100000, (n,), generator=gen, device=DEV, dtype=torch.int32)
+    print("case rope many", layout, dh, rot, dtype, flush=True)
+    out, want = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    m.moe_rope(rope, x, turns, pos, out)
+    for a in range(0, n, n // 2 + 1):
+        m.moe_rope(rope, x[a:a + n // 2 + 1], turns, pos[a:a + n // 2 + 1].clone(), want[a:a + n // 2 + 1])
+    assert torch.equal(out, want)
+    want = torch.where((pos < 0)[:, None], x, want)
+    m.moe_rope(rope, x, turns, pos, x)
+    assert torch.equal(x, want)
