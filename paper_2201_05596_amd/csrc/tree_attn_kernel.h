@@ -28,22 +28,26 @@ typedef __amdgpu_buffer_rsrc_t Window;
 __device__ __forceinline__ Window window(const void* p, int bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
 }
-template <int BYTES> __device__ __forceinline__ void load_raw(Window p, int at, int plus, uint32_t (&w)[(BYTES + 3) / 4]) {
+// AUX: 2 for bytes that nobody reads again, which need not stay in the caches
+template <int BYTES, int AUX = 0> __device__ __forceinline__ void load_raw(Window p, int at, int plus, uint32_t (&w)[(BYTES + 3) / 4]) {
     if constexpr (BYTES == 16) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b128(p, at, plus, 0);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b128(p, at, plus, AUX);
         w[0] = v[0]; w[1] = v[1]; w[2] = v[2]; w[3] = v[3];
     } else if constexpr (BYTES == 8) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(p, at, plus, 0);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(p, at, plus, AUX);
         w[0] = v[0]; w[1] = v[1];
     } else if constexpr (BYTES == 4) {
-        w[0] = __builtin_amdgcn_raw_buffer_load_b32(p, at, plus, 0);
+        w[0] = __builtin_amdgcn_raw_buffer_load_b32(p, at, plus, AUX);
     } else {
-        w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(p, at, plus, 0);
+        w[0] = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(p, at, plus, AUX);
     }
 }
 
-template <int KIND, int DH, int HALVES> struct CacheTile {        // 16 HALVES positions
+// 16 HALVES positions.  ONCE: each is read by one work-group only, and the cache as a whole is too large to be there still when the
+// next call reads it
+template <int KIND, int DH, int HALVES, bool ONCE> struct CacheTile {
     typedef Layout<KIND, DH> L;
+    static constexpr int AUX = ONCE ? 2 : 0;
     static constexpr int kw = L::kload / 4, vw = (L::vload + 3) / 4;
     uint32_t k[HALVES][L::nk][kw];
     uint32_t v[4 * HALVES][vw];
@@ -55,7 +59,7 @@ template <int KIND, int DH, int HALVES> struct CacheTile {        // 16 HALVES p
 #pragma unroll
         for (int t = 0; t < HALVES; ++t) {
 #pragma unroll
-            for (int n = 0; n < L::nk; ++n) load_raw<L::kload>(kc, r * L::row + g * L::kload, t * 16 * L::row + n * 4 * L::kload, k[t][n]);
+            for (int n = 0; n < L::nk; ++n) load_raw<L::kload, AUX>(kc, r * L::row + g * L::kload, t * 16 * L::row + n * 4 * L::kload, k[t][n]);
             if constexpr (KIND != MOE_CACHE_BF16) {
                 uint32_t w[1];
                 load_raw<L::srow>(kx, r * L::srow, t * 16 * L::srow, w);
@@ -68,7 +72,7 @@ template <int KIND, int DH, int HALVES> struct CacheTile {        // 16 HALVES p
 #pragma unroll
         for (int j = 0; j < 4 * HALVES; ++j) {
             const int at = (j >> 2) * 16 + (j & 3);
-            load_raw<L::vload>(vc, g * 4 * L::row + c * L::vload, at * L::row, v[j]);
+            load_raw<L::vload, AUX>(vc, g * 4 * L::row + c * L::vload, at * L::row, v[j]);
             if constexpr (KIND != MOE_CACHE_BF16) vs[j] = (uint8_t)__builtin_amdgcn_raw_buffer_load_b8(vx, g * 4 * L::srow + c * L::srow / 16, at * L::srow, 0);
         }
     }
@@ -264,13 +268,16 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
     // Keys and values of the next step are loaded into the registers that a step is done with; behind the last step nothing is
     // read (an empty window), so that loads are no branches and their waits are counted
     constexpr int HALVES = SHARED ? 1 : 2;
-    CacheTile<KIND, DH, HALVES> tile, later;          // SHARED: of two rounds
+    // Blocks of rows read the same positions again (WR = 4).  us with loads that leave traces in the caches and without: 64 sequences
+    // of 64 to 2040 positions, 16 heads in bf16 112 / 102, 128 of 1 to 4095 in 8 bits 109 / 101; four blocks of 128 rows 76 / 84
+    typedef CacheTile<KIND, DH, HALVES, WR != 4> Tile;
+    Tile tile, later;                  // SHARED: of two rounds
     // the 16 HALVES positions from `at` half tiles on
     auto there = [&](const Piece& p, const uint8_t* from, int at, int row) {
         return window(from + (long long)at * (16 * row), at < 2 * p.cached ? max(min(p.s.len - at * 16, 16 * HALVES), 0) * row : 0);
     };
-    auto load_keys = [&](const Piece& p, CacheTile<KIND, DH, HALVES>& x, int at) { x.load_keys(there(p, p.kc, at, L::row), there(p, p.kx, at, L::srow), lane); };
-    auto load_values = [&](const Piece& p, CacheTile<KIND, DH, HALVES>& x, int at) { x.load_values(there(p, p.vc, at, L::row), there(p, p.vx, at, L::srow), lane); };
+    auto load_keys = [&](const Piece& p, Tile& x, int at) { x.load_keys(there(p, p.kc, at, L::row), there(p, p.kx, at, L::srow), lane); };
+    auto load_values = [&](const Piece& p, Tile& x, int at) { x.load_values(there(p, p.vc, at, L::row), there(p, p.vx, at, L::srow), lane); };
     auto load_first = [&](const Piece& p) {
         if constexpr (SHARED) {
             load_keys(p, tile, 2 * p.t0 + wave);
@@ -383,7 +390,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
         if constexpr (SHARED) {
             // A round is two tiles, of which every wave brings 16 positions into operand order; while one round is multiplied the
             // next one is written beside it and the one after that is on its way from memory.
-            auto write = [&](const CacheTile<KIND, DH, 1>& x, int buffer) {
+            auto write = [&](const Tile& x, int buffer) {
                 uint4* to = lds16 + (buffer * 2 + wave / 2) * FRAGS * 64 + lane;
 #pragma unroll
                 for (int i = 0; i < KS; ++i) to[(wave % 2 * KS + i) * 64] = x.key(0, i, lane);
@@ -400,7 +407,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                 }
             };
             // the round of tiles `first` and first + 1 in `buffer`; x: the next round's part
-            auto round = [&](int first, int buffer, CacheTile<KIND, DH, 1>& x) {
+            auto round = [&](int first, int buffer, Tile& x) {
                 constexpr int half = NF / 2;
                 constexpr bool EARLY = KIND != MOE_CACHE_BF16;         // registers: two rounds in flight take 64 in bf16
 #pragma unroll
