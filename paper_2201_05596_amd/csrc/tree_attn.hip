@@ -107,10 +107,10 @@ static TreePlan tree_plan(int R, int N, int head_dim, int kind) {
     // their own share the tiles in LDS, 16 rows each while the cache's reading takes the time, else 32.  us for 16 sequences of
     // 4096 positions, 8 key/value heads of 128, in 8 bits and in bf16, with rows x the waves that have their own:
     //                  16 x 1      16 x 2      32 x 2      32 x 4
-    //      16 rows    27 / 44     34 / 47     38 / 47     50 / 50
-    //      32 rows    39 / 72     35 / 46     36 / 49     50 / 51
-    //      64 rows    69 / 127    54 / 60     40 / 51     51 / 54
-    //     128 rows   129 / 244    85 / 142    62 / 69     56 / 67
+    //      16 rows    31 / 48     37 / 49     40 / 50     50 / 50
+    //      32 rows    50 / 88     38 / 50     41 / 52     49 / 51
+    //      64 rows    82 / 145    61 / 87     43 / 55     50 / 54
+    //     128 rows   153 / 268   102 / 157    69 / 93     55 / 68
     p.mt = rows <= 32 ? 1 : 2;
     p.wr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
     // Shares are as many as work-groups run at once.  Two per CU have enough of the cache on its way, and a third only adds ends of

@@ -269,7 +269,9 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
     // read (an empty window), so that loads are no branches and their waits are counted
     constexpr int HALVES = SHARED ? 1 : 2;
     // Blocks of rows read the same positions again (WR = 4).  us with loads that leave traces in the caches and without: 64 sequences
-    // of 64 to 2040 positions, 16 heads in bf16 112 / 102, 128 of 1 to 4095 in 8 bits 109 / 101; four blocks of 128 rows 76 / 84
+    // of 64 to 2040 positions, 16 heads in bf16 112 / 102, 128 of 1 to 4095 in 8 bits 109 / 101; four blocks of 128 rows 76 / 84.  (A
+    // call on the cache of the call before it, with nothing between, can be slower without: 134 MB in 8 bits 27 / 31; in a model the
+    // other layers' caches and weights pass in between.)
     typedef CacheTile<KIND, DH, HALVES, WR != 4> Tile;
     Tile tile, later;                  // SHARED: of two rounds
     // the 16 HALVES positions from `at` half tiles on
