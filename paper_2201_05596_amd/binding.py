@@ -462,6 +462,14 @@ def _rows(t, device: int, dtype, rows: int, cols: int, name: str):
     return t.data_ptr(), between if rows > 1 else cols
 
 
+def _workspace(ws, device: int, need: int):
+    """(address, bytes) of a workspace tensor of any type; None where nothing is needed (the library then refuses the shape)."""
+    nbytes = 0 if ws is None else ws.numel() * ws.element_size()
+    if nbytes < need:
+        raise ValueError(f"workspace: {nbytes} bytes, this shape needs {need}")
+    return (None, 0) if ws is None else (_at(ws, device, ws.dtype, ws.numel(), "ws"), nbytes)
+
+
 def make_rope(head_dim: int, rot_dim: int, layout, dtype, base: float = 10000.0, amplitude: float = 1.0, scaling="plain",
               factor: float = 1.0, original_len: float = 1.0, low: float = 1.0, high: float = 4.0) -> MoeRope:
     """layout: "half" or "interleaved"; scaling: "plain", "linear" or "by_parts" (or the MOE_ROPE_* numbers)."""
@@ -578,13 +586,11 @@ def moe_tree_attention(cache, n_draft: int, q, k, v, k_cache, v_cache, k_scale, 
     bf, i32, dev = torch.bfloat16, torch.int32, torch._C._cuda_getDevice()
     B, dh = cache.n_seq, cache.head_dim
     T, qw, kw = B * n_draft, cache.n_heads * dh, cache.n_kv_heads * dh
-    need, nbytes = _tree_workspace_need(bytes(cache), n_draft), 0 if ws is None else ws.numel() * ws.element_size()
-    if nbytes < need:
-        raise ValueError(f"workspace: {nbytes} bytes, this shape needs {need}")
+    wp, nbytes = _workspace(ws, dev, _tree_workspace_need(bytes(cache), n_draft))
     rc = load_library().moe_tree_attention(
         ctypes.byref(cache), n_draft, *_rows(q, dev, bf, T, qw, "q"), *_rows(k, dev, bf, T, kw, "k"), *_rows(v, dev, bf, T, kw, "v"),
         *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), _at(lens, dev, i32, B, "lens"), _at(counts, dev, i32, B, "counts"),
-        _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, dev, bf, T, qw, "out"), _at(ws, dev, ws.dtype, ws.numel(), "ws"), nbytes,
+        _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), *_rows(out, dev, bf, T, qw, "out"), wp, nbytes,
         torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_tree_attention", rc)
 
@@ -605,16 +611,14 @@ def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, 
     T, d, E = shape.T, shape.d_model, shape.E
     width = d + 2 * cache.n_kv_heads * cache.head_dim
     w = _block_weights(shape, weights, width)
-    need, nbytes = _draft_workspace_need(bytes(shape), bytes(cache), n_draft), 0 if ws is None else ws.numel() * ws.element_size()
-    if nbytes < need:
-        raise ValueError(f"workspace: {nbytes} bytes, this shape needs {need}")
+    wp, nbytes = _workspace(ws, dev, _draft_workspace_need(bytes(shape), bytes(cache), n_draft))
     rc = load_library().moe_draft_block_forward(
         ctypes.byref(shape), ctypes.byref(cache), n_draft, None if rope is None else ctypes.byref(rope), ctypes.byref(w), _at(x, dev, el, T * d, "x"),
         _at(turns, dev, torch.float64, 0 if rope is None else rope.rot_dim // 2, "turns"), _at(pos, dev, i32, T, "pos"),
         *_cache_args(cache, dev, k_cache, v_cache, k_scale, v_scale), _at(lens, dev, i32, cache.n_seq, "lens"),
         _at(tree, dev, i32, T * ((n_draft + 31) // 32), "tree"), _at(qkv, dev, el, T * width, "qkv"), _at(out, dev, el, T * d, "out"),
         _at(x1_out, dev, el, T * d, "x1_out"), _at(moe_in_out, dev, el, T * d, "moe_in_out"), _at(logits_out, dev, f32, T * E, "logits_out"),
-        _at(ws, dev, ws.dtype, ws.numel(), "ws"), nbytes, torch._C._cuda_getCurrentRawStream(dev))
+        wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_draft_block_forward", rc)
 
 

@@ -211,3 +211,20 @@ def test_draft_block_arguments():
     assert need > 0 and block_call(wsn=need - 1) == -3
     assert B.moe_draft_block_workspace_bytes(s, c, 3) == 0
     assert B.moe_draft_block_workspace_bytes(B.make_shape(8, 512, 1024, 4, 1, 8, "f32"), c, 4) == 0
+
+
+def test_binding_without_a_workspace(device0):
+    """None is a workspace that is too small, and for a shape that is refused the shape's own error."""
+    bf, i32, u8, F = torch.bfloat16, torch.int32, torch.uint8, FakeDevice
+
+    def call(max_len, ws):
+        c = B.make_cache_shape(1, 4, 4, 64, max_len, "bf16")
+        rows = F((4, 256), bf)
+        cache = F((1, 4, max_len, 64), bf)
+        B.moe_tree_attention(c, 4, rows, rows, rows, cache, cache, None, None, F((1,), i32), None, None, rows, ws)
+
+    with pytest.raises(ValueError, match="workspace"):
+        call(100, None)
+    for ws in (None, F((16,), u8)):
+        with pytest.raises(B.MoeError, match="unsupported|not supported|shape"):
+            call((1 << 24) + 1, ws)
