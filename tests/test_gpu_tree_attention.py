@@ -354,3 +354,33 @@ def test_tree_every_length(kind, dh, N):
                 scale[b, :, n:] = 255
     s.run()
     s.check()
+
+
+def test_tree_graphs_that_share_a_workspace():
+    """Two captured calls of different kinds on one workspace, replayed in turn: each finds what it needs written by itself."""
+    steps = [Step("fp8", 3, 9, 8, 2, 128, 3001, [3001, 17, 1200], seed=21), Step("fp4", 2, 20, 8, 2, 64, 900, [900, 1], seed=22)]
+    ws = max((s.ws for s in steps), key=torch.numel)
+    graphs = []
+    for s in steps:
+        s.ws = ws
+        s.run()
+        torch.cuda.synchronize()
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            s.run()
+    wants = [s.run().clone() for s in steps]
+    for _ in range(3):
+        for s, graph, want in zip(steps, graphs, wants):
+            s.out.fill_(9.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(s.out, want)
+            s.check()
+
+
+def test_tree_thousands_of_sequences():
+    B, rng = 4000, np.random.default_rng(7)
+    print("case tree thousands", flush=True)
+    s = Step("fp8", B, 2, 2, 1, 64, 24, [int(v) for v in rng.integers(0, 25, B)], [int(v) for v in rng.integers(0, 3, B)], seed=23)
+    s.run()
+    s.check()
