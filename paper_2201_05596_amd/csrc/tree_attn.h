@@ -29,6 +29,7 @@ constexpr int kItemSteps = 8;
 // 28 / 29 / 31 / 42; four of 16384 23 / 23 / 25 / 30
 constexpr int kLeastSteps = 4;
 constexpr float kLowest = -3.40282347e38f;
+__device__ __forceinline__ float score_factor(int head_dim) { return 1.44269504f * rsqrtf((float)head_dim); }     // c above
 
 struct TreePlan {                      // how the host sets a call up
     int mt, wr;                        // 16-row tiles per wave; waves with rows of their own, the other factor of 4 splits positions
@@ -68,7 +69,7 @@ template <bool SAME> __device__ __forceinline__ Sequence sequence(const TreeArgs
 
 struct TreeParts {                     // workspace: parts of items that lie in several shares
     float* o;                          // [slot][ROWS][DH]
-    float* ml;                         // [slot][ROWS][2]: maximum (times c), sum
+    float* ml;                         // [slot][ROWS][2]: maximum, sum
     int4* split;                       // per share: the item that begins and does not end in it: sequence (-1: none), item, last share, slot
     int groups;
 };

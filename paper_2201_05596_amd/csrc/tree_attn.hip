@@ -17,6 +17,7 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
     constexpr int NF = DH / 16;
     __shared__ float ml[SETS][16][2], o[SETS][16][16][NF];
     const int R = a.R, tid = threadIdx.x;
+    const float c = score_factor(DH);
     int w0 = blockIdx.x;
     if constexpr (SETS > 1) {                                 // few items: the blockIdx.x-th share that has one, not a work-group for each
         __shared__ int some[4 * SETS], found;
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) m = w + u * SETS <= w1 ? fmaxf(m, x[u].x) : m;
-        const float f = __builtin_amdgcn_exp2f(M - m);
+        const float f = __builtin_amdgcn_exp2f((M - m) * c);
         M = m;
         L *= f;
 #pragma unroll
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
             if (w + u * SETS > w1) break;
-            const float h = __builtin_amdgcn_exp2f(x[u].x - m);
+            const float h = __builtin_amdgcn_exp2f((x[u].x - m) * c);
             L += x[u].y * h;
 #pragma unroll
             for (int i = 0; i < NF; ++i) v[i] += e[u][i] * h;
@@ -76,12 +77,12 @@ __global__ __launch_bounds__(256 * SETS) void tree_merge_kernel(const TreeArgs a
         if (set) return;
         const float own = M;
         for (int i = 1; i < SETS; ++i) M = fmaxf(M, ml[i][local][0]);
-        float f = __builtin_amdgcn_exp2f(own - M);
+        float f = __builtin_amdgcn_exp2f((own - M) * c);
         L *= f;
 #pragma unroll
         for (int j = 0; j < NF; ++j) v[j] *= f;
         for (int i = 1; i < SETS; ++i) {
-            f = __builtin_amdgcn_exp2f(ml[i][local][0] - M);
+            f = __builtin_amdgcn_exp2f((ml[i][local][0] - M) * c);
             L += ml[i][local][1] * f;
 #pragma unroll
             for (int j = 0; j < NF; ++j) v[j] += o[i][local][piece][j] * f;

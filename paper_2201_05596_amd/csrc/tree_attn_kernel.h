@@ -132,12 +132,11 @@ __device__ __forceinline__ float row_max(float v) { v = fmaxf(v, __shfl_xor(v, 1
 template <int DH, int MT> struct Rows {          // a wave's rows: lane (n, g) holds row n of every 16, elements (4 g + i) DH / 16 + q in o[.][q][i]
     f32x4 o[MT][DH / 16];
     float l[MT];                                 // sums of the lane's own positions
-    float m[MT], mc[MT];                         // maximum score, and c times it
-    __device__ __forceinline__ void clear(float c) {
+    float m[MT];                                 // maximum score
+    __device__ __forceinline__ void clear() {
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
             m[t] = kLowest;
-            mc[t] = kLowest * c;
             l[t] = 0.f;
 #pragma unroll
             for (int q = 0; q < DH / 16; ++q) o[t][q] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -162,14 +161,14 @@ template <int DH, int MT> __device__ __forceinline__ void raise_maximum(Rows<DH,
         for (int t = 0; t < MT; ++t) {
             const float m = fmaxf(r.m[t], row_max(top[t])), f = __builtin_amdgcn_exp2f((r.m[t] - m) * c);
             r.m[t] = m;
-            r.mc[t] = m * c;
             r.l[t] *= f;
 #pragma unroll
             for (int q = 0; q < DH / 16; ++q) r.o[t][q] *= f;
         }
     }
 }
-// A tile's scores -> probabilities, as the second product's operands.  Rounded to bf16 they add as much to the result's error as
+// A tile's scores -> probabilities, as the second product's operands.  Scores are subtracted before the factor c: of c s - c m, with
+// c m rounded, what rounding leaves grows with the scores, beyond exp2's range from 2^34 on.  Rounded to bf16 they add as much to the result's error as
 // its own rounding does (1.3 to 1.4 times the error without); PARTS = 2 keeps what is left in a second number, for a product more.
 template <int DH, int MT, int PARTS>
 __device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[MT][2], float c, uint4 (&out)[MT][PARTS]) {
@@ -178,7 +177,7 @@ __device__ __forceinline__ void probabilities(Rows<DH, MT>& r, const f32x4 (&s)[
         float p[8];
         uint32_t w[PARTS][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(s[t][i / 4][i % 4], c, -r.mc[t]));
+        for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f((s[t][i / 4][i % 4] - r.m[t]) * c);
         r.l[t] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
         for (int n = 0; n < PARTS; ++n) {
@@ -217,7 +216,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wr = wave / WP, wp = wave % WP, n = lane & 15, g4 = lane >> 4;
     const int R = a.R;
-    const float c = 1.44269504f * rsqrtf((float)DH), ahead = 8.f / c;
+    const float c = score_factor(DH), ahead = 8.f / c;
 
     // consecutive shares on one XCD: they read the same keys and values where an item's rows take several blocks
     const int w = (blockIdx.x % 8) * (parts.groups / 8) + blockIdx.x / 8;
@@ -313,7 +312,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
             for (int i = 0; i < KS; ++i) q[t][i] = *reinterpret_cast<const uint4*>(src + L::dim(i, g4));
         }
         Rows<DH, MT> r;
-        r.clear(c);
+        r.clear();
 
         // The drafted tokens, dealt to the waves that split positions, come first: their loads are on their way together with the
         // queries' and the first keys'.
@@ -556,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
                     float v[8];
 #pragma unroll
                     for (int f = 0; f < NF; ++f) v[f] = r.o[m][f][i];
-                    put(row0 + m * 16 + n, (g4 * 4 + i) * NF, v, NF, r.mc[m], l);
+                    put(row0 + m * 16 + n, (g4 * 4 + i) * NF, v, NF, r.m[m], l);
                 }
             }
         } else {
@@ -565,7 +564,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
             for (int m = 0; m < MT; ++m) {
                 const float l = row_sum(r.l[m]);
                 float* o = lds + (wave * QT + m * 16 + n) * OS;
-                if (g4 == 0) { ml[(wave * QT + m * 16 + n) * 2] = r.mc[m]; ml[(wave * QT + m * 16 + n) * 2 + 1] = l; }
+                if (g4 == 0) { ml[(wave * QT + m * 16 + n) * 2] = r.m[m]; ml[(wave * QT + m * 16 + n) * 2 + 1] = l; }
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -581,7 +580,7 @@ __global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, con
 #pragma unroll
                 for (int i = 0; i < WP; ++i) {
                     const int at = (set * WP + i) * QT + row % QT;
-                    const float f = __builtin_amdgcn_exp2f(ml[at * 2] - M);
+                    const float f = __builtin_amdgcn_exp2f((ml[at * 2] - M) * c);
                     l += ml[at * 2 + 1] * f;
 #pragma unroll
                     for (int j = 0; j < NF; ++j) v[j] += lds[at * OS + first + j] * f;
