@@ -20,7 +20,16 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kTile = 32;              // positions per step of a wave; one word of a row's mask
-constexpr int kMaxGroups = 768;
+constexpr int kComputeUnits = 256;
+// Work-groups of the main kernel that a compute unit takes at once, which is also how many shares there are for it; the kernel is built
+// for so many.  Two have enough of the cache on its way, and a third only adds ends of items (64 sequences of 64 to 2040 positions, 16
+// heads of 128 in bf16: 102 us with 512 shares, 118 with 768), unless a wave's tile is small and its own: 4096 positions in 4 bits
+// 128 / 111 us, heads of 64 in 8 bits 117 / 103, in 4 bits 77 / 69.
+constexpr int groups_per_unit(int kind, int head_dim, int wr) {
+    const int bits = kind == MOE_CACHE_BF16 ? 16 : kind == MOE_CACHE_FP8 ? 8 : 4;
+    return wr == 1 && 2 * kTile * head_dim * bits / 8 <= 4096 ? 3 : 2;
+}
+constexpr int kMaxGroups = 3 * kComputeUnits;
 // What an item's beginning and end take, in steps.  us of the kernel with 0 / 4 / 8 / 12: 64 sequences of 50 to 1024 positions, 16
 // heads of 128 in bf16 136 / 107 / 102 / 105; 64 of 100 to 8192, 8 heads in 8 bits 132 / 120 / 107 / 105
 constexpr int kItemSteps = 8;

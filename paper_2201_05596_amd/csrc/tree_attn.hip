@@ -114,11 +114,7 @@ static TreePlan tree_plan(int R, int N, int head_dim, int kind) {
     //     128 rows   153 / 268   102 / 157    69 / 93     55 / 68
     p.mt = rows <= 32 ? 1 : 2;
     p.wr = rows <= 16 ? 1 : rows <= 64 ? 2 : 4;
-    // Shares are as many as work-groups run at once.  Two per CU have enough of the cache on its way, and a third only adds ends of
-    // items (64 sequences of 64 to 2040 positions, 16 heads of 128 in bf16: 102 us with 512, 118 with 768), unless a wave's tile is
-    // small: 4096 positions in 4 bits 128 / 111 us, heads of 64 in 8 bits 117 / 103, in 4 bits 77 / 69.
-    const int tile = 2 * kTile * head_dim * (kind == MOE_CACHE_BF16 ? 16 : kind == MOE_CACHE_FP8 ? 8 : 4) / 8;
-    p.groups = p.wr == 1 && tile <= 4096 ? kMaxGroups : 512;
+    p.groups = groups_per_unit(kind, head_dim, p.wr) * kComputeUnits;
     const int block = 16 * p.mt * p.wr;
     p.row_blocks = (rows + block - 1) / block;
     p.partial_bytes = (size_t)2 * p.groups * block * head_dim * sizeof(float);

@@ -207,7 +207,7 @@ __device__ __forceinline__ void mask_scores(f32x4 (&s)[2], uint32_t seen, int g)
 }
 
 template <int KIND, int DH, int MT, int WR>
-__global__ __launch_bounds__(256, 2) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
+__global__ __launch_bounds__(256, groups_per_unit(KIND, DH, WR)) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
     typedef Layout<KIND, DH> L;
     constexpr int WP = 4 / WR, QT = 16 * MT, ROWS = QT * WR, KS = DH / 32, NF = DH / 16, OS = DH + 4, FRAGS = 2 * KS + NF;
     // Numbers per probability.  Beyond 32 rows per key/value head a second one takes time that nothing hides.  us with one / two: 16 x 32
