@@ -5,6 +5,7 @@ hipcc cross-compiles without a GPU.  Usage: ``python -m paper_2201_05596_amd.bui
 from __future__ import annotations
 
 import os
+import re
 import subprocess
 import sys
 from concurrent.futures import ThreadPoolExecutor
@@ -26,14 +27,31 @@ FLAGS = [
 ]
 
 
+# Sources whose kernels must keep nothing in scratch memory: a build that does not is refused
+NO_SCRATCH = ("tree_attn_bf16.hip", "tree_attn_fp8.hip", "tree_attn_fp4.hip")
+
+
+def kernels_in_scratch(remarks: str) -> list:
+    """Names of the kernels that the compiler's remarks on resource usage say have values in scratch memory."""
+    sizes = re.findall(r"Function Name: (\S+).*?ScratchSize \[bytes/lane\]: (\d+)", remarks, re.S)
+    if not sizes:
+        raise RuntimeError("the compiler says nothing on resource usage")
+    return [name for name, size in sizes if int(size)]
+
+
 def _compile(src: str) -> str:
     obj_dir = os.path.join(HERE, "_build")
     os.makedirs(obj_dir, exist_ok=True)
     obj = os.path.join(obj_dir, src.replace(".hip", ".o"))
     cmd = [HIPCC, *FLAGS, "-c", os.path.join(CSRC, src), "-o", obj]
+    if src in NO_SCRATCH:
+        cmd.append("-Rpass-analysis=kernel-resource-usage")
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         raise RuntimeError(f"hipcc failed for {src}:\n{r.stdout}\n{r.stderr}")
+    if src in NO_SCRATCH and (bad := kernels_in_scratch(r.stderr)):
+        os.remove(obj)
+        raise RuntimeError(f"{src}: values in scratch memory: {', '.join(bad)}")
     return obj
 
 

@@ -206,6 +206,10 @@ __device__ __forceinline__ void mask_scores(f32x4 (&s)[2], uint32_t seen, int g)
         if (!(seen & (1u << (i / 4 * 16 + i % 4)))) s[i / 4][i % 4] = -INFINITY;
 }
 
+// Nothing of it may be in scratch memory, which build.py and the tests look at.  A version under work kept a share's bookkeeping there
+// (`split`, `Piece`) and got it back wrong; that version is gone and the cause was not found.  (Where an earlier one spilled `split`, its
+// assembly stores the record with all lanes active and loads it in lane 0 alone, as it should, and its results were right.)  Scalars
+// beyond the registers for them are in lanes of one vector register, which nothing else writes.
 template <int KIND, int DH, int MT, int WR>
 __global__ __launch_bounds__(256, groups_per_unit(KIND, DH, WR)) void tree_attn_kernel(const TreeArgs a, const TreeParts parts) {
     typedef Layout<KIND, DH> L;

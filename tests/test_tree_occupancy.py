@@ -1,5 +1,6 @@
 """What the attention for drafted tokens rests on in the built library: as many work-groups per compute unit as there are shares for
-one (a lane has 512 registers for the waves of its SIMD; a unit has 160 KB of LDS)."""
+one (a lane has 512 registers for the waves of its SIMD; a unit has 160 KB of LDS), nothing in scratch memory, and what scalar registers
+do not hold in lanes of a register of its own."""
 import os
 import re
 import subprocess
@@ -53,3 +54,27 @@ def test_work_groups_per_unit(kernels):
         tiles = 4 * (dh // 32 * 2 + dh // 16) * 1024 if wr > 1 else 0
         merge = 4 * 16 * mt * (dh + 4 + 2) * 4 if wr < 4 else 0
         assert (3 if three else 2) * max(tiles, merge) <= 160 * 1024, (kind, dh, mt, wr)
+
+
+def test_nothing_in_scratch_memory(kernels):
+    assert [k for k, (_, scratch, text) in kernels.items() if scratch or "scratch_" in text] == []
+
+
+def test_lanes_that_hold_scalars_are_written_by_nothing_else(kernels):
+    vector = re.compile(r"\bv(?:\[(\d+):(\d+)\]|(\d+)\b)")
+    numbers = lambda text: {n for a, b, c in vector.findall(text) for n in range(int(a or c), int(b or c) + 1)}  # noqa: E731
+    for key, (_, _, text) in kernels.items():
+        code = [line.split("//")[0].strip() for line in text.splitlines()]
+        held = set().union(*(numbers(line.split(",")[0]) for line in code if line.startswith("v_writelane")))
+        assert held, key
+        assert not [line for line in code if not line.startswith(("v_writelane", "v_readlane")) and numbers(line) & held], key
+
+
+def test_a_build_with_scratch_memory_is_refused():
+    remark = lambda name, size: (f"k.h:1:1: remark: Function Name: {name} [-Rpass-analysis=kernel-resource-usage]\n"  # noqa: E731
+                                 f"k.h:1:1: remark:     ScratchSize [bytes/lane]: {size} [-Rpass-analysis=kernel-resource-usage]\n")
+    assert B.kernels_in_scratch(remark("a", 0) + remark("b", 16) + remark("c", 0)) == ["b"]
+    assert B.kernels_in_scratch(remark("a", 0)) == []
+    with pytest.raises(RuntimeError):
+        B.kernels_in_scratch("")
+    assert set(B.NO_SCRATCH) <= set(B.SOURCES)
