@@ -116,8 +116,10 @@ int launch_rope(const moe_rope_t* rope, int n_rows, int n_heads, const void* x, 
     RopeArgs a{x, out, turns, pos, x_stride, out_stride, n_rows, n_heads, rope->head_dim, rope->rot_dim, 1, rope->amplitude};
     // Rows of few pieces together, as long as there are work-groups enough: 16384 rows of one head of 64 10.4 / 4.1 us, of 4 of 128
     // 12.2 / 7.8; of 40 heads a row stays alone (61 us, two rows 63, four 67)
+    // A grid has fewer than 2^32 threads, so that 2^24 rows go two by two.
     const long long pieces = (long long)n_heads * rope->head_dim / 8;
-    while (a.rows_per_block < 16 && a.rows_per_block * pieces < 512 && n_rows / (2 * a.rows_per_block) >= 1024) a.rows_per_block *= 2;
+    const auto more = [&](int rows) { return n_rows / rows >= 1 << 24 || (rows < 16 && rows * pieces < 512 && n_rows / (2 * rows) >= 1024); };
+    while (more(a.rows_per_block)) a.rows_per_block *= 2;
     const dim3 grid((unsigned)((n_rows + a.rows_per_block - 1) / a.rows_per_block));
     const size_t lds = (size_t)a.rows_per_block * (rope->rot_dim / 2) * sizeof(float2);
     const bool copy = out != x, half = rope->layout == MOE_ROPE_HALF;
