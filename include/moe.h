@@ -380,8 +380,8 @@ int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const vo
                        const int32_t* tree, void* out, int64_t out_stride, void* ws, size_t ws_bytes, void* stream);
 
 /* moe_draft_block_forward -- a decoder block (moe_decode_block_forward) over n_draft new tokens per sequence, bf16, with
- * rotary positions, shared key/value heads and a cache of any kind.  With T = shape.T = n_seq * n_draft rows, d = d_model =
- * n_heads * head_dim and G = n_kv_heads:
+ * rotary positions, shared key/value heads and a cache of any kind.  With T = shape.T = n_seq * n_draft rows (fewer
+ * than 2^24), d = d_model = n_heads * head_dim and G = n_kv_heads:
  *   a      = LayerNorm(x; ln1_gamma, ln1_beta)
  *   qkv    = a Wqkv + bqkv                    Wqkv [d, d + 2 G head_dim], columns q | k | v; q and k then turned by moe_rope
  *   o      = moe_tree_attention(q, k, v; cache, lens, tree)

@@ -1360,7 +1360,7 @@ int check_draft_block(const moe_shape_t* s, const moe_cache_shape_t* c, int32_t 
     if (rc == MOE_OK) rc = check_tree(c, n_draft);
     if (rc != MOE_OK) return rc;
     if ((long long)c->n_seq * n_draft != s->T || c->n_heads * c->head_dim != s->d_model) return MOE_ERR_INVALID_ARG;
-    return s->dtype == MOE_BF16 ? MOE_OK : MOE_ERR_UNSUPPORTED;
+    return s->dtype == MOE_BF16 && s->T < kMaxRows ? MOE_OK : MOE_ERR_UNSUPPORTED;       // (256 threads per row, fewer than 2^32 in a grid)
 }
 
 }  // namespace
@@ -1389,7 +1389,6 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
                           static_cast<const void*>(moe_in_out), static_cast<const void*>(logits_out)})
         if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
     const int T = shape->T, d = shape->d_model, H = cache->n_heads, G = cache->n_kv_heads, dh = cache->head_dim, width = (H + 2 * G) * dh;
-    if (T > kMaxRows) return MOE_ERR_UNSUPPORTED;
     const DraftLayout L = draft_layout(shape, cache, n_draft);
     if (!ws || !aligned16(ws) || ws_bytes < L.total) return MOE_ERR_WORKSPACE;
 
