@@ -388,10 +388,14 @@ int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const vo
  *   x1     = x + o Wo + bo
  *   out    = x1 + moe_layer_forward(LayerNorm(x1; ln2_gamma, ln2_beta))
  * rope may be NULL (no rotary positions; turns and pos are NULL then), else pos [T] are the rows' positions, whose q and k
- * stay as they are where pos is negative.  lens, tree and the caches are those of moe_tree_attention; a sequence with fewer
- * tokens has rows that no other token sees (the MoE layer routes them as it does every row).  The caches are not written: qkv [T, d + 2 G head_dim] is an output, of which the
- * caller hands the accepted rows' k and v columns to moe_cache_write.  Weights, exports and flags are those of
- * moe_decode_block_forward.  ws >= moe_draft_block_workspace_bytes(shape, cache, n_draft). */
+ * stay as they are where pos is negative.  lens, tree and the caches are those of moe_tree_attention.  The caches are not
+ * written: qkv [T, d + 2 G head_dim] is an output, of which the caller hands the accepted rows' k and v columns to
+ * moe_cache_write.  Weights, exports and flags are those of moe_decode_block_forward.
+ * All n_draft rows of every sequence are computed.  In a step where some sequences have fewer tokens, the rows behind them
+ * reach no other row's attention (as long as no mask bit of another row is set for them), but the MoE layer routes them as it
+ * does every row: they take places within the experts' capacity, ahead of later sequences' rows, which may then be dropped.
+ * Such a step wants a capacity that the padded rows cannot fill; with capacity = T nothing is ever dropped.
+ * ws >= moe_draft_block_workspace_bytes(shape, cache, n_draft). */
 size_t moe_draft_block_workspace_bytes(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft);
 int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* cache, int32_t n_draft, const moe_rope_t* rope,
                             const moe_block_weights_t* weights, const void* x, const double* turns, const int32_t* pos,
