@@ -1318,7 +1318,7 @@ int moe_tree_attention(const moe_cache_shape_t* cache, int32_t n_draft, const vo
         return MOE_ERR_INVALID_ARG;
     if (!ws || !aligned16(ws) || ws_bytes < align_up(tree_attn_ws_bytes(cache, n_draft))) return MOE_ERR_WORKSPACE;
     const TreeArgs a{u16(q), u16(k), u16(v), q_stride, k_stride, v_stride, out_stride, k_cache, v_cache, k_scale, v_scale,
-                     lens, counts, tree, u16(out), cache->n_seq, n_draft, cache->n_heads, cache->n_kv_heads,
+                     lens, counts, tree, u16(out), cache->n_seq, n_draft, cache->n_kv_heads,
                      cache->n_heads / cache->n_kv_heads, cache->max_len};
     return launch_tree_attn(a, cache->kind, cache->head_dim, ws, static_cast<hipStream_t>(stream));
 }
@@ -1404,7 +1404,7 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
     if (rope) rc = launch_rope(rope, T, H + G, rows, width, turns, pos, rows, width, st);
     if (rc != MOE_OK) return rc;
     const TreeArgs a{rows, rows + H * dh, rows + (H + G) * dh, width, width, width, d, k_cache, v_cache, k_scale, v_scale,
-                     lens, nullptr, tree, attn, cache->n_seq, n_draft, H, G, H / G, cache->max_len};
+                     lens, nullptr, tree, attn, cache->n_seq, n_draft, G, H / G, cache->max_len};
     rc = launch_tree_attn(a, cache->kind, dh, at<void>(ws, L.tree_ws), st);
     if (rc != MOE_OK) return rc;
     return block_tail(shape, w, x, attn, at<uint16_t>(ws, L.proj), x1_out ? u16(x1_out) : at<uint16_t>(ws, L.x1),

@@ -360,7 +360,7 @@ struct TreeArgs {
     const uint8_t *k_scale, *v_scale;
     const int32_t *lens, *counts, *tree;
     uint16_t* out;
-    int n_seq, N, H, G, R, max_len;    // N drafted tokens per sequence, R = H / G
+    int n_seq, N, G, R, max_len;       // N drafted tokens per sequence, R query heads per key/value head
 };
 size_t tree_attn_ws_bytes(const moe_cache_shape_t* c, int n_draft);
 long long tree_attn_steps(const moe_cache_shape_t* c, int n_draft);     // work of the largest call of a shape; below 2^30

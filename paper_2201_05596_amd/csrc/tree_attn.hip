@@ -141,12 +141,12 @@ int launch_tree_attn(const TreeArgs& a, int kind, int head_dim, void* ws, hipStr
     if (rc != MOE_OK) return rc;
     const int block = 16 * p.mt * p.wr;
     const long long items = (long long)a.n_seq * a.G * p.row_blocks;
-    const bool many = items * 8 <= p.groups;                  // parts per item
-    const dim3 grid((unsigned)(many ? items : p.groups), (unsigned)(std::min(block, a.N * a.R + 15) / 16));
+    const bool few = items * 8 <= p.groups;                   // items, which then have many parts each
+    const dim3 grid((unsigned)(few ? items : p.groups), (unsigned)(std::min(block, a.N * a.R + 15) / 16));
     static_assert(kMaxGroups <= 1024, "a thread per share");
 #define MOE_MERGE(DH) \
     do { \
-        if (many) hipLaunchKernelGGL((tree_merge_kernel<DH, 4>), grid, dim3(1024), 0, s, a, parts, block); \
+        if (few) hipLaunchKernelGGL((tree_merge_kernel<DH, 4>), grid, dim3(1024), 0, s, a, parts, block); \
         else hipLaunchKernelGGL((tree_merge_kernel<DH, 1>), grid, dim3(256), 0, s, a, parts, block); \
     } while (0)
     if (head_dim == 128) MOE_MERGE(128);

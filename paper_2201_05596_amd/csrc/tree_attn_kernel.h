@@ -12,7 +12,6 @@ template <int KIND, int DH> struct Layout {
     static constexpr int bits = CacheKind<KIND>::bits;
     static constexpr int row = DH * bits / 8;                     // bytes per position
     static constexpr int srow = KIND == MOE_CACHE_BF16 ? 0 : DH / kScaleBlock;
-    static constexpr int per = 128 / bits;                        // elements in 16 bytes
     static constexpr int kload = DH / 4 * bits / 8 >= 16 ? 16 : DH / 4 * bits / 8;     // bytes per key load
     static constexpr int nk = DH / 4 * bits / 8 / kload;          // key loads per row
     static constexpr int vload = DH / 16 * bits / 8;              // bytes per value load
