@@ -497,12 +497,13 @@ def moe_rope(rope: MoeRope, x, turns, pos, out) -> None:
     rows, cols = x.shape
     if rows == 0:
         return
-    if cols == 0 or cols % rope.head_dim:
+    heads = cols // rope.head_dim if rope.head_dim > 0 else 1      # (no such head: the library refuses the shape)
+    if rope.head_dim > 0 and (cols == 0 or cols % rope.head_dim):
         raise ValueError(f"x: {cols} columns are no heads of {rope.head_dim}")
     dev = torch._C._cuda_getDevice()
     xp, xs = _rows(x, dev, dtype, rows, cols, "x")
     op, os_ = _rows(out, dev, dtype, rows, cols, "out")
-    rc = load_library().moe_rope(ctypes.byref(rope), rows, cols // rope.head_dim, xp, xs, _at(turns, dev, torch.float64, rope.rot_dim // 2, "turns"),
+    rc = load_library().moe_rope(ctypes.byref(rope), rows, heads, xp, xs, _at(turns, dev, torch.float64, rope.rot_dim // 2, "turns"),
                                  _at(pos, dev, torch.int32, rows, "pos"), op, os_, torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_rope", rc)
 
