@@ -367,9 +367,9 @@ int moe_cache_read(const moe_cache_shape_t* cache, int32_t n_rows, const void* k
  *   out   [T, n_heads * head_dim]: out[b, i, h] = softmax(q . K^T / sqrt(head_dim)) V over what it sees; exactly 0 if it
  *         sees nothing.  Rows from counts[b] on stay as they are.
  * Keys and values that a token does not see have no part in its result, whatever they hold.  (An infinite element of a
- * cached value that is seen gives an infinity or NaN; drafted tokens' infinities add up as they are.)  Softmax statistics and sums
- * are in 32 bits; for the product with the values the probabilities are rounded to two bf16 numbers each (16 bits), and to
- * one where more than 32 rows (n_draft * n_heads / n_kv_heads) share a key/value head.  The caches are only read.
+ * value that is seen, whatever its weight, gives an infinity or NaN.)  Softmax statistics and sums are in 32 bits; for the
+ * product with the values the probabilities are rounded to two bf16 numbers each (16 bits), and to one (8 bits) where more
+ * than 32 rows (n_draft * n_heads / n_kv_heads) share a key/value head.  The caches are only read.
  * n_seq * n_draft * n_heads is below 2^31, and 2^30 is above the steps of 32 positions that the longest lengths take: n_seq *
  * n_kv_heads * (ceil(max_len / 32) + ceil(n_draft / 32) + 8) * ceil(n_draft * n_heads / n_kv_heads / 128).
  * ws >= moe_tree_attention_workspace_bytes(cache, n_draft), which is 0 for shapes that are rejected. */

@@ -95,3 +95,18 @@ def test_small_differences_of_large_scores(kind, sign, N, H, G):
     q[..., 0], q[..., 32:] = 2048.0, 1.0
     s.run()
     check(s)
+
+
+@pytest.mark.parametrize("N,H,G", ROWS)
+def test_infinite_drafted_value_of_no_weight(N, H, G):
+    """A drafted value that every token sees is infinite in one element, and cached scores are larger by thousands: that element is an
+    infinity or NaN, the others are what they are without it."""
+    s = Step("bf16", 2, N, H, G, 64, 300, [300, 7], tree=None, seed=9)
+    nq, nk = H * 64, G * 64
+    s.qkv[:, :nq], s.caches[0][:, :, 5] = s.qkv[:, :nq].abs() + 1, 100.0
+    want = s.run().clone().view(2, N, H, 64)
+    s.qkv.view(2, N, -1)[:, 0, nq + nk + 3] = float("inf")
+    s.out.fill_(9.0)
+    got = s.run().view(2, N, H, 64)
+    rest = [i for i in range(64) if i != 3]
+    assert not torch.isfinite(got[..., 3]).any() and torch.equal(got[..., rest], want[..., rest])
