@@ -1,7 +1,7 @@
 // Rotary positions: pairs of a head's dimensions turned by the angle position * frequency.
 //   (x, y) -> amplitude (x cos - y sin, y cos + x sin)
-// Bound by the rows' traffic (each element read and written once): 16384 rows of 40 heads of 128 take 57 us, 5.9 TB/s, where a
-// large copy reaches 5.2.  A work-group takes a few rows of all heads: their angles are the same in every head, so they are worked
+// Bound by the rows' traffic (each element read and written once): 16384 rows of 40 heads of 128 take 57 us, 5.9 TB/s (float: 120,
+// 5.6), where a large copy reaches 5.2.  A work-group takes a few rows of all heads: their angles are the same in every head, so they are worked
 // out once, into LDS.
 #include "moe_internal.h"
 
@@ -115,15 +115,15 @@ int launch_rope(const moe_rope_t* rope, int n_rows, int n_heads, const void* x, 
                 const int32_t* pos, void* out, long long out_stride, hipStream_t s) {
     RopeArgs a{x, out, turns, pos, x_stride, out_stride, n_rows, n_heads, rope->head_dim, rope->rot_dim, 1, rope->amplitude};
     // Rows of few pieces together, as long as there are work-groups enough: 16384 rows of one head of 64 10.4 / 4.1 us, of 4 of 128
-    // 12.2 / 7.8; of 40 heads a row stays alone (61 us, two rows 63, four 67)
-    // A grid has fewer than 2^32 threads, so that 2^24 rows go two by two.
+    // 12.2 / 7.8; of 40 heads a row stays alone (61 us, two rows 63, four 67), except that 2^24 go two by two: a grid has fewer than
+    // 2^32 threads.
     const long long pieces = (long long)n_heads * rope->head_dim / 8;
     const auto more = [&](int rows) { return n_rows / rows >= 1 << 24 || (rows < 16 && rows * pieces < 512 && n_rows / (2 * rows) >= 1024); };
     while (more(a.rows_per_block)) a.rows_per_block *= 2;
     const dim3 grid((unsigned)((n_rows + a.rows_per_block - 1) / a.rows_per_block));
     const size_t lds = (size_t)a.rows_per_block * (rope->rot_dim / 2) * sizeof(float2);
     const bool copy = out != x, half = rope->layout == MOE_ROPE_HALF;
-    // 32 MB of bf16 are all the L2 caches: 4096 rows of 48 heads of 128 18.9 us with ordinary stores / 14.4, 16384 rows 62.0 / 57.6
+    // 32 MB of bf16 are all the L2 caches: 4096 rows of 40 heads of 128 18.9 us with ordinary stores / 14.2, 16384 rows 62.0 / 57.5
     const bool big = (long long)n_rows * n_heads * rope->head_dim >= 1 << 24;
 #define MOE_ROPE_SIZE(T, V, HALF, COPY) \
     do { \

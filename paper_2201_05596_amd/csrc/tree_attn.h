@@ -4,12 +4,13 @@
 // scores K Q^T in tiles of 16 positions x 16 rows, then O^T += V^T P^T, with one pass over the positions and a running maximum
 // and sum per row.  The first product's result is laid out as the second one's operand has to be, so probabilities stay in
 // their lanes; keys go from memory into operand order by the choice of addresses, values by a transposition in registers.
-// Up to about 64 rows per key/value head the reading of the cache bounds it; beyond that the issue of instructions: with 128 rows on
-// 8 bits the matrix unit is busy for 0.36 of the time, the vector unit (softmax, change of order, conversion) for 0.42 and its
-// exponentials on top of that, with two waves per SIMD to overlap them.  us without
-// the merge (5 to 11): 64 sequences of 64 to 2040 positions, 16 heads of 128 in bf16, 8 tokens each: 97 (5.7 TB/s); 128 of 1 to
-// 4095, 8 heads in 8 bits, 4 rows each: 96 (5.8 TB/s); 16 of 2000 to 16001, 8 heads in 8 bits, 128 rows each: 102 (590 TFLOP/s); 8 of
-// 3000 to 8100, 4 heads in bf16, 512 rows each: 62 (600 TFLOP/s); at lengths where the items' ends vanish 6.2 TB/s, 600 to 880 TFLOP/s.
+// Up to 16 rows per key/value head, in bf16 up to 64, the reading of the cache bounds it; beyond that the issue of instructions: with
+// 128 rows on 8 bits the matrix unit is busy for 0.35 of the time, the vector unit (softmax, change of order, conversion) for 0.46
+// and its exponentials on top of that, with two waves per SIMD to overlap them.  us without the merge (5 to 11): 64 sequences of 64
+// to 2040 positions, 16 heads of 128 in bf16, 8 tokens each: 98 (5.7 TB/s); 128 of 1 to 4095, 8 heads in 8 bits, 4 rows each: 96
+// (5.8 TB/s); 64 of 4096, 8 heads in 4 bits, 16 rows each: 59 (4.8 TB/s); 16 of 2000 to 16001, 8 heads in 8 bits, 128 rows each: 104
+// (580 TFLOP/s); 8 of 3000 to 8100, 4 heads in bf16, 512 rows each: 65 (570 TFLOP/s).
+// (The times of the rules below are from before scores were subtracted ahead of the factor c, which takes 1 to 2 % beyond 16 rows.)
 #pragma once
 
 #include "cache_kind.h"
