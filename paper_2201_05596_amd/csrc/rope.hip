@@ -1,8 +1,8 @@
 // Rotary positions: pairs of a head's dimensions turned by the angle position * frequency.
 //   (x, y) -> amplitude (x cos - y sin, y cos + x sin)
 // Bound by the rows' traffic (each element read and written once): 16384 rows of 40 heads of 128 take 57 us, 5.9 TB/s (float: 120,
-// 5.6), where a large copy reaches 5.2.  A work-group takes a few rows of all heads: their angles are the same in every head, so they are worked
-// out once, into LDS.
+// 5.6), where a large copy reaches 5.2.  A work-group takes a few rows of all heads: their angles are the same in every head, so they
+// are worked out once, into LDS.
 #include "moe_internal.h"
 
 namespace moe {

@@ -22,7 +22,7 @@ template <int KIND, int DH> struct Layout {
     }
 };
 
-// Memory from p on, of which `bytes` may be read (the same in every lane): loads behind them give 0
+// Memory from p on, of which `bytes` may be read (the same in every lane): loads behind them give 0, by lane and by scalar offset alike
 typedef __amdgpu_buffer_rsrc_t Window;
 __device__ __forceinline__ Window window(const void* p, int bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, __builtin_amdgcn_readfirstlane(bytes), 0x00027000);
