@@ -67,3 +67,16 @@ def test_tree_longest_distances():
     m.moe_rope(rope, near, turns, rows, near)
     m.moe_rope(rope, q, turns, rows, out)
     assert torch.equal(out, near)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("N,H,G", [(5, 2, 1), (31, 1, 1), (40, 2, 2), (33, 4, 1), (70, 2, 1)])
+def test_tree_all_bits_set(kind, N, H, G):
+    """Every token sees every other, later ones too; bits from the count on are ignored, those behind n_draft in the last word too."""
+    counts = [N, 1, 0, (N + 1) // 2, N - 1]
+    print("case tree all bits", kind, N, H, G, flush=True)
+    s = Step(kind, 5, N, H, G, 64, 50, [50, 0, 20, 33, 0], counts, tree=np.full((5, N, (N + 31) // 32), -1, np.int32), seed=N)
+    for b, n in enumerate(counts):
+        s.qkv.view(5, N, -1)[b, n:] = float("nan")
+    s.run()
+    s.check()
