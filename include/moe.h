@@ -403,6 +403,66 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
                             const int32_t* lens, const int32_t* tree, void* qkv, void* out, void* x1_out, void* moe_in_out,
                             float* logits_out, void* ws, size_t ws_bytes, void* stream);
 
+/* ---- experts in 8-bit integers: weights of half the size, products at twice the rate ----
+ *
+ * A row of activations, or a column of weights, is held as codes and a scale.  With m the largest magnitude of its values,
+ *   M = max(m, 2^-100),  r = 127 / M,  s = M / 127      (r and s rounded to 32 bits)
+ *   code = v r rounded to the nearest whole number, ties to even (the product itself is not rounded);  a value reads as code s.
+ * A row or column that holds an infinity or NaN has codes 0 and scale NaN, so that whatever it takes part in is NaN.
+ * A product of rows and columns is  acc (s_row s_col) + bias,  acc the exact sum of the products of codes (K <= 131072: it
+ * stays below 2^31), the rest in 32 bits.  It does not depend on an order of summation: any split, tile or number of rows gives
+ * the same bits.  (A scale product outside of float's range gives zeros, infinities or NaN.)
+ *
+ * Rows of codes are at distances of a multiple of 16 bytes, at least K rounded up to 64; what is between K and there may be
+ * anything (moe_i8_quantize_rows writes zeros).  K and N are multiples of 8, at most 131072.
+ * Weights are laid out once, in the order of the matrix instructions: moe_i8_weights_bytes(G, K, N) bytes (0 = not covered), from
+ * bf16 weights [G,K,N] by moe_i8_quantize_weights, scale [G,N], or from codes [G,K,N] that a program has by moe_i8_pack_weights.
+ * Outputs may overlap no input. */
+size_t moe_i8_weights_bytes(int32_t G, int32_t K, int32_t N);
+int moe_i8_quantize_weights(int32_t G, int32_t K, int32_t N, const void* W, void* packed, float* scale, void* stream);
+int moe_i8_pack_weights(int32_t G, int32_t K, int32_t N, const int8_t* codes, void* packed, void* stream);
+
+/* moe_i8_quantize_rows -- rows x [n_rows, n_cols] of dtype (moe_dtype_t) at distances of x_stride elements (a multiple of 8, float:
+ * 4; at most 2^24) into codes at distances of codes_stride bytes, and scale [n_rows].  Up to 2^24 rows. */
+int moe_i8_quantize_rows(int32_t dtype, int32_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, int8_t* codes,
+                         int64_t codes_stride, float* scale, void* stream);
+
+/* moe_i8_linear -- out [n_rows, N] = codes W with both scales, + bias [N] (bf16, or NULL), through gelu_tanh if product->gelu;
+ * rounded once to out_dtype, rows at distances of out_stride elements (a multiple of 8, float: 4).  Up to 2^24 rows. */
+typedef struct {
+    int32_t n_rows, K, N;
+    int32_t out_dtype;     /* moe_dtype_t                                        */
+    int32_t gelu;          /* 0 or 1                                             */
+} moe_i8_linear_t;
+int moe_i8_linear(const moe_i8_linear_t* product, const int8_t* codes, int64_t codes_stride, const float* row_scale,
+                  const void* W, const float* col_scale, const void* bias, void* out, int64_t out_stride, void* stream);
+
+/* Weights of 8-bit experts, each as laid out above with its scales: W1 [E,d,f], s1 [E,f], W2 [E,f,d], s2 [E,d] and for the dense
+ * branch Wd1 [d,f], sd1 [f], Wd2 [f,d], sd2 [d] (residual layers, else NULL).  Biases are bf16 and may be NULL. */
+typedef struct {
+    const void* W1; const float* s1; const void* b1;
+    const void* W2; const float* s2; const void* b2;
+    const void* Wd1; const float* sd1; const void* bd1;
+    const void* Wd2; const float* sd2; const void* bd2;
+} moe_i8_weights_t;
+
+/* moe_i8_expert_ffn -- moe_expert_ffn with 8-bit experts: for c < expert_rows[e], with q() for codes and scale of a row,
+ *   h = gelu_tanh(q(xe[e,c,:]) W1[e] + b1[e]) rounded to bf16,   ye[e,c,:] = q(h) W2[e] + b2[e]
+ * Other rows of ye are left untouched.
+ * moe_i8_layer_forward -- moe_layer_forward with 8-bit experts (and dense branch): the gate on x as it is, then the FFNs as
+ * above on q(x), combined in 32 bits; expert results of top-2 and residual layers, and a dense branch's of more than 32 tokens,
+ * are rounded to bf16 before they are added up.
+ * Both: shape.dtype is MOE_BF16, T and E * capacity at most 2^24, shape.flags 0 or MOE_FLAG_PACKED_GATE (layer only has a
+ * gate); the dense branch's members of `weights` are not looked at by moe_i8_expert_ffn.
+ * ws >= moe_i8_workspace_bytes(shape), 0 for shapes that are rejected. */
+size_t moe_i8_workspace_bytes(const moe_shape_t* shape);
+int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights, const void* xe, const int32_t* expert_rows,
+                      void* ye, void* ws, size_t ws_bytes, void* stream);
+int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weights, const void* x, const float* Wg,
+                         const float* bg, void* out, float* logits_out, int32_t* expert_idx_out, int32_t* slot_idx_out,
+                         float* gate_w_out, int32_t* expert_rows_out, int32_t* slot_token_out, void* ws, size_t ws_bytes,
+                         void* stream);
+
 /* Stage timing of moe_layer_forward, for benchmarks (the paper reports the MoE
  * kernels' latency as a whole, Sec. 5.4; this splits it per kernel).
  * moe_profile_enable(n > 0) creates events for the next n calls (the one place

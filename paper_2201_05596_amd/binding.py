@@ -32,7 +32,8 @@ ENTRY_POINTS = ("moe_workspace_bytes", "moe_status_string", "moe_version", "moe_
                 "moe_expert_ffn", "moe_expert_ffn_slice", "moe_expert_ffn_slice_reduce", "moe_combine", "moe_layer_forward", "moe_decode_block_workspace_bytes",
                 "moe_decode_block_forward", "moe_rope_frequencies", "moe_rope", "moe_cache_bytes", "moe_cache_scale_bytes",
                 "moe_cache_write", "moe_cache_read", "moe_tree_attention_workspace_bytes", "moe_tree_attention",
-                "moe_draft_block_workspace_bytes", "moe_draft_block_forward", "moe_profile_enable", "moe_profile_select",
+                "moe_draft_block_workspace_bytes", "moe_draft_block_forward", "moe_i8_weights_bytes", "moe_i8_quantize_weights", "moe_i8_pack_weights",
+                "moe_i8_quantize_rows", "moe_i8_linear", "moe_i8_workspace_bytes", "moe_i8_expert_ffn", "moe_i8_layer_forward", "moe_profile_enable", "moe_profile_select",
                 "moe_profile_stride", "moe_profile_calls",
                 "moe_profile_stage_count", "moe_profile_stage_name", "moe_profile_elapsed")
 
@@ -61,6 +62,17 @@ class MoeRope(ctypes.Structure):
 
 class MoeCacheShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("n_seq", "n_heads", "n_kv_heads", "head_dim", "max_len", "kind")]
+
+
+class MoeI8Linear(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("n_rows", "K", "N", "out_dtype", "gelu")]
+
+
+I8_WEIGHT_FIELDS = ("W1", "s1", "b1", "W2", "s2", "b2", "Wd1", "sd1", "bd1", "Wd2", "sd2", "bd2")
+
+
+class MoeI8Weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in I8_WEIGHT_FIELDS]
 
 
 class MoeError(RuntimeError):
@@ -142,6 +154,23 @@ def load_library() -> ctypes.CDLL:
     lib.moe_draft_block_workspace_bytes.argtypes = [sp, cp, i32]
     lib.moe_draft_block_forward.restype = i32
     lib.moe_draft_block_forward.argtypes = [sp, cp, i32, rp, ctypes.POINTER(MoeBlockWeights)] + [vp] * 14 + [vp, st, vp]
+    lib.moe_i8_weights_bytes.restype = st
+    lib.moe_i8_weights_bytes.argtypes = [i32] * 3
+    lib.moe_i8_quantize_weights.restype = i32
+    lib.moe_i8_quantize_weights.argtypes = [i32] * 3 + [vp] * 4
+    lib.moe_i8_pack_weights.restype = i32
+    lib.moe_i8_pack_weights.argtypes = [i32] * 3 + [vp] * 3
+    lib.moe_i8_quantize_rows.restype = i32
+    lib.moe_i8_quantize_rows.argtypes = [i32] * 3 + [vp, i64, vp, i64, vp, vp]
+    lib.moe_i8_linear.restype = i32
+    lib.moe_i8_linear.argtypes = [ctypes.POINTER(MoeI8Linear), vp, i64] + [vp] * 5 + [i64, vp]
+    lib.moe_i8_workspace_bytes.restype = st
+    lib.moe_i8_workspace_bytes.argtypes = [sp]
+    wp = ctypes.POINTER(MoeI8Weights)
+    lib.moe_i8_expert_ffn.restype = i32
+    lib.moe_i8_expert_ffn.argtypes = [sp, wp] + [vp] * 4 + [st, vp]
+    lib.moe_i8_layer_forward.restype = i32
+    lib.moe_i8_layer_forward.argtypes = [sp, wp] + [vp] * 11 + [st, vp]
     lib.moe_profile_enable.restype = i32
     lib.moe_profile_enable.argtypes = [i32]
     lib.moe_profile_select.restype = i32
@@ -621,6 +650,137 @@ def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, 
         _at(x1_out, dev, el, T * d, "x1_out"), _at(moe_in_out, dev, el, T * d, "moe_in_out"), _at(logits_out, dev, f32, T * E, "logits_out"),
         wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_draft_block_forward", rc)
+
+
+# ---- products in 8-bit integers ----------------------------------------------------------------------------------
+
+def _i8_row_bytes(K: int) -> int:
+    return (K + 63) // 64 * 64
+
+
+def moe_i8_weights_bytes(G: int, K: int, N: int) -> int:
+    return int(load_library().moe_i8_weights_bytes(int(G), int(K), int(N)))
+
+
+def _i8_matrix(t: torch.Tensor, name: str):
+    """(groups, K, N, empty buffer) for weights [G,K,N] or [K,N]."""
+    if t.dim() not in (2, 3):
+        raise ValueError(f"{name}: expected [K, N] or [G, K, N], got {tuple(t.shape)}")
+    G, K, N = (1, *t.shape) if t.dim() == 2 else t.shape
+    nbytes = moe_i8_weights_bytes(G, K, N)
+    if nbytes == 0:
+        raise MoeError("moe_i8_weights_bytes", -2, "unsupported size")
+    return G, K, N, torch.empty(nbytes, dtype=torch.int8, device=t.device)
+
+
+def moe_i8_quantize_weights(W: torch.Tensor):
+    """(packed codes, scale [G,N] or [N]) of bf16 weights [G,K,N] or [K,N]; torch owns the new buffers."""
+    G, K, N, packed = _i8_matrix(W, "W")
+    scale = torch.empty(W.shape[:-2] + (N,), dtype=torch.float32, device=W.device)
+    dev = torch._C._cuda_getDevice()
+    _check("moe_i8_quantize_weights", load_library().moe_i8_quantize_weights(
+        G, K, N, _at(W, dev, torch.bfloat16, G * K * N, "W"), packed.data_ptr(), scale.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
+    return packed, scale
+
+
+def moe_i8_pack_weights(codes: torch.Tensor) -> torch.Tensor:
+    """Packed copy of int8 codes [G,K,N] or [K,N]; torch owns the new buffer."""
+    G, K, N, packed = _i8_matrix(codes, "codes")
+    dev = torch._C._cuda_getDevice()
+    _check("moe_i8_pack_weights", load_library().moe_i8_pack_weights(
+        G, K, N, _at(codes, dev, torch.int8, G * K * N, "codes"), packed.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
+    return packed
+
+
+def moe_i8_quantize_rows(x, codes, scale) -> None:
+    """x: [rows, cols] bf16 or float32, columns of wider rows if need be; codes: int8 [rows, at least cols rounded up to 64]."""
+    rows, cols = x.shape
+    if rows == 0:
+        return
+    if x.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError(f"x: expected float32 or bfloat16, got {x.dtype}")
+    if codes.dim() != 2 or codes.shape[1] < _i8_row_bytes(cols):
+        raise ValueError(f"codes: expected {rows} rows of at least {_i8_row_bytes(cols)}, got {tuple(codes.shape)}")
+    dev = torch._C._cuda_getDevice()
+    xp, xs = _rows(x, dev, x.dtype, rows, cols, "x")
+    rc = load_library().moe_i8_quantize_rows(
+        MOE_F32 if x.dtype == torch.float32 else MOE_BF16, rows, cols, xp, xs, *_rows(codes, dev, torch.int8, rows, codes.shape[1], "codes"),
+        _at(scale, dev, torch.float32, rows, "scale"), torch._C._cuda_getCurrentRawStream(dev))
+    _check("moe_i8_quantize_rows", rc)
+
+
+def make_i8_linear(n_rows: int, K: int, N: int, out_dtype, gelu: bool = False) -> MoeI8Linear:
+    if isinstance(out_dtype, torch.dtype):
+        out_dtype = {torch.float32: MOE_F32, torch.bfloat16: MOE_BF16}[out_dtype]
+    elif isinstance(out_dtype, str):
+        out_dtype = {"f32": MOE_F32, "bf16": MOE_BF16}[out_dtype]
+    return MoeI8Linear(n_rows, K, N, int(out_dtype), int(bool(gelu)))
+
+
+def moe_i8_linear(product: MoeI8Linear, codes, row_scale, W, col_scale, bias, out) -> None:
+    """codes: int8 [n_rows, at least K rounded up to 64]; W, col_scale: as moe_i8_quantize_weights gave them; bias: bf16 or None."""
+    rows, K, N = product.n_rows, product.K, product.N
+    if rows == 0:
+        return
+    if codes.dim() != 2 or codes.shape[1] < _i8_row_bytes(K):
+        raise ValueError(f"codes: expected {rows} rows of at least {_i8_row_bytes(K)}, got {tuple(codes.shape)}")
+    f32, dev = torch.float32, torch._C._cuda_getDevice()
+    rc = load_library().moe_i8_linear(
+        ctypes.byref(product), *_rows(codes, dev, torch.int8, rows, codes.shape[1], "codes"), _at(row_scale, dev, f32, rows, "row_scale"),
+        _at(W, dev, torch.int8, _i8_weights_need(1, K, N), "W"), _at(col_scale, dev, f32, N, "col_scale"), _at(bias, dev, torch.bfloat16, N, "bias"),
+        *_rows(out, dev, f32 if product.out_dtype == MOE_F32 else torch.bfloat16, rows, N, "out"), torch._C._cuda_getCurrentRawStream(dev))
+    _check("moe_i8_linear", rc)
+
+
+def moe_i8_workspace_bytes(shape: MoeShape) -> int:
+    return int(load_library().moe_i8_workspace_bytes(ctypes.byref(shape)))
+
+
+@functools.lru_cache(maxsize=256)
+def _i8_weights_need(G: int, K: int, N: int) -> int:
+    return moe_i8_weights_bytes(G, K, N)
+
+
+@functools.lru_cache(maxsize=256)
+def _i8_workspace_need(shape: bytes) -> int:
+    return moe_i8_workspace_bytes(MoeShape.from_buffer_copy(shape))
+
+
+def _i8_weights(shape, weights: dict, device: int, dense: bool) -> MoeI8Weights:
+    d, f, E = shape.d_model, shape.d_ffn, shape.E
+    up, down, f32, i8, bf = _i8_weights_need, (f, d), torch.float32, torch.int8, torch.bfloat16
+    sizes = {"W1": (i8, up(E, d, f)), "s1": (f32, E * f), "b1": (bf, E * f), "W2": (i8, up(E, *down)), "s2": (f32, E * d), "b2": (bf, E * d)}
+    if dense:
+        sizes |= {"Wd1": (i8, up(1, d, f)), "sd1": (f32, f), "bd1": (bf, f), "Wd2": (i8, up(1, *down)), "sd2": (f32, d), "bd2": (bf, d)}
+    return MoeI8Weights(**{n: _at(weights.get(n), device, *sizes[n], n) for n in sizes})
+
+
+def moe_i8_expert_ffn(shape, weights: dict, xe, expert_rows, ye, ws) -> None:
+    """`weights`: name -> tensor (or None) for the fields of moe_i8_weights_t."""
+    bf, dev = torch.bfloat16, torch._C._cuda_getDevice()
+    n = shape.E * shape.capacity
+    w = _i8_weights(shape, weights, dev, False)
+    wp, nbytes = _workspace(ws, dev, _i8_workspace_need(bytes(shape)))
+    rc = load_library().moe_i8_expert_ffn(
+        ctypes.byref(shape), ctypes.byref(w), _at(xe, dev, bf, n * shape.d_model, "xe"), _at(expert_rows, dev, torch.int32, shape.E, "expert_rows"),
+        _at(ye, dev, bf, n * shape.d_model, "ye"), wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
+    _check("moe_i8_expert_ffn", rc)
+
+
+def moe_i8_layer_forward(shape, weights: dict, x, Wg, bg, out, logits_out, expert_idx_out, slot_idx_out, gate_w_out, expert_rows_out,
+                         slot_token_out, ws) -> None:
+    """`weights` as in moe_i8_expert_ffn, with the dense branch's for residual layers."""
+    bf, i32, f32, dev = torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getDevice()
+    T, d, E, k, C = shape.T, shape.d_model, shape.E, shape.top_k, shape.capacity
+    w = _i8_weights(shape, weights, dev, True)
+    wp, nbytes = _workspace(ws, dev, _i8_workspace_need(bytes(shape)))
+    rc = load_library().moe_i8_layer_forward(
+        ctypes.byref(shape), ctypes.byref(w), _at(x, dev, bf, T * d, "x"), _at(Wg, dev, f32, _wg(shape), "Wg"), _at(bg, dev, f32, E, "bg"),
+        _at(out, dev, bf, T * d, "out"), _at(logits_out, dev, f32, T * E, "logits_out"), _at(expert_idx_out, dev, i32, T * k, "expert_idx_out"),
+        _at(slot_idx_out, dev, i32, T * k, "slot_idx_out"), _at(gate_w_out, dev, f32, T * k, "gate_w_out"),
+        _at(expert_rows_out, dev, i32, E, "expert_rows_out"), _at(slot_token_out, dev, i32, E * C, "slot_token_out"), wp, nbytes,
+        torch._C._cuda_getCurrentRawStream(dev))
+    _check("moe_i8_layer_forward", rc)
 
 
 def moe_profile_enable(max_calls: int) -> None:

@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "call_tag.h"
+#include "i8.h"
 #include "moe_internal.h"
 
 using namespace moe;
@@ -244,13 +245,9 @@ struct WsLayout {
     size_t logits, wg_frags, hist, flags, expert_idx, slot_idx, gate_w, rows, order, slot_token, h, ye, hd, dense, partial, total;
 };
 
-WsLayout ws_layout(const moe_shape_t* s) {
-    WsLayout L{};
-    const size_t T = s->T, d = s->d_model, f = s->d_ffn, E = s->E, k = s->top_k, C = s->capacity;
-    const size_t es = esize(s->dtype);
-    const FfnPlan plan = plan_ffn(s);
-    size_t off = 0;
-    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+// the gate's regions and tables, from `off` on
+template <typename Take> void gate_layout(const moe_shape_t* s, WsLayout& L, const size_t& off, Take take) {
+    const size_t T = s->T, E = s->E, k = s->top_k, C = s->capacity;
     L.logits = take(T * E * 4);
     L.wg_frags = take(s->dtype == MOE_BF16 ? gate_bf16_ws_bytes(s->d_model, s->E) : 0);
     L.hist = take(route_scratch_ints(s->T, s->E, s->top_k, !gate_on_bf16(s)) * 4);
@@ -264,6 +261,16 @@ WsLayout ws_layout(const moe_shape_t* s) {
     L.rows = take(E * 4);
     L.order = take(2 * (E + 1) * 4);  // two launch orders of the experts, each followed by the tile-dealing flag
     L.slot_token = take(E * C * 4);
+}
+
+WsLayout ws_layout(const moe_shape_t* s) {
+    WsLayout L{};
+    const size_t T = s->T, d = s->d_model, f = s->d_ffn, E = s->E, C = s->capacity;
+    const size_t es = esize(s->dtype);
+    const FfnPlan plan = plan_ffn(s);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+    gate_layout(s, L, off, take);
     L.h = take(E * C * f * es);
     L.ye = take(E * C * d * es);
     L.hd = take(s->residual ? T * f * es : 0);
@@ -1409,6 +1416,271 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
     if (rc != MOE_OK) return rc;
     return block_tail(shape, w, x, attn, at<uint16_t>(ws, L.proj), x1_out ? u16(x1_out) : at<uint16_t>(ws, L.x1),
                       moe_in_out ? u16(moe_in_out) : xn, at<uint16_t>(ws, L.moe_out), lin_partial, at<void>(ws, L.moe_ws), out, logits_out, stream);
+}
+
+}  // extern "C"
+
+// ---- products in 8-bit integers -----------------------------------------------------------------------------------
+namespace {
+
+constexpr long long kI8MaxBlocks = (1 << 23) - 1;    // work-groups of a launch: their threads are counted in 32 bits
+
+int check_i8_shape(const moe_shape_t* s) {
+    const int rc = check_shape(s);
+    if (rc != MOE_OK) return rc;
+    if (s->flags & MOE_FLAG_PACKED_WEIGHTS) return MOE_ERR_INVALID_ARG;      // of bf16 weights
+    if (s->dtype != MOE_BF16 || s->d_model > kI8MaxK || s->d_ffn > kI8MaxK) return MOE_ERR_UNSUPPORTED;
+    const long long rows = std::max<long long>(s->T, (long long)s->E * s->capacity);
+    if (rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    // the most work-groups that a product can have: tiles of 128 rows by 256 columns, or of 16 columns where rows are few
+    const long long n = std::max(s->d_model, s->d_ffn), tiles = (rows + 127) / 128 + s->E + 8;
+    return tiles * ((n + 15) / 16) > kI8MaxBlocks ? MOE_ERR_UNSUPPORTED : MOE_OK;
+}
+
+int check_i8_weights(const moe_shape_t* s, const moe_i8_weights_t* w, bool dense) {
+    if (!w || !w->W1 || !w->s1 || !w->W2 || !w->s2) return MOE_ERR_INVALID_ARG;
+    const bool all = w->Wd1 && w->sd1 && w->Wd2 && w->sd2, any = w->Wd1 || w->sd1 || w->bd1 || w->Wd2 || w->sd2 || w->bd2;
+    if (dense && (s->residual ? !all : any)) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {w->W1, (const void*)w->s1, w->b1, w->W2, (const void*)w->s2, w->b2, w->Wd1, (const void*)w->sd1, w->bd1, w->Wd2,
+                          (const void*)w->sd2, w->bd2})
+        if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    return MOE_OK;
+}
+
+// Rows of a group that the kernel of few rows takes, making the second product's codes from bf16
+constexpr int kI8FewRows = 32;
+
+struct I8Layout {
+    WsLayout gate;
+    size_t x, x_scale, h, h_max, hq, h_scale, ye, hd, hd_max, hdq, hd_scale, dense, total;
+};
+I8Layout i8_layout(const moe_shape_t* s) {
+    I8Layout L{};
+    const size_t T = s->T, d = s->d_model, E = s->E, C = s->capacity, rows = std::max(T, E * C);
+    const size_t dq = i8_row_bytes(s->d_model), fq = i8_row_bytes(s->d_ffn);
+    size_t off = 0;
+    auto take = [&](size_t bytes) { const size_t o = off; off += align_up(bytes); return o; };
+    gate_layout(s, L.gate, off, take);
+    L.x = take(rows * dq);                    // of the tokens, or of dispatched rows
+    L.x_scale = take(rows * 4);
+    L.h = take(E * C * fq * 2);
+    L.hq = take(E * C * fq);
+    L.h_scale = take(E * C * 4);
+    L.ye = take(E * C * d * 2);
+    const size_t t = s->residual ? T : 0;
+    L.hd = take(t * fq * 2);
+    L.hdq = take(t * fq);
+    L.hd_scale = take(t * 4);
+    L.dense = take(t * d * 4);                // in 32 bits where tokens are few
+    L.h_max = off;                            // next to each other: cleared together
+    off += E * C * 4;
+    L.hd_max = off;
+    off = align_up(off + t * 4);
+    L.total = off;
+    return L;
+}
+int check_i8_ws(const moe_shape_t* s, const void* ws, size_t ws_bytes) {
+    return !ws || !aligned16(ws) || ws_bytes < i8_layout(s).total ? MOE_ERR_WORKSPACE : MOE_OK;
+}
+
+// One group's (or all experts') two products and what is between them
+struct I8Ffn {
+    I8GemmArgs first, second;
+    bool few;
+    uint16_t* h;
+    int8_t* hq;
+    float* h_scale;
+    int n_rows;                               // rows of h, used or not
+};
+I8Ffn i8_ffn(const moe_shape_t* s, int G, int max_rows, int group_rows, const int32_t* rows, const int8_t* x, const float* x_scale, const void* W1,
+             const float* s1, const void* b1, const void* W2, const float* s2, const void* b2, uint16_t* h, uint32_t* h_max, int8_t* hq, float* h_scale) {
+    const int dq = i8_row_bytes(s->d_model), fq = i8_row_bytes(s->d_ffn);
+    I8Ffn p{};
+    I8GemmArgs& a = p.first;
+    a.A = reinterpret_cast<const uint16_t*>(x); a.a_scale = x_scale; a.B = u16(W1); a.b_scale = s1; a.bias = u16(b1); a.packed = 1;
+    a.rows = rows; a.fixed_rows = rows ? 0 : group_rows; a.max_rows = max_rows; a.G = G; a.K = dq / 2; a.lda = dq / 2; a.N = s->d_ffn;
+    a.a_group_stride = a.o_group_stride = group_rows; a.out = h; a.ldo = fq; a.ksplit = 1;
+    p.few = max_rows <= kI8FewRows;
+    I8GemmArgs& b = p.second;
+    b = a;
+    b.B = u16(W2); b.b_scale = s2; b.bias = u16(b2); b.K = fq / 2; b.N = s->d_model; b.ldo = s->d_model;
+    if (p.few) {
+        a.out_max = h_max;
+        b.A = h; b.lda = fq; b.a_max = h_max; b.a_scale = nullptr;
+    } else {
+        b.A = reinterpret_cast<const uint16_t*>(hq); b.lda = fq / 2; b.a_scale = h_scale;
+    }
+    p.h = h; p.hq = hq; p.h_scale = h_scale; p.n_rows = G * group_rows;
+    return p;
+}
+
+int i8_product(const I8GemmArgs& a, const I8GemmArgs* b, bool few, int epi, hipStream_t st) {
+    if (few) {
+        const int most = b ? std::max(a.max_rows, b->max_rows) : a.max_rows;
+        return launch_i8_few(a, b, epi, i8_few_columns(few_groups(a) + (b ? few_groups(*b) : 0), most, a.N), st);
+    }
+    const bool large = a.max_rows > 128 || (b && b->max_rows > 128);
+    return launch_i8_wide(a, b, large ? 256 : 128, epi, st);
+}
+
+// h into codes, unless the second product makes them itself
+int i8_between(const moe_shape_t* s, const I8Ffn& p, const int32_t* rows, hipStream_t st) {
+    if (p.few) return MOE_OK;
+    const long long fq = i8_row_bytes(s->d_ffn);
+    return launch_i8_rows(I8RowsArgs{p.h, fq, fq, p.hq, p.h_scale, rows, rows ? p.n_rows / p.first.G : 0, p.n_rows, s->d_ffn, nullptr, 0}, MOE_BF16, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t moe_i8_weights_bytes(int32_t G, int32_t K, int32_t N) {
+    if (G < 1 || K < 8 || N < 8 || K % 8 || N % 8 || K > kI8MaxK || N > kI8MaxK) return 0;
+    return (long long)G * ((N + 127) / 128) * 2 >= 1ll << 22 ? 0 : i8_weight_bytes(G, K, N);
+}
+
+static int check_i8_matrix(int32_t G, int32_t K, int32_t N, std::initializer_list<const void*> ptrs) {
+    if (G < 1 || K < 8 || N < 8) return MOE_ERR_INVALID_ARG;
+    for (const void* p : ptrs)
+        if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    return moe_i8_weights_bytes(G, K, N) ? MOE_OK : MOE_ERR_UNSUPPORTED;
+}
+
+int moe_i8_pack_weights(int32_t G, int32_t K, int32_t N, const int8_t* codes, void* packed, void* stream) {
+    const int rc = check_i8_matrix(G, K, N, {codes, packed});
+    return rc != MOE_OK ? rc : launch_i8_pack(codes, packed, G, K, N, static_cast<hipStream_t>(stream));
+}
+
+int moe_i8_quantize_weights(int32_t G, int32_t K, int32_t N, const void* W, void* packed, float* scale, void* stream) {
+    const int rc = check_i8_matrix(G, K, N, {W, packed, scale});
+    return rc != MOE_OK ? rc : launch_i8_weights(u16(W), packed, scale, G, K, N, static_cast<hipStream_t>(stream));
+}
+
+int moe_i8_quantize_rows(int32_t dtype, int32_t n_rows, int32_t n_cols, const void* x, int64_t x_stride, int8_t* codes, int64_t codes_stride,
+                         float* scale, void* stream) {
+    if ((dtype != MOE_F32 && dtype != MOE_BF16) || n_rows < 1 || n_cols < 1) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, (const void*)codes, (const void*)scale})
+        if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    if (n_cols % 8 || n_cols > kI8MaxK || n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    if (!row_stride_ok(x_stride, n_cols, dtype == MOE_F32 ? 4 : 8) || !row_stride_ok(codes_stride, i8_row_bytes(n_cols), 16)) return MOE_ERR_INVALID_ARG;
+    return launch_i8_rows(I8RowsArgs{x, x_stride, codes_stride, codes, scale, nullptr, 0, n_rows, n_cols, nullptr, 0}, dtype,
+                          static_cast<hipStream_t>(stream));
+}
+
+int moe_i8_linear(const moe_i8_linear_t* product, const int8_t* codes, int64_t codes_stride, const float* row_scale, const void* W,
+                  const float* col_scale, const void* bias, void* out, int64_t out_stride, void* stream) {
+    const moe_i8_linear_t* p = product;
+    if (!p || p->n_rows < 1 || p->K < 1 || p->N < 1 || (p->out_dtype != MOE_F32 && p->out_dtype != MOE_BF16) || (p->gelu != 0 && p->gelu != 1))
+        return MOE_ERR_INVALID_ARG;
+    for (const void* q : {(const void*)codes, (const void*)row_scale, W, (const void*)col_scale, (const void*)out})
+        if (!q || !aligned16(q)) return MOE_ERR_INVALID_ARG;
+    if (bias && !aligned16(bias)) return MOE_ERR_INVALID_ARG;
+    if (p->K % 8 || p->N % 8 || p->K > kI8MaxK || p->N > kI8MaxK || p->n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
+    if (((p->n_rows + 127ll) / 128 + 9) * ((p->N + 15) / 16) > kI8MaxBlocks) return MOE_ERR_UNSUPPORTED;
+    if (!row_stride_ok(codes_stride, i8_row_bytes(p->K), 16) || !row_stride_ok(out_stride, p->N, p->out_dtype == MOE_F32 ? 4 : 8)) return MOE_ERR_INVALID_ARG;
+    I8GemmArgs a{};
+    a.A = reinterpret_cast<const uint16_t*>(codes); a.lda = codes_stride / 2; a.a_scale = row_scale; a.B = u16(W); a.b_scale = col_scale;
+    a.bias = u16(bias); a.packed = 1; a.fixed_rows = a.max_rows = p->n_rows; a.G = 1; a.K = i8_row_bytes(p->K) / 2; a.N = p->N;
+    a.out = u16(out); a.ldo = out_stride; a.out32 = p->out_dtype == MOE_F32; a.ksplit = 1;
+    return i8_product(a, nullptr, p->n_rows <= kI8FewRows, p->gelu ? EPI_GELU : EPI_STORE, static_cast<hipStream_t>(stream));
+}
+
+size_t moe_i8_workspace_bytes(const moe_shape_t* shape) { return check_i8_shape(shape) == MOE_OK ? i8_layout(shape).total : 0; }
+
+int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights, const void* xe, const int32_t* expert_rows, void* ye, void* ws,
+                      size_t ws_bytes, void* stream) {
+    int rc = check_i8_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if ((rc = check_i8_weights(shape, weights, false)) != MOE_OK) return rc;
+    for (const void* p : {xe, (const void*)expert_rows, (const void*)ye})
+        if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_i8_ws(shape, ws, ws_bytes)) != MOE_OK) return rc;
+    const I8Layout L = i8_layout(shape);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int E = shape->E, C = shape->capacity, d = shape->d_model;
+    int8_t* x = at<int8_t>(ws, L.x);
+    float* x_scale = at<float>(ws, L.x_scale);
+    I8Ffn p = i8_ffn(shape, E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
+                     at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
+    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, d, p.few ? at<uint32_t>(ws, L.h_max) : nullptr, (long long)E * C},
+                        MOE_BF16, st);
+    if (rc != MOE_OK) return rc;
+    if ((rc = i8_product(p.first, nullptr, p.few, EPI_GELU, st)) != MOE_OK) return rc;
+    if ((rc = i8_between(shape, p, expert_rows, st)) != MOE_OK) return rc;
+    p.second.out = u16(ye);
+    return i8_product(p.second, nullptr, p.few, EPI_STORE, st);
+}
+
+int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weights, const void* x, const float* Wg, const float* bg, void* out,
+                         float* logits_out, int32_t* expert_idx_out, int32_t* slot_idx_out, float* gate_w_out, int32_t* expert_rows_out,
+                         int32_t* slot_token_out, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_i8_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if ((rc = check_i8_weights(shape, weights, true)) != MOE_OK) return rc;
+    if (!x || !Wg || !out) return MOE_ERR_INVALID_ARG;
+    for (const void* p : {x, (const void*)Wg, (const void*)bg, (const void*)out, (const void*)logits_out, (const void*)expert_idx_out,
+                          (const void*)slot_idx_out, (const void*)gate_w_out, (const void*)expert_rows_out, (const void*)slot_token_out})
+        if (p && !aligned16(p)) return MOE_ERR_INVALID_ARG;
+    if ((rc = check_i8_ws(shape, ws, ws_bytes)) != MOE_OK) return rc;
+    const I8Layout L = i8_layout(shape);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int T = shape->T, E = shape->E, C = shape->capacity, d = shape->d_model, k = shape->top_k;
+    float* logits = logits_out ? logits_out : at<float>(ws, L.gate.logits);
+    int32_t* expert_idx = expert_idx_out ? expert_idx_out : at<int32_t>(ws, L.gate.expert_idx);
+    int32_t* slot_idx = slot_idx_out ? slot_idx_out : at<int32_t>(ws, L.gate.slot_idx);
+    float* gate_w = gate_w_out ? gate_w_out : at<float>(ws, L.gate.gate_w);
+    int32_t* rows = expert_rows_out ? expert_rows_out : at<int32_t>(ws, L.gate.rows);
+    int32_t* slot_token = slot_token_out ? slot_token_out : at<int32_t>(ws, L.gate.slot_token);
+    int32_t* order = at<int32_t>(ws, L.gate.order);
+    int8_t* xq = at<int8_t>(ws, L.x);
+    float* x_scale = at<float>(ws, L.x_scale);
+
+    rc = run_gate(shape, x, Wg, bg, logits, expert_idx, slot_idx, gate_w, rows, slot_token, order, ws, L.gate, false, st);
+    if (rc != MOE_OK) return rc;
+    // an expert has at most one row of a token
+    I8Ffn e = i8_ffn(shape, E, std::min(C, T), C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
+                     at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
+    e.first.row_map = slot_token; e.first.map_stride = C;
+    e.first.order = e.second.order = order;
+    e.first.slots = e.second.slots = (int)std::min<long long>((long long)T * k, E);
+    e.first.expect_rows = e.second.expect_rows = (int)(((long long)T * k + E - 1) / E);
+    I8Ffn n{};
+    if (shape->residual)
+        n = i8_ffn(shape, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
+                   at<uint16_t>(ws, L.hd), at<uint32_t>(ws, L.hd_max), at<int8_t>(ws, L.hdq), at<float>(ws, L.hd_scale));
+    const long long most = e.few || n.few ? (long long)E * C + (shape->residual ? T : 0) : 0;
+    rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, T, d, most ? at<uint32_t>(ws, L.h_max) : nullptr, most}, MOE_BF16, st);
+    if (rc != MOE_OK) return rc;
+
+    if (k == 1 && !shape->residual) {         // the combine is in the second product
+        if ((rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
+        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+        I8GemmArgs& a = e.second;
+        a.out = u16(out); a.scatter_map = slot_token; a.scatter_stride = C; a.gate_w = gate_w; a.top_k = 1; a.zero_slot_idx = slot_idx; a.T = T;
+        return i8_product(a, nullptr, e.few, EPI_SCATTER, st);
+    }
+    e.second.out = at<uint16_t>(ws, L.ye);
+    const void* addend = nullptr;
+    PartSums dense{};
+    if (shape->residual) {
+        n.second.out = at<uint16_t>(ws, L.dense);
+        n.second.out32 = n.few;               // few tokens: rounded once, with the experts' results added
+        if (n.few) dense = PartSums{at<float>(ws, L.dense), 1, nullptr};
+        else addend = at<void>(ws, L.dense);
+        const bool together = e.few == n.few;
+        // the dense branch's tiles, which are full, first
+        if ((rc = i8_product(n.first, together ? &e.first : nullptr, n.few, EPI_GELU, st)) != MOE_OK) return rc;
+        if (!together && (rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
+        if ((rc = i8_between(shape, n, nullptr, st)) != MOE_OK) return rc;
+        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+        if ((rc = i8_product(n.second, together ? &e.second : nullptr, n.few, EPI_STORE, st)) != MOE_OK) return rc;
+        if (!together && (rc = i8_product(e.second, nullptr, e.few, EPI_STORE, st)) != MOE_OK) return rc;
+    } else {
+        if ((rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
+        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+        if ((rc = i8_product(e.second, nullptr, e.few, EPI_STORE, st)) != MOE_OK) return rc;
+    }
+    return launch_combine(at<void>(ws, L.ye), MOE_BF16, expert_idx, slot_idx, gate_w, addend, out, T, k, C, d, st, dense);
 }
 
 int moe_profile_enable(int max_calls) {

@@ -19,7 +19,7 @@
 // matrix instructions, and the epilogue's exp and rcp are taken eight at a time.
 #pragma once
 
-#include "ffn_common.h"
+#include "i8.h"
 #include <type_traits>
 
 namespace moe {
@@ -63,6 +63,10 @@ template <int OFF, bool NT> __device__ __forceinline__ void dma16_at(const uint1
 __device__ __forceinline__ void mfma(f32x4_t& d, const bf16x8_t& a, const bf16x8_t& b) {
     asm volatile("v_mfma_f32_16x16x32_bf16 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
 }
+// the same on 8-bit integers: 16 bytes of an operand are 16 codes, the accumulator's bits are integers
+__device__ __forceinline__ void mfma_i8(f32x4_t& d, const bf16x8_t& a, const bf16x8_t& b) {
+    asm volatile("v_mfma_i32_16x16x64_i8 %0, %1, %2, %0" : "+a"(d) : "v"(a), "v"(b));
+}
 __device__ __forceinline__ void set_acc(f32x4_t& d, float v) {
     float x[4];
 #pragma unroll
@@ -96,10 +100,12 @@ __device__ __forceinline__ void gelu_tanh8(float (&v)[8]) {
 enum WidePolicy { WIDE_CACHED, WIDE_STREAMED, WIDE_BY_GROUP };
 constexpr bool wide_hints(int epi) { return epi == EPI_STORE || epi == EPI_GELU || epi == EPI_SCATTER; }   // the epilogues that have the hint
 
-template <int BM, int EPI, bool RAGGED, int POLICY>
-__global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs a0, const WsGemmArgs a1, const int split) {
+// Args: WsGemmArgs for bf16, I8GemmArgs for codes, whose bytes are the same and whose K counts pairs of codes
+template <int BM, int EPI, bool RAGGED, int POLICY, class Args>
+__global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const Args a0, const Args a1, const int split) {
+    constexpr bool I8 = std::is_same<Args, I8GemmArgs>::value;
     const bool second = (int)blockIdx.x >= split;                // uniform over the work-group
-    const WsGemmArgs& a = second ? a1 : a0;
+    const Args& a = second ? a1 : a0;
     const int block = second ? (int)blockIdx.x - split : (int)blockIdx.x;
 
     extern __shared__ __attribute__((aligned(16))) char lds[];   // activation ring, then weight ring
@@ -138,8 +144,16 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
         // All of a tile's table look-ups and its bias are asked for before the first is waited for: with the choice between
         // table and group inside the loop the compiler made each row's look-up a memory round trip of its own.
         const int n_lane = n0 + wn * 128 + c * 8;                // this lane's eight columns
-        const bool has_bias = EPI != EPI_PARTIAL && a.bias != nullptr;
+        const bool has_bias = !I8 && EPI != EPI_PARTIAL && a.bias != nullptr;
         const uint4 bias_raw = has_bias ? *reinterpret_cast<const uint4*>(a.bias + (size_t)g * a.N + min(n_lane, a.N - 8)) : make_uint4(0, 0, 0, 0);
+        // codes: one row's scale, one column's scale and bias for each thread, shared through LDS behind the main loop
+        float i8_row = 0.f, i8_col = 0.f, i8_bias = 0.f;
+        if constexpr (I8) {
+            const int row = m0 + min(tid, nrows - 1), col = min(n0 + tid, a.N - 1);
+            i8_col = a.b_scale[(size_t)g * a.N + col];
+            if (a.bias) i8_bias = bf16_to_f32(a.bias[(size_t)g * a.N + col]);
+            i8_row = a.a_scale[a.row_map ? (size_t)a.row_map[(size_t)g * a.map_stride + row] : (size_t)g * a.a_group_stride + row];
+        }
         const uint16_t* a_src[ACT];
         const int a_piece = (lane & 7);
         int a_row[ACT];
@@ -150,11 +164,13 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
 #pragma unroll
             for (int i = 0; i < ACT; ++i) a_row[i] = map[a_row[i]];
         }
-        const uint16_t* a_group = a.A + (a.row_map ? (size_t)0 : (size_t)g * a.a_group_stride * a.K);
+        size_t lda = a.K;
+        if constexpr (I8) lda = a.lda;
+        const uint16_t* a_group = a.A + (a.row_map ? (size_t)0 : (size_t)g * a.a_group_stride * lda);
 #pragma unroll
         for (int i = 0; i < ACT; ++i) {
             const int rt = (w * ACT + i) * 8 + (lane >> 3);
-            a_src[i] = a_group + (size_t)a_row[i] * a.K + (a_piece ^ ((rt >> 1) & 7)) * 8 - (i & 3) * 512;
+            a_src[i] = a_group + (size_t)a_row[i] * lda + (a_piece ^ ((rt >> 1) & 7)) * 8 - (i & 3) * 512;
         }
         // weights: wave w copies fragments 4w..4w+3 of the tile's sixteen in each of a chunk's two 32-deep steps
         const int p_ng = (a.N + 127) / 128, kb_n = (a.K + 31) / 32;
@@ -202,6 +218,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
         unpack_bias8(bias_raw, bias);
 #pragma unroll
         for (int j = 0; j < 8; ++j) asm volatile("" : "+v"(bias[j]));   // waited for here, not behind the direct loads
+        if constexpr (I8) asm volatile("" : "+v"(i8_row), "+v"(i8_col), "+v"(i8_bias));
         f32x4_t acc[ACT][8];
 
         // fragments of one 32-deep step: activations of sub-tiles 2i + wm, weights of this wave's 128 columns
@@ -226,7 +243,8 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
                 for (int q = 0; q < ACT; ++q) {
                     const int i = j % 2 ? ACT - 1 - q : q;
                     if (q == ACT / 2) dma(jc);
-                    mfma(acc[i][j], cur.a[i], cur.b[j]);
+                    if constexpr (I8) mfma_i8(acc[i][j], cur.a[i], cur.b[j]);
+                    else mfma(acc[i][j], cur.a[i], cur.b[j]);
                 }
             };
             MOE_EACH8(column);
@@ -274,6 +292,20 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
         for (; ch < chunks; ++ch) chunk_steps(ch, std::false_type());   // everything is on its way
 
         // ---- epilogue ----------------------------------------------------------------------------------------
+        float col_scale[8];
+        if constexpr (I8) {
+            float* share = reinterpret_cast<float*>(lds);        // rows' scales, columns' scales, columns' biases
+            wait_vmcnt_barrier<0>();                             // the ring has been read
+            share[tid] = i8_row;
+            share[256 + tid] = i8_col;
+            share[512 + tid] = i8_bias;
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                col_scale[j] = share[256 + wn * 128 + c * 8 + j];
+                bias[j] = share[512 + wn * 128 + c * 8 + j];
+            }
+        }
         if (n_lane >= a.N) return;
         int kg_e = kg;
         asm volatile("" : "+v"(kg_e));                           // the address is formed here, not kept through the main loop
@@ -287,7 +319,9 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
 #pragma unroll
             for (int q = 0; q < ACT * 4; ++q) gate[q] = a.gate_w[(size_t)tok[q] * a.top_k];
         }
-        uint16_t* dst = a.out + ((size_t)g * a.o_group_stride + m0 + wm * 16 + kg_e * 4) * a.N + n_lane;
+        size_t ldo = a.N;
+        if constexpr (I8) ldo = a.ldo;
+        uint16_t* dst = a.out + ((size_t)g * a.o_group_stride + m0 + wm * 16 + kg_e * 4) * ldo + n_lane;
 #pragma unroll
         for (int i = 0; i < ACT; ++i) {
 #pragma unroll
@@ -296,15 +330,31 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
                 float v[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] = acc[i][j][r];
+                if constexpr (I8) {
+                    const float rs = reinterpret_cast<const float*>(lds)[rl];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = i8_value(__float_as_int(v[j]), rs * col_scale[j], bias[j]);
+                }
                 if constexpr (EPI == EPI_STORE || EPI == EPI_GELU) {
                     if (EPI == EPI_GELU) gelu_tanh8(v);
-                    if (rl < nrows) {
+                    bool stored = false;
+                    if constexpr (I8) {
+                        if (a.out32) {
+                            stored = true;
+                            float* o32 = reinterpret_cast<float*>(a.out) + (dst - a.out);
+                            if (rl < nrows) {
+                                *reinterpret_cast<float4*>(o32) = make_float4(v[0], v[1], v[2], v[3]);
+                                *reinterpret_cast<float4*>(o32 + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                            }
+                        }
+                    }
+                    if (!stored && rl < nrows) {
                         const uint4 o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
                                                    pack_bf16x2(v[6], v[7]));
                         if (EPI == EPI_STORE) *reinterpret_cast<uint4*>(dst) = o;
                         else store_stream16(dst, o);
                     }
-                    dst += r < 3 ? (size_t)a.N : (size_t)a.N * 29;
+                    dst += r < 3 ? ldo : ldo * 29;
                 } else {
                     if (rl >= nrows) continue;
                     if constexpr (EPI == EPI_SCATTER) finish_row<EPI, 8>(a, g, m0 + rl, 0, n_lane, v, tok[4 * i + r], gate[4 * i + r]);
@@ -329,19 +379,19 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const WsGemmArgs 
     else run_rows(std::false_type());
 }
 
-template <int BM, int EPI, bool RAGGED, int POLICY> static int launch_wide_p(const WsGemmArgs& a, const WsGemmArgs* b, hipStream_t s) {
+template <int BM, int EPI, bool RAGGED, int POLICY, class Args> static int launch_wide_p(const Args& a, const Args* b, hipStream_t s) {
     const int n_tiles = (a.N + kWideCols - 1) / kWideCols;
     const long long blocks_a = tile_grid_blocks(a, n_tiles, (a.max_rows + BM - 1) / BM);
     const long long blocks_b = b ? tile_grid_blocks(*b, n_tiles, (b->max_rows + BM - 1) / BM) : 0;
     const long long blocks = blocks_a + blocks_b;                // both multiples of the XCD count
     if (blocks > (1ll << 30)) return MOE_ERR_UNSUPPORTED;        // block indices are ints in the kernel
     static OncePerDevice asked;
-    const int rc = ask_lds(reinterpret_cast<const void*>(&wide_kernel<BM, EPI, RAGGED, POLICY>), kWideLds, asked);
+    const int rc = ask_lds(reinterpret_cast<const void*>(&wide_kernel<BM, EPI, RAGGED, POLICY, Args>), kWideLds, asked);
     if (rc != MOE_OK) return rc;
-    hipLaunchKernelGGL((wide_kernel<BM, EPI, RAGGED, POLICY>), dim3((unsigned)blocks), dim3(kWideThreads), kWideLds, s, a, b ? *b : a, (int)blocks_a);
+    hipLaunchKernelGGL((wide_kernel<BM, EPI, RAGGED, POLICY, Args>), dim3((unsigned)blocks), dim3(kWideThreads), kWideLds, s, a, b ? *b : a, (int)blocks_a);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
-template <int BM, int EPI, bool RAGGED> static int launch_wide_r(const WsGemmArgs& a, const WsGemmArgs* b, int policy, hipStream_t s) {
+template <int BM, int EPI, bool RAGGED, class Args> static int launch_wide_r(const Args& a, const Args* b, int policy, hipStream_t s) {
     if constexpr (wide_hints(EPI)) {
         if (policy == WIDE_STREAMED) return launch_wide_p<BM, EPI, RAGGED, WIDE_STREAMED>(a, b, s);
         if constexpr (BM == 256) {
@@ -350,7 +400,7 @@ template <int BM, int EPI, bool RAGGED> static int launch_wide_r(const WsGemmArg
     }
     return launch_wide_p<BM, EPI, RAGGED, WIDE_CACHED>(a, b, s);
 }
-template <int EPI> int launch_wide_epi(const WsGemmArgs& a, const WsGemmArgs* b, int tile_rows, int policy, hipStream_t s) {
+template <int EPI, class Args> int launch_wide_epi(const Args& a, const Args* b, int tile_rows, int policy, hipStream_t s) {
     if (tile_rows == 256)
         return a.K % kChunk ? launch_wide_r<256, EPI, true>(a, b, policy, s) : launch_wide_r<256, EPI, false>(a, b, policy, s);
     return a.K % kChunk ? launch_wide_r<128, EPI, true>(a, b, policy, s) : launch_wide_r<128, EPI, false>(a, b, policy, s);

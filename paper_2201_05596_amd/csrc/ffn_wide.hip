@@ -3,10 +3,10 @@
 
 namespace moe {
 
-extern template int launch_wide_epi<EPI_STORE>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
-extern template int launch_wide_epi<EPI_GELU>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
-extern template int launch_wide_epi<EPI_SCATTER>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
-extern template int launch_wide_epi<EPI_PARTIAL>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
+extern template int launch_wide_epi<EPI_STORE, WsGemmArgs>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
+extern template int launch_wide_epi<EPI_GELU, WsGemmArgs>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
+extern template int launch_wide_epi<EPI_SCATTER, WsGemmArgs>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
+extern template int launch_wide_epi<EPI_PARTIAL, WsGemmArgs>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
 
 // Both halves of an FFN have weights of this size: beyond 128 MB a pass evicts what the next one would have found in the
 // Infinity Cache.  (64 groups x 128 rows x 4096 x 1024, 537 MB: 105 -> 91 us with the hint, 16 rows 89 -> 79 = 6.8 TB/s; 32

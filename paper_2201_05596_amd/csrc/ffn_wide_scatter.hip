@@ -3,6 +3,6 @@
 
 namespace moe {
 
-template int launch_wide_epi<EPI_SCATTER>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
+template int launch_wide_epi<EPI_SCATTER, WsGemmArgs>(const WsGemmArgs&, const WsGemmArgs*, int, int, hipStream_t);
 
 }  // namespace moe
