@@ -1447,9 +1447,6 @@ int check_i8_weights(const moe_shape_t* s, const moe_i8_weights_t* w, bool dense
     return MOE_OK;
 }
 
-// Rows of a group that the kernel of few rows takes, making the second product's codes from bf16
-constexpr int kI8FewRows = 32;
-
 struct I8Layout {
     WsLayout gate;
     size_t x, x_scale, h, h_max, hq, h_scale, ye, hd, hd_max, hdq, hd_scale, dense, total;
@@ -1492,7 +1489,7 @@ struct I8Ffn {
     float* h_scale;
     int n_rows;                               // rows of h, used or not
 };
-I8Ffn i8_ffn(const moe_shape_t* s, int G, int max_rows, int group_rows, const int32_t* rows, const int8_t* x, const float* x_scale, const void* W1,
+I8Ffn i8_ffn(const moe_shape_t* s, bool few, int G, int max_rows, int group_rows, const int32_t* rows, const int8_t* x, const float* x_scale, const void* W1,
              const float* s1, const void* b1, const void* W2, const float* s2, const void* b2, uint16_t* h, uint32_t* h_max, int8_t* hq, float* h_scale) {
     const int dq = i8_row_bytes(s->d_model), fq = i8_row_bytes(s->d_ffn);
     I8Ffn p{};
@@ -1500,7 +1497,7 @@ I8Ffn i8_ffn(const moe_shape_t* s, int G, int max_rows, int group_rows, const in
     a.A = reinterpret_cast<const uint16_t*>(x); a.a_scale = x_scale; a.B = u16(W1); a.b_scale = s1; a.bias = u16(b1); a.packed = 1;
     a.rows = rows; a.fixed_rows = rows ? 0 : group_rows; a.max_rows = max_rows; a.G = G; a.K = dq / 2; a.lda = dq / 2; a.N = s->d_ffn;
     a.a_group_stride = a.o_group_stride = group_rows; a.out = h; a.ldo = fq; a.ksplit = 1;
-    p.few = max_rows <= kI8FewRows;
+    p.few = few;
     I8GemmArgs& b = p.second;
     b = a;
     b.B = u16(W2); b.b_scale = s2; b.bias = u16(b2); b.K = fq / 2; b.N = s->d_model; b.ldo = s->d_model;
@@ -1515,12 +1512,7 @@ I8Ffn i8_ffn(const moe_shape_t* s, int G, int max_rows, int group_rows, const in
 }
 
 int i8_product(const I8GemmArgs& a, const I8GemmArgs* b, bool few, int epi, hipStream_t st) {
-    if (few) {
-        const int most = b ? std::max(a.max_rows, b->max_rows) : a.max_rows;
-        return launch_i8_few(a, b, epi, i8_few_columns(few_groups(a) + (b ? few_groups(*b) : 0), most, a.N), st);
-    }
-    const bool large = a.max_rows > 128 || (b && b->max_rows > 128);
-    return launch_i8_wide(a, b, large ? 256 : 128, epi, st);
+    return few ? launch_i8_few(a, b, epi, st) : i8_wide_faster(a, b) ? launch_i8_wide(a, b, epi, st) : launch_i8_tile(a, b, epi, st);
 }
 
 // h into codes, unless the second product makes them itself
@@ -1582,7 +1574,7 @@ int moe_i8_linear(const moe_i8_linear_t* product, const int8_t* codes, int64_t c
     a.A = reinterpret_cast<const uint16_t*>(codes); a.lda = codes_stride / 2; a.a_scale = row_scale; a.B = u16(W); a.b_scale = col_scale;
     a.bias = u16(bias); a.packed = 1; a.fixed_rows = a.max_rows = p->n_rows; a.G = 1; a.K = i8_row_bytes(p->K) / 2; a.N = p->N;
     a.out = u16(out); a.ldo = out_stride; a.out32 = p->out_dtype == MOE_F32; a.ksplit = 1;
-    return i8_product(a, nullptr, p->n_rows <= kI8FewRows, p->gelu ? EPI_GELU : EPI_STORE, static_cast<hipStream_t>(stream));
+    return i8_product(a, nullptr, i8_few_faster_alone(p->n_rows, p->N), p->gelu ? EPI_GELU : EPI_STORE, static_cast<hipStream_t>(stream));
 }
 
 size_t moe_i8_workspace_bytes(const moe_shape_t* shape) { return check_i8_shape(shape) == MOE_OK ? i8_layout(shape).total : 0; }
@@ -1600,7 +1592,7 @@ int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights,
     const int E = shape->E, C = shape->capacity, d = shape->d_model;
     int8_t* x = at<int8_t>(ws, L.x);
     float* x_scale = at<float>(ws, L.x_scale);
-    I8Ffn p = i8_ffn(shape, E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
+    I8Ffn p = i8_ffn(shape, i8_few_faster(E, C, d, shape->d_ffn), E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
                      at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
     rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, d, p.few ? at<uint32_t>(ws, L.h_max) : nullptr, (long long)E * C},
                         MOE_BF16, st);
@@ -1638,15 +1630,17 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
     rc = run_gate(shape, x, Wg, bg, logits, expert_idx, slot_idx, gate_w, rows, slot_token, order, ws, L.gate, false, st);
     if (rc != MOE_OK) return rc;
     // an expert has at most one row of a token
-    I8Ffn e = i8_ffn(shape, E, std::min(C, T), C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
+    const int max_rows = std::min(C, T), touched = (int)std::min<long long>((long long)T * k, E);
+    const bool few = i8_few_faster(touched, max_rows, d, shape->d_ffn);
+    I8Ffn e = i8_ffn(shape, few, E, max_rows, C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
                      at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
     e.first.row_map = slot_token; e.first.map_stride = C;
     e.first.order = e.second.order = order;
-    e.first.slots = e.second.slots = (int)std::min<long long>((long long)T * k, E);
+    e.first.slots = e.second.slots = touched;
     e.first.expect_rows = e.second.expect_rows = (int)(((long long)T * k + E - 1) / E);
     I8Ffn n{};
     if (shape->residual)
-        n = i8_ffn(shape, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
+        n = i8_ffn(shape, T <= kI8FewRows && few, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
                    at<uint16_t>(ws, L.hd), at<uint32_t>(ws, L.hd_max), at<int8_t>(ws, L.hdq), at<float>(ws, L.hd_scale));
     const long long most = e.few || n.few ? (long long)E * C + (shape->residual ? T : 0) : 0;
     rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, T, d, most ? at<uint32_t>(ws, L.h_max) : nullptr, most}, MOE_BF16, st);

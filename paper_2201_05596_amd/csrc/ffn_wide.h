@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const Args a0, co
                     if (!stored && rl < nrows) {
                         const uint4 o = make_uint4(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]),
                                                    pack_bf16x2(v[6], v[7]));
-                        if (EPI == EPI_STORE) *reinterpret_cast<uint4*>(dst) = o;
+                        if (EPI == EPI_STORE && !I8) *reinterpret_cast<uint4*>(dst) = o;
                         else store_stream16(dst, o);
                     }
                     dst += r < 3 ? ldo : ldo * 29;

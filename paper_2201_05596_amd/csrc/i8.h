@@ -66,10 +66,15 @@ int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s);
 // ceil(N / 128)
 int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipStream_t s);
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s);
-// (i8_few.hip) few rows, bound by the read of the weights; NF 16-column fragments per work-group; b: a second product in the launch
-int launch_i8_few(const I8GemmArgs& a, const I8GemmArgs* b, int epi, int NF, hipStream_t s);
-int i8_few_columns(long long groups, int max_rows, int N);
-// (i8_wide.hip) tiles of 256 or 128 rows
-int launch_i8_wide(const I8GemmArgs& a, const I8GemmArgs* b, int tile_rows, int epi, hipStream_t s);
+// (i8_few.hip) few rows, bound by the read of the weights; b: a second product in the launch, or nullptr
+int launch_i8_few(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
+constexpr int kI8FewRows = 32;                                   // of a group, where a product makes codes from bf16
+bool i8_few_faster(int groups, int max_rows, int d, int f);      // for both products of FFNs
+bool i8_few_faster_alone(int rows, int N);                       // for one product
+// (i8_tile.hip) tiles of up to 128 rows, two work-groups per compute unit
+int launch_i8_tile(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
+// (i8_wide.hip) tiles of 256 rows
+int launch_i8_wide(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
+bool i8_wide_faster(const I8GemmArgs& a, const I8GemmArgs* b);   // than tiles of 128 rows
 
 }  // namespace moe

@@ -3,23 +3,39 @@
 
 namespace moe {
 
-int launch_i8_wide(const I8GemmArgs& first, const I8GemmArgs* second, int tile_rows, int epi, hipStream_t s) {
+template <int EPI> static int launch_i8_epi(const I8GemmArgs& a, const I8GemmArgs* b, int policy, hipStream_t s) {
+    return a.K % kChunk ? launch_wide_r<256, EPI, true>(a, b, policy, s) : launch_wide_r<256, EPI, false>(a, b, policy, s);
+}
+
+// Against tiles of 128 rows with two work-groups per compute unit (i8_tile.hip), which hide a tile's epilogue and stores and deal finer
+// pieces, but load half as many bytes more per product.  us here / there: 16384 rows, N = 4096, K = 512 / 1024 / 2048 / 4096: 69 / 60, 92 / 88,
+// 134 / 150, 230 / 267; fewer than 160 tiles of 256 rows leave compute units idle (4096 rows, N = 1024, K = 1024: 17.4 / 10.6; 1024 rows,
+// N = 2048, K = 4096: 42 / 26); 64 experts of up to 200 rows, 1024 x 4096 and back 78 + 64 / 91 + 92; of up to 128 rows the same;
+// a dense branch of 8192 tokens with 32 experts of up to 320 rows, 1024 x 4096: 134 / 108, back 94 / 100.
+bool i8_wide_faster(const I8GemmArgs& a, const I8GemmArgs* b) {
+    auto tiles = [](const I8GemmArgs& x) { return (long long)few_groups(x) * ((x.max_rows + 255) / 256) * ((x.N + kWideCols - 1) / kWideCols); };
+    const int most = b && b->max_rows > a.max_rows ? b->max_rows : a.max_rows;
+    if (most <= 128 || tiles(a) + (b ? tiles(*b) : 0) < 160) return false;
+    const long long dense = a.G == 1 ? tiles(a) : b && b->G == 1 ? tiles(*b) : 0;
+    return !(a.K <= 512 && dense >= 512);                        // (pairs of codes)
+}
+
+int launch_i8_wide(const I8GemmArgs& first, const I8GemmArgs* second, int epi, hipStream_t s) {
     if (first.G <= 0 || first.max_rows <= 0) return MOE_OK;
     if (first.K % 32 || first.N % 8 || (second && (second->K != first.K || second->N != first.N))) return MOE_ERR_INVALID_ARG;
     I8GemmArgs a = first, b = second ? *second : first;
-    if (second && b.max_rows > 128 && a.max_rows <= 128) std::swap(a, b);      // the full tiles first
     // weights that one row tile reads once and that do not stay in the Infinity Cache (wide_policy in ffn_wide.hip has the figures)
     auto streams = [](const I8GemmArgs& x) { return (long long)x.G * x.K * x.N * 2 > (128ll << 20); };
     a.stream = streams(a);
     b.stream = streams(b);
     const I8GemmArgs* pb = second ? &b : nullptr;
-    int policy = WIDE_CACHED;
-    if (a.stream && a.max_rows <= tile_rows && (!pb || (b.stream && b.max_rows <= tile_rows))) policy = WIDE_STREAMED;
-    else if (tile_rows == 256 && (a.stream || (pb && b.stream))) policy = WIDE_BY_GROUP;
+    const int policy = a.stream && a.max_rows <= 256 && (!pb || (b.stream && b.max_rows <= 256)) ? WIDE_STREAMED
+                       : a.stream || (pb && b.stream)                                           ? WIDE_BY_GROUP
+                                                                                                : WIDE_CACHED;
     switch (epi) {
-        case EPI_STORE: return launch_wide_epi<EPI_STORE>(a, pb, tile_rows, policy, s);
-        case EPI_GELU: return launch_wide_epi<EPI_GELU>(a, pb, tile_rows, policy, s);
-        case EPI_SCATTER: return second ? MOE_ERR_INVALID_ARG : launch_wide_epi<EPI_SCATTER>(a, pb, tile_rows, policy, s);
+        case EPI_STORE: return launch_i8_epi<EPI_STORE>(a, pb, policy, s);
+        case EPI_GELU: return launch_i8_epi<EPI_GELU>(a, pb, policy, s);
+        case EPI_SCATTER: return second ? MOE_ERR_INVALID_ARG : launch_i8_epi<EPI_SCATTER>(a, pb, policy, s);
         default: return MOE_ERR_INVALID_ARG;
     }
 }
