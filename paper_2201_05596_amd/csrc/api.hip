@@ -1528,7 +1528,7 @@ extern "C" {
 
 size_t moe_i8_weights_bytes(int32_t G, int32_t K, int32_t N) {
     if (G < 1 || K < 8 || N < 8 || K % 8 || N % 8 || K > kI8MaxK || N > kI8MaxK) return 0;
-    return (long long)G * ((N + 127) / 128) * 2 >= 1ll << 22 ? 0 : i8_weight_bytes(G, K, N);
+    return (long long)G * ((N + 127) / 128) * 4 >= 1ll << 22 ? 0 : i8_weight_bytes(G, K, N);
 }
 
 static int check_i8_matrix(int32_t G, int32_t K, int32_t N, std::initializer_list<const void*> ptrs) {

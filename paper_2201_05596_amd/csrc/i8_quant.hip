@@ -1,4 +1,5 @@
-// Rows and weights into 8 bits (i8.h), and codes into the order of the products.  Bound by traffic.
+// Rows and weights into 8 bits (i8.h), and codes into the order of the products.  Bound by traffic: what is large passes the caches by
+// (16384 rows of 4096, 201 MB read and written: 37.1 us through the caches, 32.7 = 6.1 TB/s past them; 33 MB 9.8 and 10.7).
 #include "i8.h"
 
 namespace moe {
@@ -17,15 +18,15 @@ __device__ __forceinline__ uint32_t wave_max_bits(uint32_t m) {
 template <typename T> struct Piece;
 template <> struct Piece<uint16_t> {
     uint4 v;
-    __device__ __forceinline__ void load(const uint16_t* p) { v = *reinterpret_cast<const uint4*>(p); }
+    template <bool BIG> __device__ __forceinline__ void load(const uint16_t* p) { v = BIG ? load_stream16(p) : *reinterpret_cast<const uint4*>(p); }
     __device__ __forceinline__ void none() { v = make_uint4(0, 0, 0, 0); }
     __device__ __forceinline__ void get(float (&f)[8]) const { unpack_bias8(v, f); }
 };
 template <> struct Piece<float> {
     float4 a, b;
-    __device__ __forceinline__ void load(const float* p) {
-        a = reinterpret_cast<const float4*>(p)[0];
-        b = reinterpret_cast<const float4*>(p)[1];
+    template <bool BIG> __device__ __forceinline__ void load(const float* p) {
+        a = BIG ? __builtin_bit_cast(float4, load_stream16(p)) : reinterpret_cast<const float4*>(p)[0];
+        b = BIG ? __builtin_bit_cast(float4, load_stream16(p + 4)) : reinterpret_cast<const float4*>(p)[1];
     }
     __device__ __forceinline__ void none() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
     __device__ __forceinline__ void get(float (&f)[8]) const {
@@ -34,7 +35,8 @@ template <> struct Piece<float> {
 };
 
 // TPR threads (a wave or a work-group) hold a row of up to 8 NP TPR values from its one read to its codes.
-template <typename T, int TPR, int NP>
+// BIG: rows and codes past the caches
+template <typename T, int TPR, int NP, bool BIG>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8RowsArgs a) {
     constexpr int PER = TPR < 256 ? 256 / TPR : 1;               // rows of a work-group
     __shared__ uint32_t part[TPR / kWave];
@@ -49,7 +51,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int at = tid + i * TPR;
-        if (at < pieces) p[i].load(x + (size_t)at * 8);
+        if (at < pieces) p[i].template load<BIG>(x + (size_t)at * 8);
         else p[i].none();
     }
     uint32_t m = 0;
@@ -79,14 +81,19 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
 #pragma unroll
         for (int q = 0; q < 8; ++q) c[q] = m < 0x7f800000u ? i8_code_bits(f[q], inv) : 0u;
         const u32x2_t o = {i8_pack4(c[0], c[1], c[2], c[3]), i8_pack4(c[4], c[5], c[6], c[7])};
-        if (at < padded) *reinterpret_cast<u32x2_t*>(out + (size_t)at * 8) = o;      // zeros behind the row's end
+        if (at >= padded) continue;                              // zeros behind the row's end
+        if (BIG) __builtin_nontemporal_store(o, reinterpret_cast<u32x2_t*>(out + (size_t)at * 8));
+        else *reinterpret_cast<u32x2_t*>(out + (size_t)at * 8) = o;
     }
 }
 
 template <typename T, int TPR, int NP> int launch_rows_p(const I8RowsArgs& a, hipStream_t s) {
     constexpr int per = TPR < 256 ? 256 / TPR : 1;
     const long long blocks = ((long long)a.n_rows + per - 1) / per;
-    hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, s, a);
+    if ((long long)a.n_rows * a.cols * (long long)sizeof(T) > (64ll << 20))
+        hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, true>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, s, a);
+    else
+        hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, false>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, s, a);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 template <typename T> int launch_rows_t(const I8RowsArgs& a, hipStream_t s) {
@@ -105,92 +112,122 @@ template <typename T> int launch_rows_t(const I8RowsArgs& a, hipStream_t s) {
     return launch_rows_p<T, 1024, 16>(a, s);
 }
 
-// 64 columns of a group, all of K, by a work-group of 1024 threads: 8 columns of one of 128 k-rows for each thread and round.
-// Codes cross LDS: a thread's piece of the packed order is 16 k of one column.
-constexpr int kWCols = 64, kWRows = 128, kWThreads = 1024, kWPitch = kWCols + 4;
-static_assert(kWThreads == kWRows * kWCols / 8, "a thread per 8 columns of a row");
-
+// COLS columns of a group, all of K, by a work-group of THREADS: four consecutive k-rows of 8 columns for each thread and round, so that
+// a thread has whole words of the packed order (4 k of a column).  They cross LDS once, which then holds a round's bytes in that order.
 // QUANTISE: from bf16, with the columns' scales; else codes are there.  KEEP: rounds whose values stay in registers from the
-// first pass (the columns' largest magnitudes) to the second; longer K is read again
-template <bool QUANTISE, int KEEP>
-__global__ __launch_bounds__(kWThreads) void i8_weights_kernel(const void* __restrict__ W, int8_t* __restrict__ packed,
-                                                               float* __restrict__ scale, int K, int N, int tiles) {
-    __shared__ uint32_t most[kWThreads / kWave][kWCols];
-    __shared__ int8_t codes[kWRows][kWPitch];
-    const int tid = threadIdx.x, kr = tid >> 3, cp = tid & 7;
-    const long long g = blockIdx.x / tiles;
-    const int n0 = (int)(blockIdx.x % tiles) * kWCols, n = n0 + cp * 8;
-    const int KB = (K + 63) / 64, NG = (N + 127) / 128, rounds = (K + kWRows - 1) / kWRows;
+// first pass (the columns' largest magnitudes) to the second; a longer K is read again, mostly from the Infinity Cache.
+// LARGE: W's last reading and the result past the caches.
+// 64 columns are whole cache lines of W; with 32 there are twice the work-groups, for a single matrix.  Neighbouring tiles, which then share
+// lines, are eight work-groups apart: on the same XCD.  us with 32 / 64 columns: 1000 x 4000 9.0 / 10.2; 64 x 2048 x 8192 876 / 773, past the
+// caches 928 / 692 (3.2 GB: 4.7 TB/s; a thread for 8 columns of one row with the transposition byte by byte in LDS 1083); 16 x 8192 x 2048, read twice,
+// 315 / 285, past the caches 346 / 244.
+template <bool QUANTISE, int KEEP, int THREADS, int COLS, bool LARGE>
+__global__ __launch_bounds__(THREADS, KEEP > 4 ? 2 : 4) void i8_weights_kernel(const void* __restrict__ W, int8_t* __restrict__ packed,
+                                                             float* __restrict__ scale, int K, int N, int tiles, int all) {
+    constexpr int OCTETS = COLS / 8;
+    constexpr int ROWS = THREADS / OCTETS * 4, WAVES = THREADS / kWave;        // k-rows of a round: whole blocks of 64
+    static_assert(ROWS % 64 == 0, "whole blocks");
+    __shared__ uint32_t most[WAVES][COLS];
+    __shared__ uint32_t words[ROWS * COLS / 4];                // [block][fragment][k-group][column of the fragment][4 k]
+    const int tid = threadIdx.x, cp = tid % OCTETS, quad = tid / OCTETS;
+    const int pair = blockIdx.x >> 4, tile = ((pair << 3) + (blockIdx.x & 7)) * 2 + (blockIdx.x >> 3 & 1);
+    const long long g = tile / tiles;
+    const int n0 = tile % tiles * COLS, n = n0 + cp * 8;
+    if (tile >= all) return;
+    const int KB = (K + 63) / 64, NG = (N + 127) / 128, rounds = (K + ROWS - 1) / ROWS;
     const uint16_t* wb = static_cast<const uint16_t*>(W) + (size_t)g * K * N + n;
     const int8_t* wc = static_cast<const int8_t*>(W) + (size_t)g * K * N + n;
-    auto load = [&](int round) {
-        const int k = round * kWRows + kr;
-        return k < K && n < N ? *reinterpret_cast<const uint4*>(wb + (size_t)k * N) : make_uint4(0, 0, 0, 0);
+    auto load = [&](int round, uint4 (&v)[4], bool last) {       // last: nobody reads it again
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = round * ROWS + quad * 4 + i;
+            v[i] = k < K && n < N ? (LARGE && last ? load_stream16(wb + (size_t)k * N) : *reinterpret_cast<const uint4*>(wb + (size_t)k * N)) : make_uint4(0, 0, 0, 0);
+        }
     };
-    uint4 held[KEEP > 0 ? KEEP : 1];
+    uint4 held[KEEP > 0 ? KEEP : 1][4];
     float inv[8];
-    bool dead[8];
     if constexpr (QUANTISE) {
         uint32_t m[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        auto see = [&](const uint4& v) {
-            float f[8];
-            unpack_bias8(v, f);
+        auto see = [&](const uint4 (&v)[4]) {
 #pragma unroll
-            for (int q = 0; q < 8; ++q) m[q] = max(m[q], __float_as_uint(f[q]) & 0x7fffffffu);
+            for (int i = 0; i < 4; ++i) {
+                float f[8];
+                unpack_bias8(v[i], f);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) m[q] = max(m[q], __float_as_uint(f[q]) & 0x7fffffffu);
+            }
         };
         if constexpr (KEEP > 0) {
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) held[i] = load(i);
+            for (int i = 0; i < KEEP; ++i) load(i, held[i], true);
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) see(held[i]);
         } else {
-#pragma unroll 4
-            for (int i = 0; i < rounds; ++i) see(load(i));
+            uint4 next[4];
+            load(0, held[0], false);
+            for (int i = 0; i < rounds; ++i) {
+                load(i + 1, next, false);                        // (zeros behind K)
+                see(held[0]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) held[0][q] = next[q];
+            }
         }
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
 #pragma unroll
-            for (int s = 8; s < 64; s <<= 1) m[q] = max(m[q], (uint32_t)__shfl_xor((int)m[q], s));
-            if ((tid & 63) < 8) most[tid >> 6][cp * 8 + q] = m[q];
+            for (int s = OCTETS; s < 64; s <<= 1) m[q] = max(m[q], (uint32_t)__shfl_xor((int)m[q], s));
+            if ((tid & 63) < OCTETS) most[tid >> 6][cp * 8 + q] = m[q];
         }
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
             uint32_t b = 0;
 #pragma unroll
-            for (int w = 0; w < kWThreads / kWave; ++w) b = max(b, most[w][cp * 8 + q]);
+            for (int w = 0; w < WAVES; ++w) b = max(b, most[w][cp * 8 + q]);
             inv[q] = i8_inverse(b);
-            dead[q] = b >= 0x7f800000u;
-            if (kr == 0 && n < N) scale[(size_t)g * N + n + q] = i8_scale(b);
+            if (quad == 0 && n < N) scale[(size_t)g * N + n + q] = i8_scale(b);
+            if (b >= 0x7f800000u) inv[q] = __uint_as_float(0x7fc00000u);
         }
     }
-    auto finish = [&](int round, const uint4& v) {
-        u32x2_t o = {0, 0};
-        const int k = round * kWRows + kr;
+    auto finish = [&](int round, const uint4 (&v)[4]) {
+        uint32_t o[8];                                           // word q: column q's four codes
         if constexpr (QUANTISE) {
-            float f[8];
-            unpack_bias8(v, f);
-            uint32_t c[8];
+            float f[4][8];
 #pragma unroll
-            for (int q = 0; q < 8; ++q) c[q] = dead[q] ? 0u : i8_code_bits(f[q], inv[q]);
-            o = u32x2_t{i8_pack4(c[0], c[1], c[2], c[3]), i8_pack4(c[4], c[5], c[6], c[7])};
-        } else if (k < K && n < N) {
-            o = *reinterpret_cast<const u32x2_t*>(wc + (size_t)k * N);
+            for (int i = 0; i < 4; ++i) unpack_bias8(v[i], f[i]);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                o[q] = i8_pack4(i8_code_bits(f[0][q], inv[q]), i8_code_bits(f[1][q], inv[q]), i8_code_bits(f[2][q], inv[q]), i8_code_bits(f[3][q], inv[q]));
+                if (inv[q] != inv[q]) o[q] = 0;                  // a column that is not all numbers
+            }
+        } else {
+            u32x2_t r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = round * ROWS + quad * 4 + i;
+                r[i] = k < K && n < N ? *reinterpret_cast<const u32x2_t*>(wc + (size_t)k * N) : u32x2_t{0, 0};
+            }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const int s = q & 3;
+                auto word = [&](int i) { return (q < 4 ? r[i].x : r[i].y) >> (8 * s); };
+                o[q] = i8_pack4(word(0), word(1), word(2), word(3));
+            }
         }
-        __syncthreads();                                         // the round before has been read
-        *reinterpret_cast<uint32_t*>(&codes[kr][cp * 8]) = o.x;
-        *reinterpret_cast<uint32_t*>(&codes[kr][cp * 8 + 4]) = o.y;
-        __syncthreads();
-        // half a piece per thread: k-block, k-group, half | fragment, column of eight
-        const int half = tid & 1, c = (tid >> 1) & 7, kq = (tid >> 4) & 3, j = (tid >> 6) & 7, kb = tid >> 9;
-        uint32_t b[8];
+        const int at = (((quad >> 4) * 8 * 4 + (quad >> 2 & 3)) * OCTETS + cp) * 4 + (quad & 3);
+        if (round > 0) __syncthreads();                          // the round before has been read
 #pragma unroll
-        for (int q = 0; q < 8; ++q) b[q] = (uint8_t)codes[kb * 64 + kq * 16 + half * 8 + q][c * 8 + j];
-        const int kbg = round * 2 + kb;
-        if (kbg < KB) {
-            const size_t at = ((((size_t)g * KB + kbg) * NG + n0 / 128) * 8 + j) * 64 + kq * 16 + n0 % 128 / 8 + c;
-            *reinterpret_cast<u32x2_t*>(packed + at * 16 + half * 8) =
-                u32x2_t{i8_pack4(b[0], b[1], b[2], b[3]), i8_pack4(b[4], b[5], b[6], b[7])};
+        for (int q = 0; q < 8; ++q) words[at + q * (4 * OCTETS * 4)] = o[q];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {                            // a round's pieces of 16 bytes, two for each thread
+            const int p = tid + i * THREADS, c = p % OCTETS, kq = p / OCTETS & 3, j = p / (4 * OCTETS) & 7, kb = round * (ROWS / 64) + p / (32 * OCTETS);
+            if (kb < KB) {
+                const size_t to = ((((size_t)g * KB + kb) * NG + n0 / 128) * 8 + j) * 64 + kq * 16 + n0 % 128 / 8 + c;
+                const uint4 o = *reinterpret_cast<const uint4*>(words + p * 4);
+                if (LARGE) store_stream16(packed + to * 16, o);
+                else *reinterpret_cast<uint4*>(packed + to * 16) = o;
+            }
         }
     };
     if constexpr (KEEP > 0) {
@@ -198,15 +235,25 @@ __global__ __launch_bounds__(kWThreads) void i8_weights_kernel(const void* __res
         for (int i = 0; i < KEEP; ++i)
             if (i < rounds) finish(i, held[i]);
     } else {
-        for (int i = 0; i < rounds; ++i) finish(i, QUANTISE ? load(i) : make_uint4(0, 0, 0, 0));
+        if (QUANTISE) load(0, held[0], true);
+        for (int i = 0; i < rounds; ++i) {
+            uint4 next[4];
+            if (QUANTISE) load(i + 1, next, true);
+            finish(i, held[0]);
+            if (QUANTISE) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) held[0][q] = next[q];
+            }
+        }
     }
 }
 
-template <bool QUANTISE, int KEEP> int launch_weights_k(const void* W, void* packed, float* scale, int G, int K, int N, hipStream_t s) {
-    const int tiles = (N + 127) / 128 * 2;                       // whole blocks of 128 columns, zeros behind N
-    const long long blocks = (long long)G * tiles;
-    if (blocks >= (1ll << 31)) return MOE_ERR_UNSUPPORTED;
-    hipLaunchKernelGGL((i8_weights_kernel<QUANTISE, KEEP>), dim3((unsigned)blocks), dim3(kWThreads), 0, s, W, static_cast<int8_t*>(packed), scale, K, N, tiles);
+template <bool QUANTISE, int KEEP, int THREADS, int COLS, bool LARGE> int launch_weights_k(const void* W, void* packed, float* scale, int G, int K, int N, hipStream_t s) {
+    const int tiles = (N + 127) / 128 * (128 / COLS);         // whole blocks of 128 columns, zeros behind N
+    const long long blocks = ((long long)G * tiles + 15) / 16 * 16;
+    if (blocks * THREADS >= (1ll << 32)) return MOE_ERR_UNSUPPORTED;
+    hipLaunchKernelGGL((i8_weights_kernel<QUANTISE, KEEP, THREADS, COLS, LARGE>), dim3((unsigned)blocks), dim3(THREADS), 0, s, W, static_cast<int8_t*>(packed), scale,
+                       K, N, tiles, G * tiles);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -218,14 +265,18 @@ int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s) {
 }
 
 int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipStream_t s) {
-    return launch_weights_k<false, 0>(codes, packed, nullptr, G, K, N, s);
+    return launch_weights_k<false, 0, 512, 32, false>(codes, packed, nullptr, G, K, N, s);
 }
 
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s) {
-    if (K <= 4 * kWRows) return launch_weights_k<true, 4>(W, packed, scale, G, K, N, s);
-    if (K <= 8 * kWRows) return launch_weights_k<true, 8>(W, packed, scale, G, K, N, s);
-    if (K <= 16 * kWRows) return launch_weights_k<true, 16>(W, packed, scale, G, K, N, s);
-    return launch_weights_k<true, 0>(W, packed, scale, G, K, N, s);
+    if ((long long)G * K * N > (32ll << 20)) {
+        if (K <= 1024) return launch_weights_k<true, 4, 512, 64, true>(W, packed, scale, G, K, N, s);
+        if (K <= 2048) return launch_weights_k<true, 8, 512, 64, true>(W, packed, scale, G, K, N, s);
+        return launch_weights_k<true, 0, 1024, 64, true>(W, packed, scale, G, K, N, s);
+    }
+    if (K <= 1024) return launch_weights_k<true, 2, 512, 32, false>(W, packed, scale, G, K, N, s);
+    if (K <= 4096) return launch_weights_k<true, 8, 512, 32, false>(W, packed, scale, G, K, N, s);
+    return launch_weights_k<true, 0, 1024, 32, false>(W, packed, scale, G, K, N, s);
 }
 
 }  // namespace moe

@@ -40,7 +40,7 @@ def check_rows(x, extra=0):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("rows,cols", [(1, 8), (1, 64), (3, 72), (5, 520), (2, 2048), (7, 2056), (3, 4096), (4, 4104), (2, 8200), (3, 16384), (2, 16392),
                                        (2, 65536), (1, 65544), (2, 131072), (2048, 8), (2049, 512), (2050, 520), (2048, 1032), (2047, 1024), (2048, 2056),
-                                       (2051, 4096), (2048, 4104)])
+                                       (2051, 4096), (2048, 4104), (9000, 4096), (5000, 8200)])
 def test_rows(dtype, rows, cols):
     check_rows(spread(rows, cols, rows + cols, dtype))
 
@@ -87,7 +87,9 @@ def test_rows_behind_4_gib():
 
 
 WEIGHTS = [(1, 8, 8), (1, 64, 128), (2, 72, 136), (3, 520, 264), (1, 1000, 4000), (2, 1032, 64), (1, 2048, 192), (2, 2056, 72), (1, 8192, 128), (1, 131072, 16),
-           (70, 128, 200), (1, 512, 8), (1, 1024, 8), (5, 16, 1000)]
+           (70, 128, 200), (1, 512, 8), (1, 1024, 8), (5, 16, 1000), (1, 4096, 136), (1, 4104, 136),
+           # large ones, past the caches
+           (9, 1000, 4000), (9, 2048, 2056), (3, 2056, 5448), (1, 16392, 2056), (40, 72, 16384)]
 
 
 @pytest.mark.parametrize("G,K,N", WEIGHTS)
