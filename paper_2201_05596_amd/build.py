@@ -14,7 +14,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmoe_hip.so")
-SOURCES = ["api.hip", "gate.hip", "gate_bf16.hip", "layout.hip", "pack.hip", "block.hip", "rope.hip", "kv_cache.hip", "tree_attn.hip", "tree_attn_bf16.hip", "tree_attn_fp8.hip", "tree_attn_fp4.hip", "i8_quant.hip", "i8_few.hip", "i8_tile.hip", "i8_wide.hip", "gemm_f32.hip", "ffn_mfma.hip", "ffn_rows.hip", "ffn_tile.hip", "ffn_wide.hip",
+SOURCES = ["api.hip", "gate.hip", "gate_bf16.hip", "layout.hip", "pack.hip", "block.hip", "rope.hip", "kv_cache.hip", "tree_attn.hip", "tree_attn_bf16.hip", "tree_attn_fp8.hip", "tree_attn_fp4.hip", "i8_quant.hip", "i8_few.hip", "i8_token.hip", "i8_tile.hip", "i8_wide.hip", "gemm_f32.hip", "ffn_mfma.hip", "ffn_rows.hip", "ffn_tile.hip", "ffn_wide.hip",
            "ffn_wide_store.hip", "ffn_wide_gelu.hip", "ffn_wide_scatter.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

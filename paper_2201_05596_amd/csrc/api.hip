@@ -329,7 +329,7 @@ int run_gate_logits(const moe_shape_t* s, const void* x, const float* Wg, const 
 // top-k and the tile-local ranking) and the rest of the routing (ST_ROUTE)
 int run_gate(const moe_shape_t* s, const void* x, const float* Wg, const float* bg, float* logits, int32_t* expert_idx,
              int32_t* slot_idx, float* gate_w, int32_t* rows, int32_t* slot_token, int32_t* order, void* ws,
-             const WsLayout& L, bool profile, hipStream_t st) {
+             const WsLayout& L, bool profile, hipStream_t st, const GateRows& token_rows = GateRows{}) {
     int32_t* scratch = at<int32_t>(ws, L.hist);
     int rc;
     if (s->dtype == MOE_BF16 && gate_bf16_fused_supported(s->T, s->d_model, s->E)) {
@@ -353,7 +353,7 @@ int run_gate(const moe_shape_t* s, const void* x, const float* Wg, const float* 
         if (profile) prof_pre(ST_LOGITS, st);
         rc = launch_gate_decode(x, packed ? nullptr : Wg, packed ? Wg : nullptr, bg, logits, s->T, s->d_model, s->E,
                                 s->top_k, s->capacity, expert_idx, slot_idx, gate_w, rows, slot_token, order,
-                                at<uint64_t>(ws, L.flags), next_call_tag(), st);
+                                at<uint64_t>(ws, L.flags), next_call_tag(), token_rows, st);
         if (profile) prof_mark(ST_LOGITS, st);
         return rc;
     }
@@ -1449,8 +1449,9 @@ int check_i8_weights(const moe_shape_t* s, const moe_i8_weights_t* w, bool dense
 
 struct I8Layout {
     WsLayout gate;
-    size_t x, x_scale, h, h_max, hq, h_scale, ye, hd, hd_max, hdq, hd_scale, dense, total;
+    size_t x, x_scale, h, hq, h_scale, ye, hd, hdq, hd_scale, dense, words, total;
 };
+constexpr int kI8TokenRows = 256;             // tokens of a layer whose experts may have few rows each, at most
 I8Layout i8_layout(const moe_shape_t* s) {
     I8Layout L{};
     const size_t T = s->T, d = s->d_model, E = s->E, C = s->capacity, rows = std::max(T, E * C);
@@ -1463,16 +1464,14 @@ I8Layout i8_layout(const moe_shape_t* s) {
     L.h = take(E * C * fq * 2);
     L.hq = take(E * C * fq);
     L.h_scale = take(E * C * 4);
-    L.ye = take(E * C * d * 2);
+    const size_t few = std::min<size_t>(C, kI8FewRows);
+    L.ye = take(E * std::max(2 * C, 4 * few) * d);               // in 32 bits where rows are few
     const size_t t = s->residual ? T : 0;
     L.hd = take(t * fq * 2);
     L.hdq = take(t * fq);
     L.hd_scale = take(t * 4);
-    L.dense = take(t * d * 4);                // in 32 bits where tokens are few
-    L.h_max = off;                            // next to each other: cleared together
-    off += E * C * 4;
-    L.hd_max = off;
-    off = align_up(off + t * 4);
+    L.dense = take(t * d * (T <= kI8TokenRows ? 4 : 2));
+    L.words = take((E * few + t + i8_token_tiles(s->d_model)) * 4);      // cleared before they are used: the rows' largest magnitudes, counters
     L.total = off;
     return L;
 }
@@ -1512,7 +1511,8 @@ I8Ffn i8_ffn(const moe_shape_t* s, bool few, int G, int max_rows, int group_rows
 }
 
 int i8_product(const I8GemmArgs& a, const I8GemmArgs* b, bool few, int epi, hipStream_t st) {
-    return few ? launch_i8_few(a, b, epi, st) : i8_wide_faster(a, b) ? launch_i8_wide(a, b, epi, st) : launch_i8_tile(a, b, epi, st);
+    if (few && b) return MOE_ERR_INVALID_ARG;
+    return few ? launch_i8_few(a, epi, st) : i8_wide_faster(a, b) ? launch_i8_wide(a, b, epi, st) : launch_i8_tile(a, b, epi, st);
 }
 
 // h into codes, unless the second product makes them itself
@@ -1593,8 +1593,8 @@ int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights,
     int8_t* x = at<int8_t>(ws, L.x);
     float* x_scale = at<float>(ws, L.x_scale);
     I8Ffn p = i8_ffn(shape, i8_few_faster(E, C, d, shape->d_ffn), E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
-                     at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
-    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, d, p.few ? at<uint32_t>(ws, L.h_max) : nullptr, (long long)E * C},
+                     at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.words), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
+    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C},
                         MOE_BF16, st);
     if (rc != MOE_OK) return rc;
     if ((rc = i8_product(p.first, nullptr, p.few, EPI_GELU, st)) != MOE_OK) return rc;
@@ -1627,54 +1627,56 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
     int8_t* xq = at<int8_t>(ws, L.x);
     float* x_scale = at<float>(ws, L.x_scale);
 
-    rc = run_gate(shape, x, Wg, bg, logits, expert_idx, slot_idx, gate_w, rows, slot_token, order, ws, L.gate, false, st);
-    if (rc != MOE_OK) return rc;
     // an expert has at most one row of a token
     const int max_rows = std::min(C, T), touched = (int)std::min<long long>((long long)T * k, E);
-    const bool few = i8_few_faster(touched, max_rows, d, shape->d_ffn);
-    I8Ffn e = i8_ffn(shape, few, E, max_rows, C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
-                     at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.h_max), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
+    const bool few = T <= kI8TokenRows && i8_few_faster(touched, max_rows, d, shape->d_ffn), dense = shape->residual;
+    uint32_t* words = at<uint32_t>(ws, L.words);
+    const int n_maxes = E * max_rows + (dense ? T : 0), n_words = n_maxes + i8_token_tiles(d);
+    // few tokens: the gate's one launch finds the rows' largest magnitudes and clears the words
+    const bool by_gate = few && gate_decode_supported(T, d, E) && d % 64 == 0;
+    uint32_t* x_max = at<uint32_t>(ws, L.x_scale);
+    rc = run_gate(shape, x, Wg, bg, logits, expert_idx, slot_idx, gate_w, rows, slot_token, order, ws, L.gate, false, st,
+                  by_gate ? GateRows{x_max, words, n_words} : GateRows{});
+    if (rc != MOE_OK) return rc;
+    if (!by_gate) {
+        rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, T, d, few ? words : nullptr, n_words}, MOE_BF16, st);
+        if (rc != MOE_OK) return rc;
+    }
+    I8Ffn e = i8_ffn(shape, few, E, max_rows, few ? max_rows : C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2,
+                     weights->b2, at<uint16_t>(ws, L.h), words, at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
     e.first.row_map = slot_token; e.first.map_stride = C;
     e.first.order = e.second.order = order;
     e.first.slots = e.second.slots = touched;
     e.first.expect_rows = e.second.expect_rows = (int)(((long long)T * k + E - 1) / E);
+    e.second.out = at<uint16_t>(ws, L.ye);
     I8Ffn n{};
-    if (shape->residual)
-        n = i8_ffn(shape, T <= kI8FewRows && few, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
-                   at<uint16_t>(ws, L.hd), at<uint32_t>(ws, L.hd_max), at<int8_t>(ws, L.hdq), at<float>(ws, L.hd_scale));
-    const long long most = e.few || n.few ? (long long)E * C + (shape->residual ? T : 0) : 0;
-    rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, T, d, most ? at<uint32_t>(ws, L.h_max) : nullptr, most}, MOE_BF16, st);
-    if (rc != MOE_OK) return rc;
+    if (dense) {
+        n = i8_ffn(shape, few, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
+                   at<uint16_t>(ws, L.hd), words + E * max_rows, at<int8_t>(ws, L.hdq), at<float>(ws, L.hd_scale));
+        n.second.out = at<uint16_t>(ws, L.dense);
+    }
+    if (few) {
+        if (by_gate)
+            for (I8GemmArgs* p : {&e.first, &n.first}) { p->A = u16(x); p->lda = d; p->a_scale = nullptr; p->a_max = x_max; }
+        I8TokenArgs a{e.first, n.first, dense, T, E, k, order, words + n_maxes, expert_idx, slot_idx, gate_w, u16(out)};
+        if ((rc = launch_i8_token(a, false, st)) != MOE_OK) return rc;
+        a.experts = e.second; a.dense_branch = n.second;
+        return launch_i8_token(a, true, st);
+    }
 
-    if (k == 1 && !shape->residual) {         // the combine is in the second product
-        if ((rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
+    if (k == 1 && !dense) {                   // the combine is in the second product
+        if ((rc = i8_product(e.first, nullptr, false, EPI_GELU, st)) != MOE_OK) return rc;
         if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
         I8GemmArgs& a = e.second;
         a.out = u16(out); a.scatter_map = slot_token; a.scatter_stride = C; a.gate_w = gate_w; a.top_k = 1; a.zero_slot_idx = slot_idx; a.T = T;
-        return i8_product(a, nullptr, e.few, EPI_SCATTER, st);
+        return i8_product(a, nullptr, false, EPI_SCATTER, st);
     }
-    e.second.out = at<uint16_t>(ws, L.ye);
-    const void* addend = nullptr;
-    PartSums dense{};
-    if (shape->residual) {
-        n.second.out = at<uint16_t>(ws, L.dense);
-        n.second.out32 = n.few;               // few tokens: rounded once, with the experts' results added
-        if (n.few) dense = PartSums{at<float>(ws, L.dense), 1, nullptr};
-        else addend = at<void>(ws, L.dense);
-        const bool together = e.few == n.few;
-        // the dense branch's tiles, which are full, first
-        if ((rc = i8_product(n.first, together ? &e.first : nullptr, n.few, EPI_GELU, st)) != MOE_OK) return rc;
-        if (!together && (rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
-        if ((rc = i8_between(shape, n, nullptr, st)) != MOE_OK) return rc;
-        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
-        if ((rc = i8_product(n.second, together ? &e.second : nullptr, n.few, EPI_STORE, st)) != MOE_OK) return rc;
-        if (!together && (rc = i8_product(e.second, nullptr, e.few, EPI_STORE, st)) != MOE_OK) return rc;
-    } else {
-        if ((rc = i8_product(e.first, nullptr, e.few, EPI_GELU, st)) != MOE_OK) return rc;
-        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
-        if ((rc = i8_product(e.second, nullptr, e.few, EPI_STORE, st)) != MOE_OK) return rc;
-    }
-    return launch_combine(at<void>(ws, L.ye), MOE_BF16, expert_idx, slot_idx, gate_w, addend, out, T, k, C, d, st, dense);
+    // (the dense branch's tiles, which are full, first)
+    if ((rc = i8_product(dense ? n.first : e.first, dense ? &e.first : nullptr, false, EPI_GELU, st)) != MOE_OK) return rc;
+    if (dense && (rc = i8_between(shape, n, nullptr, st)) != MOE_OK) return rc;
+    if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+    if ((rc = i8_product(dense ? n.second : e.second, dense ? &e.second : nullptr, false, EPI_STORE, st)) != MOE_OK) return rc;
+    return launch_combine(at<void>(ws, L.ye), MOE_BF16, expert_idx, slot_idx, gate_w, dense ? at<void>(ws, L.dense) : nullptr, out, T, k, C, d, st);
 }
 
 int moe_profile_enable(int max_calls) {

@@ -360,12 +360,14 @@ __global__ __launch_bounds__(256) void gate_bf16_kernel(const uint16_t* __restri
 // the same, and gives up (leaving wrong tables, never a hung GPU) after about 10^6 polls.
 // One token, d = 1024, 128 experts: 12.4 us with four waves and a routing by 256 threads; 64 tokens, d = 2048: 23.2.
 constexpr int kDecodeWaves = 16, kDecodeBlocks = 4;      // waves; k-blocks in flight per wave
-template <int MA, int RK, int NV, bool PLAIN>
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+// MAXES: largest magnitudes of the tokens' rows on the way (for 8-bit experts), and scratch words cleared.
+template <int MA, int RK, int NV, bool PLAIN, bool MAXES>
 __global__ __launch_bounds__(kDecodeWaves * 64) void gate_decode_kernel(
     const uint16_t* __restrict__ x, const uint16_t* __restrict__ frags, const float* __restrict__ Wg, const float* __restrict__ bg, float* __restrict__ logits,
     int T, int d, int E, int ET, int C, int32_t* __restrict__ expert_idx, int32_t* __restrict__ slot_idx,
     float* __restrict__ gate_w, int32_t* __restrict__ expert_rows, int32_t* __restrict__ slot_token,
-    int32_t* __restrict__ expert_order, uint64_t* __restrict__ flags, uint64_t tag) {
+    int32_t* __restrict__ expert_order, uint64_t* __restrict__ flags, uint64_t tag, const GateRows rows) {
     static_assert(kDecodeWaves * 64 == kSingleThreads, "the routing uses the same work-group");
     constexpr int TM = 16 * MA;
     extern __shared__ __attribute__((aligned(16))) char lds[];
@@ -382,6 +384,13 @@ __global__ __launch_bounds__(kDecodeWaves * 64) void gate_decode_kernel(
 #pragma unroll
     for (int m = 0; m < MA; ++m) a_src[m] = x + (size_t)min(t0 + 16 * m + c, T - 1) * d + kg * 8;
     const uint16_t* b_src = PLAIN ? nullptr : frags + (size_t)et * 3 * kFragElems + lane * 8;
+    __shared__ uint32_t maxes[MAXES ? kDecodeWaves : 1][MAXES ? TM : 1];
+    uint32_t most[MA];
+    if constexpr (MAXES) {
+#pragma unroll
+        for (int m = 0; m < MA; ++m) most[m] = 0;
+        for (int i = (blockIdx.y * gridDim.x + blockIdx.x) * kDecodeWaves * 64 + tid; i < rows.n_zero; i += gridDim.x * gridDim.y * kDecodeWaves * 64) rows.zero[i] = 0;
+    }
     for (int i0 = 0; i0 < nkb; i0 += kDecodeBlocks) {
         bf16x8_t a[kDecodeBlocks][MA], b[kDecodeBlocks][3];
         float wv[PLAIN ? kDecodeBlocks : 1][8];
@@ -403,6 +412,14 @@ __global__ __launch_bounds__(kDecodeWaves * 64) void gate_decode_kernel(
 #pragma unroll
         for (int i = 0; i < kDecodeBlocks; ++i) {
             if (i0 + i >= nkb) break;
+            if constexpr (MAXES) {
+#pragma unroll
+                for (int m = 0; m < MA; ++m) {
+                    const u32x4_t v = __builtin_bit_cast(u32x4_t, a[i][m]);
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) most[m] = max(most[m], max(v[q] << 16 & 0x7fffffffu, v[q] & 0x7fff0000u));
+                }
+            }
             if constexpr (PLAIN) {
                 zero_past(et * 16 + c, E, wv[i]);
                 split_weights(wv[i], b[i]);
@@ -414,10 +431,24 @@ __global__ __launch_bounds__(kDecodeWaves * 64) void gate_decode_kernel(
         }
     }
 #pragma unroll
-    for (int m = 0; m < MA; ++m)
+    for (int m = 0; m < MA; ++m) {
+        if constexpr (MAXES) {                                   // a row's four lanes, then its waves
+            most[m] = max(most[m], (uint32_t)__shfl_xor((int)most[m], 16));
+            most[m] = max(most[m], (uint32_t)__shfl_xor((int)most[m], 32));
+            if (kg == 0) maxes[w][16 * m + c] = most[m];
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) part[(w * TM + 16 * m + 4 * kg + r) * 16 + c] = acc[m][r];   // D: column lane % 16, rows 4 kg + r
+    }
     __syncthreads();
+    if constexpr (MAXES) {
+        if (et == 0 && tid < TM && t0 + tid < T) {
+            uint32_t v = 0;
+#pragma unroll
+            for (int s = 0; s < kDecodeWaves; ++s) v = max(v, maxes[s][tid]);
+            rows.max[t0 + tid] = v;
+        }
+    }
     if (o_row < TM && t0 + o_row < T && o_col < E) {
         float v = bias;
 #pragma unroll
@@ -506,40 +537,42 @@ int launch_gate_logits_bf16(const void* x, const float* Wg, const void* Wg_packe
 // tag: next_call_tag().
 bool gate_decode_supported(int T, int d, int E) { return gate_bf16_supported(d, E) && T <= kRouteTokens; }
 
-template <int MA, int RK, int NV, bool PLAIN>
+template <int MA, int RK, int NV, bool PLAIN, bool MAXES>
 static int launch_decode_p(const uint16_t* x, const uint16_t* frags, const float* Wg, const float* bg, float* logits, int T, int d, int E,
                              int ET, int C, int32_t* expert_idx, int32_t* slot_idx, float* gate_w, int32_t* expert_rows,
-                             int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, hipStream_t s) {
+                             int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, const GateRows& rows, hipStream_t s) {
     const size_t route = route_single_lds_ints(E, RK) * sizeof(int32_t), sums = (size_t)kDecodeWaves * 16 * MA * 16 * 4;
     const dim3 grid((T + 16 * MA - 1) / (16 * MA), ET);              // smallest tiles: most work-groups (at most 8 x 8)
     if (grid.x * grid.y > kGateFlags) return MOE_ERR_INVALID_ARG;
-    hipLaunchKernelGGL((gate_decode_kernel<MA, RK, NV, PLAIN>), grid, dim3(kDecodeWaves * 64), route > sums ? route : sums, s, x, frags, Wg,
-                       bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, expert_rows, slot_token, expert_order, flags, tag);
+    hipLaunchKernelGGL((gate_decode_kernel<MA, RK, NV, PLAIN, MAXES>), grid, dim3(kDecodeWaves * 64), route > sums ? route : sums, s, x, frags, Wg,
+                       bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, expert_rows, slot_token, expert_order, flags, tag, rows);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
 template <int MA, int RK, int NV>
 static int launch_decode_cfg(const uint16_t* x, const uint16_t* frags, const float* Wg, const float* bg, float* logits, int T, int d, int E,
                              int ET, int C, int32_t* expert_idx, int32_t* slot_idx, float* gate_w, int32_t* expert_rows,
-                             int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, hipStream_t s) {
-    return frags ? launch_decode_p<MA, RK, NV, false>(x, frags, nullptr, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, expert_rows,
-                                                      slot_token, expert_order, flags, tag, s)
-                 : launch_decode_p<MA, RK, NV, true>(x, nullptr, Wg, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, expert_rows,
-                                                     slot_token, expert_order, flags, tag, s);
+                             int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, const GateRows& rows, hipStream_t s) {
+#define MOE_DECODE(PLAIN, MAXES) \
+    launch_decode_p<MA, RK, NV, PLAIN, MAXES>(x, PLAIN ? nullptr : frags, PLAIN ? Wg : nullptr, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, \
+                                              gate_w, expert_rows, slot_token, expert_order, flags, tag, rows, s)
+    if (rows.max) return frags ? MOE_DECODE(false, true) : MOE_DECODE(true, true);
+    return frags ? MOE_DECODE(false, false) : MOE_DECODE(true, false);
+#undef MOE_DECODE
 }
 
 int launch_gate_decode(const void* x, const float* Wg, const void* Wg_packed, const float* bg, float* logits, int T, int d,
                        int E, int k, int C, int32_t* expert_idx, int32_t* slot_idx, float* gate_w, int32_t* expert_rows,
-                       int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, hipStream_t s) {
+                       int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, const GateRows& rows, hipStream_t s) {
     if (!gate_decode_supported(T, d, E) || (!Wg && !Wg_packed) || !flags || k < 1 || k > 2) return MOE_ERR_INVALID_ARG;
     const int ET = padded_expert_tiles(E);
     const uint16_t* frags = static_cast<const uint16_t*>(Wg_packed);
     const uint16_t* xb = static_cast<const uint16_t*>(x);
 #define MOE_DECODE_CASE(kk, nv) \
     return T <= 128 ? launch_decode_cfg<1, kk, nv>(xb, frags, Wg, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, \
-                                                   expert_rows, slot_token, expert_order, flags, tag, s)              \
+                                                   expert_rows, slot_token, expert_order, flags, tag, rows, s)        \
                     : launch_decode_cfg<2, kk, nv>(xb, frags, Wg, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, gate_w, \
-                                                   expert_rows, slot_token, expert_order, flags, tag, s)
+                                                   expert_rows, slot_token, expert_order, flags, tag, rows, s)
     if (k == 1) {
         if (E <= 16) MOE_DECODE_CASE(1, 1);
         if (E <= 32) MOE_DECODE_CASE(1, 2);

@@ -12,6 +12,8 @@
 // For that reason the products count K in pairs of codes.
 #pragma once
 
+#include <algorithm>
+
 #include "ffn_common.h"
 
 namespace moe {
@@ -66,11 +68,25 @@ int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s);
 // ceil(N / 128)
 int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipStream_t s);
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s);
-// (i8_few.hip) few rows, bound by the read of the weights; b: a second product in the launch, or nullptr
-int launch_i8_few(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
+// (i8_few.hip) few rows, bound by the read of the weights; no order, no row map
+int launch_i8_few(const I8GemmArgs& a, int epi, hipStream_t s);
 constexpr int kI8FewRows = 32;                                   // of a group, where a product makes codes from bf16
+int few_columns(long long groups, int max_rows, int N);          // 16-column fragments of a work-group
 bool i8_few_faster(int groups, int max_rows, int d, int f);      // for both products of FFNs
 bool i8_few_faster_alone(int rows, int N);                       // for one product
+// (i8_token.hip) both products and the combine of a layer whose experts have few rows: the first (with h's largest magnitudes) or the second ones
+// (in 32 bits, into ye and the dense branch's rows, then combined into out)
+struct I8TokenArgs {
+    I8GemmArgs experts, dense_branch;
+    int32_t dense, T, E, top_k;
+    const int32_t* order;                                        // as the gate leaves it
+    uint32_t* done;                                              // second: i8_token_tiles(d) counters, 0 before
+    const int32_t *expert_idx, *slot_idx;
+    const float* gate_w;
+    uint16_t* out;
+};
+inline int i8_token_tiles(int N) { return (N + 127) / 128 * 8; } // column tiles of a second product, at most
+int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s);
 // (i8_tile.hip) tiles of up to 128 rows, two work-groups per compute unit
 int launch_i8_tile(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
 // (i8_wide.hip) tiles of 256 rows

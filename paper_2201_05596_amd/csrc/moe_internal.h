@@ -154,10 +154,15 @@ int launch_gate_bf16_fused(const void* x, const float* Wg, const void* Wg_packed
 // the whole gate of at most 256 bf16 tokens in one launch (logits by many work-groups, routing by the last one);
 // flags: kGateFlags words of scratch that may hold anything; tag: next_call_tag()
 constexpr int kGateFlags = 64;
+struct GateRows {              // what the launch does on the way, if max is given: bit patterns of the tokens' largest magnitudes, and words cleared
+    uint32_t* max;
+    uint32_t* zero;
+    int32_t n_zero;
+};
 bool gate_decode_supported(int T, int d, int E);
 int launch_gate_decode(const void* x, const float* Wg, const void* Wg_packed, const float* bg, float* logits, int T, int d,
                        int E, int k, int C, int32_t* expert_idx, int32_t* slot_idx, float* gate_w, int32_t* expert_rows,
-                       int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, hipStream_t s);
+                       int32_t* slot_token, int32_t* expert_order, uint64_t* flags, uint64_t tag, const GateRows& rows, hipStream_t s);
 
 // number of int32 the routing kernels need as scratch
 size_t route_scratch_ints(int T, int E, int k, bool by_logits /* tokens or shapes that the bf16 gate kernels do not take */);
