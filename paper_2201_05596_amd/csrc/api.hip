@@ -1449,7 +1449,7 @@ int check_i8_weights(const moe_shape_t* s, const moe_i8_weights_t* w, bool dense
 
 struct I8Layout {
     WsLayout gate;
-    size_t x, x_scale, h, hq, h_scale, ye, hd, hdq, hd_scale, dense, words, total;
+    size_t x, x_scale, h, hq, h_scale, ye, dense, words, total;     // h and its codes: the experts' rows [E * C], then the dense branch's [T]
 };
 constexpr int kI8TokenRows = 256;             // tokens of a layer whose experts may have few rows each, at most
 I8Layout i8_layout(const moe_shape_t* s) {
@@ -1461,15 +1461,11 @@ I8Layout i8_layout(const moe_shape_t* s) {
     gate_layout(s, L.gate, off, take);
     L.x = take(rows * dq);                    // of the tokens, or of dispatched rows
     L.x_scale = take(rows * 4);
-    L.h = take(E * C * fq * 2);
-    L.hq = take(E * C * fq);
-    L.h_scale = take(E * C * 4);
-    const size_t few = std::min<size_t>(C, kI8FewRows);
+    const size_t few = std::min<size_t>(C, kI8FewRows), t = s->residual ? T : 0;
+    L.h = take((E * C + t) * fq * 2);
+    L.hq = take((E * C + t) * fq);
+    L.h_scale = take((E * C + t) * 4);
     L.ye = take(E * std::max(2 * C, 4 * few) * d);               // in 32 bits where rows are few
-    const size_t t = s->residual ? T : 0;
-    L.hd = take(t * fq * 2);
-    L.hdq = take(t * fq);
-    L.hd_scale = take(t * 4);
     L.dense = take(t * d * (T <= kI8TokenRows ? 4 : 2));
     L.words = take((E * few + t + i8_token_tiles(s->d_model)) * 4);      // cleared before they are used: the rows' largest magnitudes, counters
     L.total = off;
@@ -1483,10 +1479,6 @@ int check_i8_ws(const moe_shape_t* s, const void* ws, size_t ws_bytes) {
 struct I8Ffn {
     I8GemmArgs first, second;
     bool few;
-    uint16_t* h;
-    int8_t* hq;
-    float* h_scale;
-    int n_rows;                               // rows of h, used or not
 };
 I8Ffn i8_ffn(const moe_shape_t* s, bool few, int G, int max_rows, int group_rows, const int32_t* rows, const int8_t* x, const float* x_scale, const void* W1,
              const float* s1, const void* b1, const void* W2, const float* s2, const void* b2, uint16_t* h, uint32_t* h_max, int8_t* hq, float* h_scale) {
@@ -1506,7 +1498,6 @@ I8Ffn i8_ffn(const moe_shape_t* s, bool few, int G, int max_rows, int group_rows
     } else {
         b.A = reinterpret_cast<const uint16_t*>(hq); b.lda = fq / 2; b.a_scale = h_scale;
     }
-    p.h = h; p.hq = hq; p.h_scale = h_scale; p.n_rows = G * group_rows;
     return p;
 }
 
@@ -1515,11 +1506,12 @@ int i8_product(const I8GemmArgs& a, const I8GemmArgs* b, bool few, int epi, hipS
     return few ? launch_i8_few(a, epi, st) : i8_wide_faster(a, b) ? launch_i8_wide(a, b, epi, st) : launch_i8_tile(a, b, epi, st);
 }
 
-// h into codes, unless the second product makes them itself
-int i8_between(const moe_shape_t* s, const I8Ffn& p, const int32_t* rows, hipStream_t st) {
-    if (p.few) return MOE_OK;
+// h into codes for the second products: the experts' rows, and behind them the dense branch's
+int i8_between(const moe_shape_t* s, const I8Layout& L, void* ws, const int32_t* rows, bool dense, hipStream_t st) {
     const long long fq = i8_row_bytes(s->d_ffn);
-    return launch_i8_rows(I8RowsArgs{p.h, fq, fq, p.hq, p.h_scale, rows, rows ? p.n_rows / p.first.G : 0, p.n_rows, s->d_ffn, nullptr, 0}, MOE_BF16, st);
+    const int grouped = s->E * s->capacity;
+    return launch_i8_rows(I8RowsArgs{at<uint16_t>(ws, L.h), fq, fq, at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale), rows, s->capacity, grouped,
+                                     grouped + (dense ? s->T : 0), s->d_ffn, nullptr, 0}, MOE_BF16, st);
 }
 
 }  // namespace
@@ -1555,7 +1547,7 @@ int moe_i8_quantize_rows(int32_t dtype, int32_t n_rows, int32_t n_cols, const vo
         if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
     if (n_cols % 8 || n_cols > kI8MaxK || n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
     if (!row_stride_ok(x_stride, n_cols, dtype == MOE_F32 ? 4 : 8) || !row_stride_ok(codes_stride, i8_row_bytes(n_cols), 16)) return MOE_ERR_INVALID_ARG;
-    return launch_i8_rows(I8RowsArgs{x, x_stride, codes_stride, codes, scale, nullptr, 0, n_rows, n_cols, nullptr, 0}, dtype,
+    return launch_i8_rows(I8RowsArgs{x, x_stride, codes_stride, codes, scale, nullptr, 0, 0, n_rows, n_cols, nullptr, 0}, dtype,
                           static_cast<hipStream_t>(stream));
 }
 
@@ -1594,11 +1586,11 @@ int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights,
     float* x_scale = at<float>(ws, L.x_scale);
     I8Ffn p = i8_ffn(shape, i8_few_faster(E, C, d, shape->d_ffn), E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
                      at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.words), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
-    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C},
+    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C},
                         MOE_BF16, st);
     if (rc != MOE_OK) return rc;
     if ((rc = i8_product(p.first, nullptr, p.few, EPI_GELU, st)) != MOE_OK) return rc;
-    if ((rc = i8_between(shape, p, expert_rows, st)) != MOE_OK) return rc;
+    if (!p.few && (rc = i8_between(shape, L, ws, expert_rows, false, st)) != MOE_OK) return rc;
     p.second.out = u16(ye);
     return i8_product(p.second, nullptr, p.few, EPI_STORE, st);
 }
@@ -1639,7 +1631,7 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
                   by_gate ? GateRows{x_max, words, n_words} : GateRows{});
     if (rc != MOE_OK) return rc;
     if (!by_gate) {
-        rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, T, d, few ? words : nullptr, n_words}, MOE_BF16, st);
+        rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, 0, T, d, few ? words : nullptr, n_words}, MOE_BF16, st);
         if (rc != MOE_OK) return rc;
     }
     I8Ffn e = i8_ffn(shape, few, E, max_rows, few ? max_rows : C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2,
@@ -1651,8 +1643,9 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
     e.second.out = at<uint16_t>(ws, L.ye);
     I8Ffn n{};
     if (dense) {
+        const size_t behind = (size_t)E * C, fq = i8_row_bytes(shape->d_ffn);
         n = i8_ffn(shape, few, 1, T, T, nullptr, xq, x_scale, weights->Wd1, weights->sd1, weights->bd1, weights->Wd2, weights->sd2, weights->bd2,
-                   at<uint16_t>(ws, L.hd), words + E * max_rows, at<int8_t>(ws, L.hdq), at<float>(ws, L.hd_scale));
+                   at<uint16_t>(ws, L.h) + behind * fq, words + E * max_rows, at<int8_t>(ws, L.hq) + behind * fq, at<float>(ws, L.h_scale) + behind);
         n.second.out = at<uint16_t>(ws, L.dense);
     }
     if (few) {
@@ -1666,15 +1659,14 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
 
     if (k == 1 && !dense) {                   // the combine is in the second product
         if ((rc = i8_product(e.first, nullptr, false, EPI_GELU, st)) != MOE_OK) return rc;
-        if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+        if ((rc = i8_between(shape, L, ws, rows, false, st)) != MOE_OK) return rc;
         I8GemmArgs& a = e.second;
         a.out = u16(out); a.scatter_map = slot_token; a.scatter_stride = C; a.gate_w = gate_w; a.top_k = 1; a.zero_slot_idx = slot_idx; a.T = T;
         return i8_product(a, nullptr, false, EPI_SCATTER, st);
     }
     // (the dense branch's tiles, which are full, first)
     if ((rc = i8_product(dense ? n.first : e.first, dense ? &e.first : nullptr, false, EPI_GELU, st)) != MOE_OK) return rc;
-    if (dense && (rc = i8_between(shape, n, nullptr, st)) != MOE_OK) return rc;
-    if ((rc = i8_between(shape, e, rows, st)) != MOE_OK) return rc;
+    if ((rc = i8_between(shape, L, ws, rows, dense, st)) != MOE_OK) return rc;
     if ((rc = i8_product(dense ? n.second : e.second, dense ? &e.second : nullptr, false, EPI_STORE, st)) != MOE_OK) return rc;
     return launch_combine(at<void>(ws, L.ye), MOE_BF16, expert_idx, slot_idx, gate_w, dense ? at<void>(ws, L.dense) : nullptr, out, T, k, C, d, st);
 }

@@ -50,7 +50,7 @@ struct I8GemmArgs : WsGemmArgs {
 // groups of a product that can have rows
 inline int few_groups(const I8GemmArgs& a) { return a.order && a.slots > 0 && a.slots < a.G ? a.slots : a.G; }
 
-// (i8_quant.hip) rows x [n_rows, cols] -> codes, scale.  rows != nullptr: row r counts if r % capacity < rows[r / capacity], others
+// (i8_quant.hip) rows x [n_rows, cols] -> codes, scale.  Of the first n_grouped rows, row r counts if r % capacity < rows[r / capacity], others
 // stay as they are.  zero: n_zero words that are cleared on the way, or nullptr.
 struct I8RowsArgs {
     const void* x;
@@ -58,7 +58,7 @@ struct I8RowsArgs {
     int8_t* codes;
     float* scale;
     const int32_t* rows;
-    int capacity, n_rows, cols;
+    int capacity, n_grouped, n_rows, cols;
     uint32_t* zero;
     long long n_zero;
 };

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
     const long long r = (long long)blockIdx.x * PER + threadIdx.x / TPR;
     if (a.zero)
         for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.n_zero; i += (long long)gridDim.x * blockDim.x) a.zero[i] = 0;
-    if (r >= a.n_rows || (a.rows && r % a.capacity >= a.rows[r / a.capacity])) return;   // the whole wave or work-group
+    if (r >= a.n_rows || (r < a.n_grouped && r % a.capacity >= a.rows[r / a.capacity])) return;   // the whole wave or work-group
     const T* x = static_cast<const T*>(a.x) + r * a.x_stride;
     Piece<T> p[NP];
     const int pieces = a.cols / 8, padded = (a.cols + 63) / 64 * 8;

@@ -10,13 +10,15 @@ namespace moe {
 
 namespace {
 
-constexpr int kTileCols = 256, kTileThreads = 256, kTileStages = 3;
+constexpr int kTileCols = 256, kTileThreads = 256;
+// stages in the ring: with 128 rows two, for three work-groups per compute unit
+constexpr int tile_stages(int rows) { return rows == 128 ? 2 : 3; }
 
 // ROWS: 128, 64 or 32 rows of a tile; NT: weights with the non-temporal hint
 template <int ROWS, int EPI, bool NT>
-__global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmArgs a0, const I8GemmArgs a1, const int split) {
-    constexpr int NS = kTileStages, STAGE = 64 * (ROWS + kTileCols);               // bytes of a stage: activations, then weights
-    static_assert(2 * NS * STAGE <= 160 * 1024 && NS * STAGE >= 4 * 768, "two work-groups per compute unit; room for the scales");
+__global__ __launch_bounds__(kTileThreads, ROWS == 128 ? 3 : 2) void i8_tile_kernel(const I8GemmArgs a0, const I8GemmArgs a1, const int split) {
+    constexpr int NS = tile_stages(ROWS), STAGE = 64 * (ROWS + kTileCols);               // bytes of a stage: activations, then weights
+    static_assert((ROWS == 128 ? 3 : 2) * NS * STAGE <= 160 * 1024 && NS * STAGE >= 4 * 1280, "work-groups per compute unit; room for the epilogue's tables");
     const bool second = (int)blockIdx.x >= split;                // uniform over the work-group
     const I8GemmArgs& a = second ? a1 : a0;
     const int block = second ? (int)blockIdx.x - split : (int)blockIdx.x;
@@ -56,6 +58,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmAr
         const int n_mine = min(n0 + tid, a.N - 1);               // one row's scale, one column's scale and bias for each thread
         const float row_scale = a.a_scale[first + s_row], col_scale = a.b_scale[(size_t)g * a.N + n_mine];
         const float bias = a.bias ? bf16_to_f32(a.bias[(size_t)g * a.N + n_mine]) : 0.f;
+        int token = 0;                                           // top-1 combine: a row's token and gate weight for each thread
+        float gate = 0.f;
+        if constexpr (EPI == EPI_SCATTER) scatter_lookup(a, g, m0 + min(tid, nrows - 1), token, gate);
         const uint16_t* a_src[NA];
 #pragma unroll
         for (int i = 0; i < NA; ++i) a_src[i] = a.A + (first + row[i]) * a.lda + ((lane & 3) ^ (lane >> 4)) * 8;
@@ -110,11 +115,15 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmAr
         }
 
         // ---- epilogue ----------------------------------------------------------------------------------------
-        float* share = reinterpret_cast<float*>(lds);            // rows' scales, columns' scales, columns' biases
+        float* share = reinterpret_cast<float*>(lds);            // rows' scales, columns' scales, columns' biases, rows' gate weights and tokens
         wait_vmcnt_barrier<0>();                                 // the ring has been read
         share[tid] = row_scale;
         share[256 + tid] = col_scale;
         share[512 + tid] = bias;
+        if constexpr (EPI == EPI_SCATTER) {
+            share[768 + tid] = gate;
+            share[1024 + tid] = __int_as_float(token);
+        }
         __syncthreads();
         const int n_lane = n0 + wn * 128 + c * 8;
         if (n_lane >= a.N) return;
@@ -123,16 +132,6 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmAr
         for (int j = 0; j < 8; ++j) {
             cs[j] = share[256 + wn * 128 + c * 8 + j];
             b8[j] = share[512 + wn * 128 + c * 8 + j];
-        }
-        // top-1 combine: tokens and gate weights of all the lane's rows in two round trips, not two for each row
-        int tok[EPI == EPI_SCATTER ? ACT * 4 : 1];
-        float gate[EPI == EPI_SCATTER ? ACT * 4 : 1];
-        if constexpr (EPI == EPI_SCATTER) {
-            const int32_t* map = a.scatter_map + (size_t)g * a.scatter_stride + m0;
-#pragma unroll
-            for (int q = 0; q < ACT * 4; ++q) tok[q] = map[min((2 * (q / 4) + wm) * 16 + kg * 4 + q % 4, nrows - 1)];
-#pragma unroll
-            for (int q = 0; q < ACT * 4; ++q) gate[q] = a.gate_w[(size_t)tok[q] * a.top_k];
         }
 #pragma unroll
         for (int i = 0; i < ACT; ++i) {
@@ -146,7 +145,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmAr
                 if constexpr (EPI == EPI_GELU) gelu_tanh8(v);
                 if (rl >= nrows) continue;
                 if constexpr (EPI == EPI_SCATTER) {
-                    finish_row<EPI, 8>(a, g, m0 + rl, 0, n_lane, v, tok[4 * i + r], gate[4 * i + r]);
+                    finish_row<EPI, 8>(a, g, m0 + rl, 0, n_lane, v, __float_as_int(share[1024 + rl]), share[768 + rl]);
                 } else {
                     const size_t at = ((size_t)g * a.o_group_stride + m0 + rl) * a.ldo + n_lane;
                     if (a.out32) {
@@ -167,7 +166,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void i8_tile_kernel(const I8GemmAr
 }
 
 template <int ROWS, int EPI, bool NT> int launch_tile(const I8GemmArgs& a, const I8GemmArgs* b, hipStream_t s) {
-    const int n_tiles = (a.N + kTileCols - 1) / kTileCols, bytes = kTileStages * 64 * (ROWS + kTileCols);
+    const int n_tiles = (a.N + kTileCols - 1) / kTileCols, bytes = tile_stages(ROWS) * 64 * (ROWS + kTileCols);
     const long long blocks_a = tile_grid_blocks(a, n_tiles, (a.max_rows + ROWS - 1) / ROWS);
     const long long blocks = blocks_a + (b ? tile_grid_blocks(*b, n_tiles, (b->max_rows + ROWS - 1) / ROWS) : 0);
     if (blocks >= 1ll << 24) return MOE_ERR_UNSUPPORTED;
