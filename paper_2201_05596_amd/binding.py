@@ -654,10 +654,6 @@ def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, 
 
 # ---- products in 8-bit integers ----------------------------------------------------------------------------------
 
-def _i8_row_bytes(K: int) -> int:
-    return (K + 63) // 64 * 64
-
-
 def moe_i8_weights_bytes(G: int, K: int, N: int) -> int:
     return int(load_library().moe_i8_weights_bytes(int(G), int(K), int(N)))
 
@@ -697,16 +693,18 @@ def moe_i8_quantize_rows(x, codes, scale) -> None:
     rows, cols = x.shape
     if rows == 0:
         return
-    if x.dtype not in (torch.float32, torch.bfloat16):
-        raise ValueError(f"x: expected float32 or bfloat16, got {x.dtype}")
-    if codes.dim() != 2 or codes.shape[1] < _i8_row_bytes(cols):
-        raise ValueError(f"codes: expected {rows} rows of at least {_i8_row_bytes(cols)}, got {tuple(codes.shape)}")
+    dtype = x.dtype
+    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+        raise ValueError(f"x: expected float32 or bfloat16, got {dtype}")
+    if codes.dim() != 2 or codes.shape[1] < (cols + 63) // 64 * 64:
+        raise ValueError(f"codes: expected {rows} rows of at least {(cols + 63) // 64 * 64}, got {tuple(codes.shape)}")
     dev = torch._C._cuda_getDevice()
-    xp, xs = _rows(x, dev, x.dtype, rows, cols, "x")
-    rc = load_library().moe_i8_quantize_rows(
-        MOE_F32 if x.dtype == torch.float32 else MOE_BF16, rows, cols, xp, xs, *_rows(codes, dev, torch.int8, rows, codes.shape[1], "codes"),
-        _at(scale, dev, torch.float32, rows, "scale"), torch._C._cuda_getCurrentRawStream(dev))
-    _check("moe_i8_quantize_rows", rc)
+    xp, xs = _rows(x, dev, dtype, rows, cols, "x")
+    cp, cs = _rows(codes, dev, torch.int8, rows, codes.shape[1], "codes")
+    rc = load_library().moe_i8_quantize_rows(MOE_BF16 if dtype is torch.bfloat16 else MOE_F32, rows, cols, xp, xs, cp, cs,
+                                             _at(scale, dev, torch.float32, rows, "scale"), torch._C._cuda_getCurrentRawStream(dev))
+    if rc:
+        _check("moe_i8_quantize_rows", rc)
 
 
 def make_i8_linear(n_rows: int, K: int, N: int, out_dtype, gelu: bool = False) -> MoeI8Linear:
@@ -722,8 +720,8 @@ def moe_i8_linear(product: MoeI8Linear, codes, row_scale, W, col_scale, bias, ou
     rows, K, N = product.n_rows, product.K, product.N
     if rows == 0:
         return
-    if codes.dim() != 2 or codes.shape[1] < _i8_row_bytes(K):
-        raise ValueError(f"codes: expected {rows} rows of at least {_i8_row_bytes(K)}, got {tuple(codes.shape)}")
+    if codes.dim() != 2 or codes.shape[1] < (K + 63) // 64 * 64:
+        raise ValueError(f"codes: expected {rows} rows of at least {(K + 63) // 64 * 64}, got {tuple(codes.shape)}")
     f32, dev = torch.float32, torch._C._cuda_getDevice()
     rc = load_library().moe_i8_linear(
         ctypes.byref(product), *_rows(codes, dev, torch.int8, rows, codes.shape[1], "codes"), _at(row_scale, dev, f32, rows, "row_scale"),
@@ -742,28 +740,39 @@ def _i8_weights_need(G: int, K: int, N: int) -> int:
 
 
 @functools.lru_cache(maxsize=256)
-def _i8_workspace_need(shape: bytes) -> int:
-    return moe_i8_workspace_bytes(MoeShape.from_buffer_copy(shape))
-
-
-def _i8_weights(shape, weights: dict, device: int, dense: bool) -> MoeI8Weights:
-    d, f, E = shape.d_model, shape.d_ffn, shape.E
-    up, down, f32, i8, bf = _i8_weights_need, (f, d), torch.float32, torch.int8, torch.bfloat16
-    sizes = {"W1": (i8, up(E, d, f)), "s1": (f32, E * f), "b1": (bf, E * f), "W2": (i8, up(E, *down)), "s2": (f32, E * d), "b2": (bf, E * d)}
+def _i8_tensors(shape: bytes, dense: bool):
+    """(name, dtype, elements) of a call's weights, the sizes of its other tensors and the bytes of its workspace."""
+    s = MoeShape.from_buffer_copy(shape)
+    T, d, f, E, k, C = s.T, s.d_model, s.d_ffn, s.E, s.top_k, s.capacity
+    f32, i8, bf, up = torch.float32, torch.int8, torch.bfloat16, moe_i8_weights_bytes
+    weights = [("W1", i8, up(E, d, f)), ("s1", f32, E * f), ("b1", bf, E * f), ("W2", i8, up(E, f, d)), ("s2", f32, E * d), ("b2", bf, E * d)]
     if dense:
-        sizes |= {"Wd1": (i8, up(1, d, f)), "sd1": (f32, f), "bd1": (bf, f), "Wd2": (i8, up(1, *down)), "sd2": (f32, d), "bd2": (bf, d)}
-    return MoeI8Weights(**{n: _at(weights.get(n), device, *sizes[n], n) for n in sizes})
+        weights += [("Wd1", i8, up(1, d, f)), ("sd1", f32, f), ("bd1", bf, f), ("Wd2", i8, up(1, f, d)), ("sd2", f32, d), ("bd2", bf, d)]
+    return tuple(weights), (T * d, _wg(s) if s.E > 0 and s.d_model > 0 else 0, E, T * E, T * k, E * C, E * C * d), moe_i8_workspace_bytes(s)
+
+
+def _i8_weights(tensors, weights: dict, device: int) -> MoeI8Weights:
+    at = []
+    for name, dtype, numel in tensors:
+        t = weights.get(name)
+        if t is None:
+            at.append(None)
+            continue
+        if t.get_device() != device or t.dtype is not dtype or t.numel() != numel or not t.is_contiguous():
+            _refuse(t, dtype, numel, name)
+        at.append(t.data_ptr())
+    return MoeI8Weights(*at)
 
 
 def moe_i8_expert_ffn(shape, weights: dict, xe, expert_rows, ye, ws) -> None:
     """`weights`: name -> tensor (or None) for the fields of moe_i8_weights_t."""
     bf, dev = torch.bfloat16, torch._C._cuda_getDevice()
-    n = shape.E * shape.capacity
-    w = _i8_weights(shape, weights, dev, False)
-    wp, nbytes = _workspace(ws, dev, _i8_workspace_need(bytes(shape)))
+    tensors, sizes, need = _i8_tensors(bytes(shape), False)
+    w = _i8_weights(tensors, weights, dev)
+    wp, nbytes = _workspace(ws, dev, need)
     rc = load_library().moe_i8_expert_ffn(
-        ctypes.byref(shape), ctypes.byref(w), _at(xe, dev, bf, n * shape.d_model, "xe"), _at(expert_rows, dev, torch.int32, shape.E, "expert_rows"),
-        _at(ye, dev, bf, n * shape.d_model, "ye"), wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
+        ctypes.byref(shape), ctypes.byref(w), _at(xe, dev, bf, sizes[6], "xe"), _at(expert_rows, dev, torch.int32, shape.E, "expert_rows"),
+        _at(ye, dev, bf, sizes[6], "ye"), wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
     _check("moe_i8_expert_ffn", rc)
 
 
@@ -771,16 +780,17 @@ def moe_i8_layer_forward(shape, weights: dict, x, Wg, bg, out, logits_out, exper
                          slot_token_out, ws) -> None:
     """`weights` as in moe_i8_expert_ffn, with the dense branch's for residual layers."""
     bf, i32, f32, dev = torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getDevice()
-    T, d, E, k, C = shape.T, shape.d_model, shape.E, shape.top_k, shape.capacity
-    w = _i8_weights(shape, weights, dev, True)
-    wp, nbytes = _workspace(ws, dev, _i8_workspace_need(bytes(shape)))
+    tensors, (n, gate, E, logits, choices, slots, _), need = _i8_tensors(bytes(shape), True)
+    w = _i8_weights(tensors, weights, dev)
+    wp, nbytes = _workspace(ws, dev, need)
     rc = load_library().moe_i8_layer_forward(
-        ctypes.byref(shape), ctypes.byref(w), _at(x, dev, bf, T * d, "x"), _at(Wg, dev, f32, _wg(shape), "Wg"), _at(bg, dev, f32, E, "bg"),
-        _at(out, dev, bf, T * d, "out"), _at(logits_out, dev, f32, T * E, "logits_out"), _at(expert_idx_out, dev, i32, T * k, "expert_idx_out"),
-        _at(slot_idx_out, dev, i32, T * k, "slot_idx_out"), _at(gate_w_out, dev, f32, T * k, "gate_w_out"),
-        _at(expert_rows_out, dev, i32, E, "expert_rows_out"), _at(slot_token_out, dev, i32, E * C, "slot_token_out"), wp, nbytes,
+        ctypes.byref(shape), ctypes.byref(w), _at(x, dev, bf, n, "x"), _at(Wg, dev, f32, gate, "Wg"), _at(bg, dev, f32, E, "bg"),
+        _at(out, dev, bf, n, "out"), _at(logits_out, dev, f32, logits, "logits_out"), _at(expert_idx_out, dev, i32, choices, "expert_idx_out"),
+        _at(slot_idx_out, dev, i32, choices, "slot_idx_out"), _at(gate_w_out, dev, f32, choices, "gate_w_out"),
+        _at(expert_rows_out, dev, i32, E, "expert_rows_out"), _at(slot_token_out, dev, i32, slots, "slot_token_out"), wp, nbytes,
         torch._C._cuda_getCurrentRawStream(dev))
-    _check("moe_i8_layer_forward", rc)
+    if rc:
+        _check("moe_i8_layer_forward", rc)
 
 
 def moe_profile_enable(max_calls: int) -> None:

@@ -80,7 +80,7 @@ __host__ __device__ __forceinline__ TileId tile_of_block(const WsGemmArgs& a, in
 // Which mapping applies is decided on the device, by the flag (bit 0) behind the launch order (only the device knows the row
 // counts); the host sizes the grid for either.
 __host__ __device__ __forceinline__ bool tile_spread_possible(const WsGemmArgs& a, int n_tiles) {
-    return a.order != nullptr && a.spread != 2 && a.ksplit == 1 && a.G >= kXcd && n_tiles % kXcd == 0;
+    return (a.order != nullptr || a.spread == 1) && a.spread != 2 && a.ksplit == 1 && a.G >= kXcd && n_tiles % kXcd == 0;
 }
 __device__ __forceinline__ bool tile_spread(const WsGemmArgs& a, int n_tiles) {
     return tile_spread_possible(a, n_tiles) && (a.spread == 1 || (a.order[a.G] & 1));
