@@ -654,6 +654,10 @@ def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, 
 
 # ---- products in 8-bit integers ----------------------------------------------------------------------------------
 
+# looked up once: a call's kernels take as long as its Python
+_BF16, _F32, _INT8 = torch.bfloat16, torch.float32, torch.int8
+_get_device, _get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
 def moe_i8_weights_bytes(G: int, K: int, N: int) -> int:
     return int(load_library().moe_i8_weights_bytes(int(G), int(K), int(N)))
 
@@ -673,19 +677,32 @@ def moe_i8_quantize_weights(W: torch.Tensor):
     """(packed codes, scale [G,N] or [N]) of bf16 weights [G,K,N] or [K,N]; torch owns the new buffers."""
     G, K, N, packed = _i8_matrix(W, "W")
     scale = torch.empty(W.shape[:-2] + (N,), dtype=torch.float32, device=W.device)
-    dev = torch._C._cuda_getDevice()
+    dev = _get_device()
     _check("moe_i8_quantize_weights", load_library().moe_i8_quantize_weights(
-        G, K, N, _at(W, dev, torch.bfloat16, G * K * N, "W"), packed.data_ptr(), scale.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
+        G, K, N, _at(W, dev, torch.bfloat16, G * K * N, "W"), packed.data_ptr(), scale.data_ptr(), _get_stream(dev)))
     return packed, scale
 
 
 def moe_i8_pack_weights(codes: torch.Tensor) -> torch.Tensor:
     """Packed copy of int8 codes [G,K,N] or [K,N]; torch owns the new buffer."""
     G, K, N, packed = _i8_matrix(codes, "codes")
-    dev = torch._C._cuda_getDevice()
+    dev = _get_device()
     _check("moe_i8_pack_weights", load_library().moe_i8_pack_weights(
-        G, K, N, _at(codes, dev, torch.int8, G * K * N, "codes"), packed.data_ptr(), torch._C._cuda_getCurrentRawStream(dev)))
+        G, K, N, _at(codes, dev, torch.int8, G * K * N, "codes"), packed.data_ptr(), _get_stream(dev)))
     return packed
+
+
+def _i8_rows(t, device: int, dtype, rows: int, cols: int, name: str):
+    """_rows, for [rows, cols or more] of which cols are read or written."""
+    shape = t.shape
+    if t.get_device() != device or t.dtype is not dtype:
+        _refuse(t, dtype, rows * cols, name)
+    if len(shape) != 2 or shape[0] != rows or shape[1] < cols:
+        raise ValueError(f"{name}: expected {rows} rows of at least {cols}, got {tuple(shape)}")
+    between, inside = t.stride()
+    if inside != 1:
+        raise ValueError(f"{name}: the elements of a row have to be adjacent")
+    return t.data_ptr(), between if rows > 1 else shape[1]
 
 
 def moe_i8_quantize_rows(x, codes, scale) -> None:
@@ -694,15 +711,13 @@ def moe_i8_quantize_rows(x, codes, scale) -> None:
     if rows == 0:
         return
     dtype = x.dtype
-    if dtype is not torch.bfloat16 and dtype is not torch.float32:
+    if dtype is not _BF16 and dtype is not _F32:
         raise ValueError(f"x: expected float32 or bfloat16, got {dtype}")
-    if codes.dim() != 2 or codes.shape[1] < (cols + 63) // 64 * 64:
-        raise ValueError(f"codes: expected {rows} rows of at least {(cols + 63) // 64 * 64}, got {tuple(codes.shape)}")
-    dev = torch._C._cuda_getDevice()
+    dev = _get_device()
     xp, xs = _rows(x, dev, dtype, rows, cols, "x")
-    cp, cs = _rows(codes, dev, torch.int8, rows, codes.shape[1], "codes")
-    rc = load_library().moe_i8_quantize_rows(MOE_BF16 if dtype is torch.bfloat16 else MOE_F32, rows, cols, xp, xs, cp, cs,
-                                             _at(scale, dev, torch.float32, rows, "scale"), torch._C._cuda_getCurrentRawStream(dev))
+    cp, cs = _i8_rows(codes, dev, _INT8, rows, (cols + 63) // 64 * 64, "codes")
+    rc = load_library().moe_i8_quantize_rows(MOE_BF16 if dtype is _BF16 else MOE_F32, rows, cols, xp, xs, cp, cs, _at(scale, dev, _F32, rows, "scale"),
+                                             _get_stream(dev))
     if rc:
         _check("moe_i8_quantize_rows", rc)
 
@@ -720,14 +735,13 @@ def moe_i8_linear(product: MoeI8Linear, codes, row_scale, W, col_scale, bias, ou
     rows, K, N = product.n_rows, product.K, product.N
     if rows == 0:
         return
-    if codes.dim() != 2 or codes.shape[1] < (K + 63) // 64 * 64:
-        raise ValueError(f"codes: expected {rows} rows of at least {(K + 63) // 64 * 64}, got {tuple(codes.shape)}")
-    f32, dev = torch.float32, torch._C._cuda_getDevice()
-    rc = load_library().moe_i8_linear(
-        ctypes.byref(product), *_rows(codes, dev, torch.int8, rows, codes.shape[1], "codes"), _at(row_scale, dev, f32, rows, "row_scale"),
-        _at(W, dev, torch.int8, _i8_weights_need(1, K, N), "W"), _at(col_scale, dev, f32, N, "col_scale"), _at(bias, dev, torch.bfloat16, N, "bias"),
-        *_rows(out, dev, f32 if product.out_dtype == MOE_F32 else torch.bfloat16, rows, N, "out"), torch._C._cuda_getCurrentRawStream(dev))
-    _check("moe_i8_linear", rc)
+    dev = _get_device()
+    cp, cs = _i8_rows(codes, dev, _INT8, rows, (K + 63) // 64 * 64, "codes")
+    op, os_ = _rows(out, dev, _F32 if product.out_dtype == MOE_F32 else _BF16, rows, N, "out")
+    rc = load_library().moe_i8_linear(ctypes.byref(product), cp, cs, _at(row_scale, dev, _F32, rows, "row_scale"), _at(W, dev, _INT8, _i8_weights_need(1, K, N), "W"),
+                                      _at(col_scale, dev, _F32, N, "col_scale"), _at(bias, dev, _BF16, N, "bias"), op, os_, _get_stream(dev))
+    if rc:
+        _check("moe_i8_linear", rc)
 
 
 def moe_i8_workspace_bytes(shape: MoeShape) -> int:
@@ -766,20 +780,20 @@ def _i8_weights(tensors, weights: dict, device: int) -> MoeI8Weights:
 
 def moe_i8_expert_ffn(shape, weights: dict, xe, expert_rows, ye, ws) -> None:
     """`weights`: name -> tensor (or None) for the fields of moe_i8_weights_t."""
-    bf, dev = torch.bfloat16, torch._C._cuda_getDevice()
+    bf, dev = torch.bfloat16, _get_device()
     tensors, sizes, need = _i8_tensors(bytes(shape), False)
     w = _i8_weights(tensors, weights, dev)
     wp, nbytes = _workspace(ws, dev, need)
     rc = load_library().moe_i8_expert_ffn(
         ctypes.byref(shape), ctypes.byref(w), _at(xe, dev, bf, sizes[6], "xe"), _at(expert_rows, dev, torch.int32, shape.E, "expert_rows"),
-        _at(ye, dev, bf, sizes[6], "ye"), wp, nbytes, torch._C._cuda_getCurrentRawStream(dev))
+        _at(ye, dev, bf, sizes[6], "ye"), wp, nbytes, _get_stream(dev))
     _check("moe_i8_expert_ffn", rc)
 
 
 def moe_i8_layer_forward(shape, weights: dict, x, Wg, bg, out, logits_out, expert_idx_out, slot_idx_out, gate_w_out, expert_rows_out,
                          slot_token_out, ws) -> None:
     """`weights` as in moe_i8_expert_ffn, with the dense branch's for residual layers."""
-    bf, i32, f32, dev = torch.bfloat16, torch.int32, torch.float32, torch._C._cuda_getDevice()
+    bf, i32, f32, dev = torch.bfloat16, torch.int32, torch.float32, _get_device()
     tensors, (n, gate, E, logits, choices, slots, _), need = _i8_tensors(bytes(shape), True)
     w = _i8_weights(tensors, weights, dev)
     wp, nbytes = _workspace(ws, dev, need)
@@ -788,7 +802,7 @@ def moe_i8_layer_forward(shape, weights: dict, x, Wg, bg, out, logits_out, exper
         _at(out, dev, bf, n, "out"), _at(logits_out, dev, f32, logits, "logits_out"), _at(expert_idx_out, dev, i32, choices, "expert_idx_out"),
         _at(slot_idx_out, dev, i32, choices, "slot_idx_out"), _at(gate_w_out, dev, f32, choices, "gate_w_out"),
         _at(expert_rows_out, dev, i32, E, "expert_rows_out"), _at(slot_token_out, dev, i32, slots, "slot_token_out"), wp, nbytes,
-        torch._C._cuda_getCurrentRawStream(dev))
+        _get_stream(dev))
     if rc:
         _check("moe_i8_layer_forward", rc)
 

@@ -142,7 +142,9 @@ def test_binding_refuses():
         m.moe_i8_quantize_rows(x.to(DEV), codes.to(DEV), torch.zeros(5, device=DEV))
     with pytest.raises(m.MoeError):
         m.moe_i8_quantize_rows(torch.zeros(4, 68, device=DEV, dtype=torch.bfloat16)[:, :60], codes.to(DEV), scale.to(DEV))
-    m.moe_i8_quantize_rows(x.to(DEV)[:0], codes.to(DEV)[:0], scale.to(DEV)[:0])      # no rows: nothing to do
+    for bad in (codes.to(DEV)[:, :48], codes.to(DEV)[:3], codes.to(DEV).view(-1), torch.zeros(4, 128, dtype=torch.int8, device=DEV)[:, ::2]):
+        with pytest.raises(ValueError, match="codes"):
+            m.moe_i8_quantize_rows(x.to(DEV), bad, scale.to(DEV))
 
 
 def test_captured_and_on_another_stream():

@@ -119,15 +119,12 @@ def test_pointers_and_workspace():
 
 
 def test_binding_checks():
-    x, codes, scale = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(4, 64, dtype=torch.int8), torch.zeros(4)
-    with pytest.raises(ValueError, match="codes: expected 4 rows of at least 64"):
-        B.moe_i8_quantize_rows(x, codes[:, :48], scale)
     with pytest.raises(ValueError, match="x: expected float32 or bfloat16"):
-        B.moe_i8_quantize_rows(x.half(), codes, scale)
+        B.moe_i8_quantize_rows(torch.zeros(4, 64, dtype=torch.float16), None, None)
     with pytest.raises(ValueError, match="expected \\[K, N\\]"):
         B.moe_i8_pack_weights(torch.zeros(64, dtype=torch.int8))
     with pytest.raises(B.MoeError) as e:
         B.moe_i8_pack_weights(torch.zeros(60, 64, dtype=torch.int8))
     assert e.value.status == -2
-    with pytest.raises(ValueError, match="codes: expected 4 rows of at least 128"):
-        B.moe_i8_linear(B.make_i8_linear(4, 72, 64, "bf16"), codes, scale, codes, scale, None, x)
+    B.moe_i8_quantize_rows(torch.zeros(0, 64), None, None)                # no rows: nothing to do
+    B.moe_i8_linear(B.make_i8_linear(0, 64, 64, "bf16"), None, None, None, None, None, None)
