@@ -410,12 +410,13 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
  *   code = v r rounded to the nearest whole number, ties to even (the product itself is not rounded);  a value reads as code s.
  * A row or column that holds an infinity or NaN has codes 0 and scale NaN, so that whatever it takes part in is NaN.
  * A product of rows and columns is  acc (s_row s_col) + bias,  acc the exact sum of the products of codes (K <= 131072: it
- * stays below 2^31), the rest in 32 bits.  It does not depend on an order of summation: any split, tile or number of rows gives
+ * stays below 2^31; a program's own codes may be -128, but not on both sides throughout such a K), the rest in 32 bits.  It does not depend on an order of summation: any split, tile or number of rows gives
  * the same bits.  (A scale product outside of float's range gives zeros, infinities or NaN.)
  *
  * Rows of codes are at distances of a multiple of 16 bytes, at least K rounded up to 64; what is between K and there may be
  * anything (moe_i8_quantize_rows writes zeros).  K and N are multiples of 8, at most 131072.
- * Weights are laid out once, in the order of the matrix instructions: moe_i8_weights_bytes(G, K, N) bytes (0 = not covered), from
+ * Weights are laid out once, in the order of the matrix instructions: moe_i8_weights_bytes(G, K, N) bytes (0 = not covered:
+ * G ceil(N / 128) is at most 2^20 - 4), from
  * bf16 weights [G,K,N] by moe_i8_quantize_weights, scale [G,N], or from codes [G,K,N] that a program has by moe_i8_pack_weights.
  * Outputs may overlap no input. */
 size_t moe_i8_weights_bytes(int32_t G, int32_t K, int32_t N);
@@ -428,7 +429,8 @@ int moe_i8_quantize_rows(int32_t dtype, int32_t n_rows, int32_t n_cols, const vo
                          int64_t codes_stride, float* scale, void* stream);
 
 /* moe_i8_linear -- out [n_rows, N] = codes W with both scales, + bias [N] (bf16, or NULL), through gelu_tanh if product->gelu;
- * rounded once to out_dtype, rows at distances of out_stride elements (a multiple of 8, float: 4).  Up to 2^24 rows. */
+ * rounded once to out_dtype, rows at distances of out_stride elements (a multiple of 8, float: 4).  Up to 2^24 rows, and
+ * (ceil(n_rows / 128) + 9) ceil(N / 16) < 2^23. */
 typedef struct {
     int32_t n_rows, K, N;
     int32_t out_dtype;     /* moe_dtype_t                                        */
@@ -450,10 +452,11 @@ typedef struct {
  *   h = gelu_tanh(q(xe[e,c,:]) W1[e] + b1[e]) rounded to bf16,   ye[e,c,:] = q(h) W2[e] + b2[e]
  * Other rows of ye are left untouched.
  * moe_i8_layer_forward -- moe_layer_forward with 8-bit experts (and dense branch): the gate on x as it is, then the FFNs as
- * above on q(x), combined in 32 bits; expert results of top-2 and residual layers, and a dense branch's of more than 32 tokens,
- * are rounded to bf16 before they are added up.
- * Both: shape.dtype is MOE_BF16, T and E * capacity at most 2^24, shape.flags 0 or MOE_FLAG_PACKED_GATE (layer only has a
- * gate); the dense branch's members of `weights` are not looked at by moe_i8_expert_ffn.
+ * above on q(x), combined in 32 bits.  In layers of more than 256 tokens, or of experts with room for more than 32 rows, top-2 and
+ * residual ones round the experts' and the dense branch's results to bf16 before they are added up, and so do those whose few
+ * rows touch many experts; others round the sum once.
+ * Both: shape.dtype is MOE_BF16, T and E * capacity at most 2^24, (ceil(rows / 128) + E + 8) ceil(max(d, f) / 16) < 2^23 with the
+ * larger of the two as rows, shape.flags 0 or MOE_FLAG_PACKED_GATE (layer only has a gate); the dense branch's members of `weights` are not looked at by moe_i8_expert_ffn.
  * ws >= moe_i8_workspace_bytes(shape), 0 for shapes that are rejected. */
 size_t moe_i8_workspace_bytes(const moe_shape_t* shape);
 int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights, const void* xe, const int32_t* expert_rows,

@@ -1511,7 +1511,7 @@ int i8_between(const moe_shape_t* s, const I8Layout& L, void* ws, const int32_t*
     const long long fq = i8_row_bytes(s->d_ffn);
     const int grouped = s->E * s->capacity;
     return launch_i8_rows(I8RowsArgs{at<uint16_t>(ws, L.h), fq, fq, at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale), rows, s->capacity, grouped,
-                                     grouped + (dense ? s->T : 0), s->d_ffn, nullptr, 0}, MOE_BF16, st);
+                                     grouped + (dense ? s->T : 0), s->d_ffn, nullptr, 0, 0}, MOE_BF16, st);
 }
 
 }  // namespace
@@ -1520,7 +1520,7 @@ extern "C" {
 
 size_t moe_i8_weights_bytes(int32_t G, int32_t K, int32_t N) {
     if (G < 1 || K < 8 || N < 8 || K % 8 || N % 8 || K > kI8MaxK || N > kI8MaxK) return 0;
-    return (long long)G * ((N + 127) / 128) * 4 >= 1ll << 22 ? 0 : i8_weight_bytes(G, K, N);
+    return (long long)G * ((N + 127) / 128) > (1 << 20) - 4 ? 0 : i8_weight_bytes(G, K, N);      // (work-groups of 1024 threads, in sixteens)
 }
 
 static int check_i8_matrix(int32_t G, int32_t K, int32_t N, std::initializer_list<const void*> ptrs) {
@@ -1547,7 +1547,7 @@ int moe_i8_quantize_rows(int32_t dtype, int32_t n_rows, int32_t n_cols, const vo
         if (!p || !aligned16(p)) return MOE_ERR_INVALID_ARG;
     if (n_cols % 8 || n_cols > kI8MaxK || n_rows > kMaxRows) return MOE_ERR_UNSUPPORTED;
     if (!row_stride_ok(x_stride, n_cols, dtype == MOE_F32 ? 4 : 8) || !row_stride_ok(codes_stride, i8_row_bytes(n_cols), 16)) return MOE_ERR_INVALID_ARG;
-    return launch_i8_rows(I8RowsArgs{x, x_stride, codes_stride, codes, scale, nullptr, 0, 0, n_rows, n_cols, nullptr, 0}, dtype,
+    return launch_i8_rows(I8RowsArgs{x, x_stride, codes_stride, codes, scale, nullptr, 0, 0, n_rows, n_cols, nullptr, 0, 0}, dtype,
                           static_cast<hipStream_t>(stream));
 }
 
@@ -1589,7 +1589,7 @@ int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights,
     // few experts of unknown sizes: each XCD a part of every one (8 experts of up to 1024 rows, 2048 / 8192: 134 + 90 -> 119 + 86 us; 32 of up to 256
     // 128 + 106 -> 128 + 134)
     if (E < 16) p.first.spread = p.second.spread = 1;
-    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C},
+    rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C, 0},
                         MOE_BF16, st);
     if (rc != MOE_OK) return rc;
     if ((rc = i8_product(p.first, nullptr, p.few, EPI_GELU, st)) != MOE_OK) return rc;
@@ -1634,7 +1634,7 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
                   by_gate ? GateRows{x_max, words, n_words} : GateRows{});
     if (rc != MOE_OK) return rc;
     if (!by_gate) {
-        rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, 0, T, d, few ? words : nullptr, n_words}, MOE_BF16, st);
+        rc = launch_i8_rows(I8RowsArgs{x, d, i8_row_bytes(d), xq, x_scale, nullptr, 0, 0, T, d, few ? words : nullptr, n_words, 0}, MOE_BF16, st);
         if (rc != MOE_OK) return rc;
     }
     I8Ffn e = i8_ffn(shape, few, E, max_rows, few ? max_rows : C, rows, xq, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2,

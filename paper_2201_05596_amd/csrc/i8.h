@@ -61,6 +61,7 @@ struct I8RowsArgs {
     int capacity, n_grouped, n_rows, cols;
     uint32_t* zero;
     long long n_zero;
+    int first;                 // the launcher's: first row of a launch
 };
 int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s);
 // (i8_quant.hip) codes of W [G, K, N] in the order of the products, a lane's 16 bytes being 16 consecutive k of a column: byte (k, n)
@@ -87,7 +88,7 @@ struct I8TokenArgs {
 };
 inline int i8_token_tiles(int N) { return (N + 127) / 128 * 8; } // column tiles of a second product, at most
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s);
-// (i8_tile.hip) tiles of up to 128 rows, two work-groups per compute unit
+// (i8_tile.hip) tiles of up to 128 rows, two or three work-groups per compute unit
 int launch_i8_tile(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
 // (i8_wide.hip) tiles of 256 rows
 int launch_i8_wide(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);

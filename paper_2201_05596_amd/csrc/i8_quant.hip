@@ -41,7 +41,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
     constexpr int PER = TPR < 256 ? 256 / TPR : 1;               // rows of a work-group
     __shared__ uint32_t part[TPR / kWave];
     const int tid = threadIdx.x % TPR;
-    const long long r = (long long)blockIdx.x * PER + threadIdx.x / TPR;
+    const long long r = a.first + (long long)blockIdx.x * PER + threadIdx.x / TPR;
     if (a.zero)
         for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < a.n_zero; i += (long long)gridDim.x * blockDim.x) a.zero[i] = 0;
     if (r >= a.n_rows || (r < a.n_grouped && r % a.capacity >= a.rows[r / a.capacity])) return;   // the whole wave or work-group
@@ -88,12 +88,17 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
 }
 
 template <typename T, int TPR, int NP> int launch_rows_p(const I8RowsArgs& a, hipStream_t s) {
-    constexpr int per = TPR < 256 ? 256 / TPR : 1;
-    const long long blocks = ((long long)a.n_rows + per - 1) / per;
-    if ((long long)a.n_rows * a.cols * (long long)sizeof(T) > (64ll << 20))
-        hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, true>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, s, a);
-    else
-        hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, false>), dim3((unsigned)blocks), dim3(TPR < 256 ? 256 : TPR), 0, s, a);
+    constexpr int threads = TPR < 256 ? 256 : TPR, per = threads / TPR;
+    constexpr int most = 1 << 21;                                // work-groups of a launch, whose threads are counted in 32 bits
+    const bool big = (long long)a.n_rows * a.cols * (long long)sizeof(T) > (64ll << 20);
+    I8RowsArgs part = a;
+    for (long long first = 0; first < a.n_rows; first += (long long)most * per) {
+        const dim3 blocks((unsigned)std::min<long long>(most, (a.n_rows - first + per - 1) / per));
+        part.first = (int)first;
+        if (big) hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, true>), blocks, dim3(threads), 0, s, part);
+        else hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, false>), blocks, dim3(threads), 0, s, part);
+        part.zero = nullptr;
+    }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 template <typename T> int launch_rows_t(const I8RowsArgs& a, hipStream_t s) {

@@ -1,9 +1,13 @@
-// Tiles of 128 rows x 256 columns on codes (i8.h), two work-groups per compute unit: one's epilogue and stores run beside the
-// other's matrix instructions.  The four-wave kernel of 256-row tiles (ffn_wide.h) has one work-group per unit, whose epilogue and
+// Tiles of 128, 64 or 32 rows x 256 columns on codes (i8.h), two or three work-groups per compute unit: one's epilogue and stores run beside the
+// others' matrix instructions.  The four-wave kernel of 256-row tiles (ffn_wide.h) has one work-group per unit, whose epilogue and
 // stores nothing hides: on codes its main loop is half as long, and with a short K that is most of a tile's time.
 //
-// A wave owns every other 16-row sub-tile of 128 columns: 128 accumulator registers, operands of one 64-deep stage.  Stages go
-// from memory straight to LDS, three in the ring; a stage's barrier also frees the slot that the stage before it left.
+// A wave owns every other 16-row sub-tile of 128 columns: 128 accumulator registers with 128 rows, operands of one 64-deep stage.  Stages go
+// from memory straight to LDS; a stage's barrier also frees the slot that the stage before it left.  Two stages in the ring with 128 rows: then
+// three work-groups fit, and what a short ring does not hide the others do (16384 rows, N = 4096, K = 512 / 1024 / 2048: 44 / 69 / 128 us, with
+// three stages and two work-groups 51 / 77 / 136); three with fewer rows, where 32 rows take 18 KB of weights and rows for each stage and loads are all there is.
+// Bound by what a compute unit takes in by direct loads (46 to 60 GB/s with 256 of them at work): 128 rows of codes of 16384 x 2048 x 4096 105 us
+// = 2.6 PFLOP/s; 50 experts of a decode step, 2048 x 8192 with up to 16 rows, 128 us = 6.6 TB/s of codes.
 #include "ffn_wide.h"
 
 namespace moe {

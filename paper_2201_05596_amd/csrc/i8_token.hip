@@ -6,8 +6,9 @@
 // token, in 32 bits, and rounds once: nobody waits for anybody.
 // Hand-over across the XCDs' separate L2s: results are written with device-scope stores (through the L2), a work-group waits for its stores before
 // it counts itself, and the last one acquires at device scope before its loads.  The counters are cleared by the gate's launch.
-// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.2 + 8.0 us; as launches that bring x into codes, multiply, multiply and combine
-// 4.2 + 6.3 + 6.0 + 4.1.  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
+// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 11.2 us behind a gate of 9.2, 26.4 for the call; as launches that bring x
+// into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1, 27.6 for the call.  16 tokens, top-2 of 64 experts beside one: 33 + 32 us
+// (212 MB of codes: 3.2 TB/s).  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
 // a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across
 // the L2s of about 4 us, as long as a launch).
 #include "i8_few.h"

@@ -324,6 +324,20 @@ def test_experts_behind_4_gib():
         assert torch.equal(ye[e], L.expert(xe[e], e)), e
 
 
+@pytest.mark.parametrize("name", ["one_token_residual", "step", "prefill"])
+@pytest.mark.parametrize("pack", [False, True])
+def test_layer_object(name, pack):
+    """MoELayer(int8=True): the entry point's bits and routing, its weights codes only."""
+    L = Layer(**LAYERS[name], seed=2)
+    want, r = L.forward()
+    plain = {n: W[0] if n[1] == "d" else W for n, W in L.plain.items()}
+    bias = {n: L.weights[n] if L.weights[n] is None or n[1] != "d" else L.weights[n][0] for n in L.weights if n[0] == "b"}
+    layer = L.m.MoELayer(L.T, L.d, L.f, L.E, L.k, L.C, "bf16", L.Wg, L.bg, **plain, **bias, pack_weights=pack, int8=True)
+    for _ in range(2):
+        assert torch.equal(layer(L.x), want) and all(torch.equal(layer.routing[n], r[n]) for n in r)
+    assert layer.i8["W1"].dtype == torch.int8 and not any(t is W for t in layer.weights for W in plain.values())
+
+
 def test_binding_refuses():
     L = Layer(**LAYERS["step_residual"], seed=1)
     out = torch.empty_like(L.x)

@@ -86,6 +86,19 @@ def test_rows_behind_4_gib():
     assert (codes.cpu().numpy() == want).all() and (scale.cpu().numpy() == s).all()
 
 
+def test_more_rows_than_a_launch_has():
+    """Launches of 2^21 work-groups, four rows each."""
+    n = (1 << 23) + 5
+    x = torch.ones((n, 8), device=DEV)
+    x[:, 3] = 2 * (torch.arange(n, device=DEV) % 61 + 1)                   # the largest: codes 127 there, 127 / it elsewhere
+    codes, scale = torch.full((n + 1, 64), 77, dtype=torch.int8, device=DEV), torch.full((n + 1,), 5.0, device=DEV)
+    U.amd().moe_i8_quantize_rows(x, codes[:n], scale[:n])
+    want, s = o.quantise(x[:61].cpu().numpy(), 1)
+    at = torch.arange(n, device=DEV) % 61
+    assert torch.equal(scale[:n], torch.from_numpy(s).to(DEV)[at]) and (codes[n] == 77).all() and scale[n] == 5
+    assert torch.equal(codes[:n, :8], torch.from_numpy(want).to(device=DEV, dtype=torch.int8)[at]) and not codes[:n, 8:].any()
+
+
 WEIGHTS = [(1, 8, 8), (1, 64, 128), (2, 72, 136), (3, 520, 264), (1, 1000, 4000), (2, 1032, 64), (1, 2048, 192), (2, 2056, 72), (1, 8192, 128), (1, 131072, 16),
            (70, 128, 200), (1, 512, 8), (1, 1024, 8), (5, 16, 1000), (1, 4096, 136), (1, 4104, 136),
            # large ones, past the caches

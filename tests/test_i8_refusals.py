@@ -12,8 +12,9 @@ FAKE, ODD, BIG = 0x1000, 0x1008, 1 << 45
 def test_weights_bytes():
     for G, K, N, n in ((1, 64, 128, 8192), (3, 8, 8, 3 * 8192), (2, 1000, 4000, 2 * 16 * 32 * 8192), (1, 131072, 8, 2048 * 8192)):
         assert B.moe_i8_weights_bytes(G, K, N) == n
-    for bad in ((0, 64, 128), (1, 0, 128), (1, 64, 0), (1, 60, 128), (1, 64, 4), (1, 131080, 8), (1, 8, 131080), (1 << 21, 8, 8), (-1, 64, 128)):
+    for bad in ((0, 64, 128), (1, 0, 128), (1, 64, 0), (1, 60, 128), (1, 64, 4), (1, 131080, 8), (1, 8, 131080), (1 << 21, 8, 8), (-1, 64, 128), ((1 << 20) - 3, 8, 8), (1 << 10, 8, 131072)):
         assert B.moe_i8_weights_bytes(*bad) == 0
+    assert B.moe_i8_weights_bytes((1 << 20) - 4, 8, 8) == ((1 << 20) - 4) * 8192
 
 
 @pytest.mark.parametrize("G,K,N,code", [(0, 64, 64, -1), (1, 0, 64, -1), (1, 64, 0, -1), (1, 4, 64, -1), (1, 60, 64, -2), (1, 64, 68, -2), (1, 131080, 64, -2),
