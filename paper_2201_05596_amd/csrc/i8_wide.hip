@@ -11,14 +11,15 @@ template <int EPI> static int launch_i8_epi(const I8GemmArgs& a, const I8GemmArg
 // pieces, but load half as many bytes more per product.  us here / there: 16384 rows, N = 4096, K = 512 / 1024 / 2048 / 4096 / 8192: 69 / 53, 92 / 77,
 // 134 / 127, 230 / 242, 435 / 516; with one tile for each compute unit (4096 rows) 19 / 18, 24 / 24, 34 / 37, 55 / 65, 99 / 123; fewer than 160
 // tiles of 256 rows leave compute units idle (4096 rows, N = 1024, K = 1024: 17.4 / 10.6; 1024 rows, N = 2048, K = 4096: 42 / 26); 64 experts of up to 200
-// rows, 1024 x 4096 and back 78 + 64 / 91 + 90; of up to 128 rows the same; a dense branch of 8192 tokens with 32 experts of up to 320 rows,
+// rows, 1024 x 4096 and back 78 + 64 / 91 + 90; of up to 128 rows the same; 16 of up to 512 rows, 2048 x 8192: 139 / 149; of groups with more rows, whose
+// weights many row tiles share: 8 experts of up to 1024 rows, 2048 x 8192: 117 / 98; a dense branch of 8192 tokens with 32 experts of up to 320 rows,
 // 1024 x 4096: 134 / 101, back 95 / 97.
 bool i8_wide_faster(const I8GemmArgs& a, const I8GemmArgs* b) {
     auto tiles = [](const I8GemmArgs& x) { return (long long)few_groups(x) * ((x.max_rows + 255) / 256) * ((x.N + kWideCols - 1) / kWideCols); };
     const int most = b && b->max_rows > a.max_rows ? b->max_rows : a.max_rows;
     if (most <= 128 || tiles(a) + (b ? tiles(*b) : 0) < 160) return false;
-    const long long dense = a.G == 1 ? tiles(a) : b && b->G == 1 ? tiles(*b) : 0;
-    return !(a.K <= 1024 && dense >= 512);                       // (pairs of codes)
+    auto high = [&](const I8GemmArgs& x) { return x.max_rows >= 1024 ? tiles(x) : 0; };
+    return !(a.K <= 1024 && high(a) + (b ? high(*b) : 0) >= 512);        // (pairs of codes)
 }
 
 int launch_i8_wide(const I8GemmArgs& first, const I8GemmArgs* second, int epi, hipStream_t s) {
