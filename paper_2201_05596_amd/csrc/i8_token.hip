@@ -2,15 +2,15 @@
 // of the dense branch, then their second products with the combine.  Bound by latency with a token or two, by the read of the weights
 // with more (i8_few.h).
 // The first launch takes the tokens in bf16 with their largest magnitudes, which the gate's launch finds on its way, and the second one h with those
-// that the first one raises: no launch makes codes.  The work-group that finishes a column tile's last group adds the groups' results up for every
-// token, in 32 bits, and rounds once: nobody waits for anybody.
-// Hand-over across the XCDs' separate L2s: results are written with device-scope stores (through the L2), a work-group waits for its stores before
-// it counts itself, and the last one acquires at device scope before its loads.  The counters are cleared by the gate's launch.
-// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 11.2 us behind a gate of 9.2, 26.4 for the call; as launches that bring x
-// into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1, 27.6 for the call.  16 tokens, top-2 of 64 experts beside one: 33 + 32 us
+// that the first one raises: no launch makes codes.  With the fewest tokens a work-group of the second one has its columns of every group.  Else
+// the work-group that finishes a column tile's last group adds the groups' results up for every token, in 32 bits, and rounds once: nobody waits for
+// anybody.  Its hand-over across the XCDs' separate L2s costs about 4 us: results are written with device-scope stores (through the L2), a work-group
+// waits for its stores before it counts itself, and the last one acquires at device scope before its loads.  The counters are cleared by the
+// gate's launch.
+// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 8.6 us behind a gate of 9.2, with a hand-over 6.7 + 11.2; as launches that
+// bring x into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1.  16 tokens, top-2 of 64 experts beside one: 33 + 32 us
 // (212 MB of codes: 3.2 TB/s).  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
-// a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across
-// the L2s of about 4 us, as long as a launch).
+// a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across the L2s).
 #include "i8_few.h"
 
 namespace moe {
@@ -116,6 +116,140 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_second_kernel(const I8
     }
 }
 
+// The second products and the combine of the fewest tokens, without a hand-over: a work-group has 8 columns of every group, its waves split K.  h's
+// rows become codes in LDS once, while the weights are on their way: kGatherAhead pairs of blocks of 64 k for each wave and group.  A pair is one operand:
+// columns 0 .. 7 are the first block's and 8 .. 15 the same eight of the second, rows 0 .. 7 of the other operand the tokens' codes of the first block and
+// 8 .. 15 those of the second, and of the results the two blocks' own quarters are taken.
+constexpr int kGatherGroups = 4, kGatherAhead = 4, kGatherPieces = 8, kGatherBytes = kTokenThreads * kGatherPieces * 8;
+__global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8TokenArgs t) {
+    __shared__ __attribute__((aligned(16))) int8_t codes[kGatherBytes];                          // [group][token's place][K]
+    __shared__ int part[kTokenWaves][kGatherGroups][4][16];
+    const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, kg = lane >> 4, half = c >> 3;
+    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int N = t.experts.N, nkb = t.experts.K / 32, bytes = t.experts.K * 2, p_ng = (N + 127) / 128, dense = t.dense ? 1 : 0;
+    const int ng = blockIdx.x >> 4, frag = blockIdx.x >> 1 & 7, col8 = (blockIdx.x & 1) * 8;     // columns 128 ng + frag + 8 (col8 .. col8 + 7)
+    const int groups = __builtin_amdgcn_readfirstlane(dense + (t.order[t.E] >> 1));
+    int g[kGatherGroups];
+#pragma unroll
+    for (int q = 0; q < kGatherGroups; ++q) g[q] = __builtin_amdgcn_readfirstlane(q < groups && q >= dense ? t.order[q - dense] : 0);
+
+    // h: a thread's pieces of 8 values (rows that no token has hold anything: nobody looks at what becomes of them)
+    const int row_pieces = bytes / 8, pieces = groups * t.T * row_pieces;
+    uint4 x[kGatherPieces];
+    uint32_t most[kGatherPieces];
+#pragma unroll
+    for (int i = 0; i < kGatherPieces; ++i) {
+        const int p = tid + i * kTokenThreads;
+        if (p >= pieces) break;
+        const int row = p / row_pieces, q = row / t.T, r = row % t.T;
+        const bool d = q < dense;
+        const long long at = d ? r : (long long)(q == 0 ? g[0] : q == 1 ? g[1] : q == 2 ? g[2] : g[3]) * t.experts.a_group_stride +
+                                         min(r, (int)t.experts.a_group_stride - 1);
+        x[i] = *reinterpret_cast<const uint4*>((d ? t.dense_branch.A : t.experts.A) + at * t.experts.lda + (p % row_pieces) * 8);
+        most[i] = (d ? t.dense_branch.a_max : t.experts.a_max)[at];
+    }
+    // weights: wave w has pairs w, w + 8, ... (behind the last block: its own again, against zeros)
+    const int pairs = (nkb + 1) / 2;
+    auto load_pair = [&](const uint16_t* b, int pair) {
+        return __builtin_bit_cast(i32x4_t, load_stream16(b + (size_t)min(2 * pair + half, nkb - 1) * p_ng * 4096));
+    };
+    const uint16_t* B[kGatherGroups];
+    i32x4_t bf[kGatherGroups][kGatherAhead];
+#pragma unroll
+    for (int q = 0; q < kGatherGroups; ++q) {
+        B[q] = (q < dense ? t.dense_branch.B : t.experts.B) + (((size_t)g[q] * nkb * p_ng + ng) * 8 + frag) * 512 + (kg * 16 + col8 + (c & 7)) * 8;
+        if (q >= groups) continue;
+#pragma unroll
+        for (int s = 0; s < kGatherAhead; ++s)
+            if (s * kTokenWaves + w < pairs) bf[q][s] = load_pair(B[q], s * kTokenWaves + w);
+    }
+    // what thread (token, column) needs for its result
+    const int token = min(tid >> 3, t.T - 1), n = ng * 128 + frag + (col8 + (tid & 7)) * 8, nc = min(n, N - 1);
+    float col_scale[kGatherGroups], bias[kGatherGroups], row_scale[3], gate[2];
+    int slot[2], expert[2];
+    if (w == 0) {
+#pragma unroll
+        for (int q = 0; q < kGatherGroups; ++q) {
+            const I8GemmArgs& a = q < dense ? t.dense_branch : t.experts;
+            col_scale[q] = a.b_scale[(size_t)g[q] * N + nc];
+            bias[q] = a.bias ? bf16_to_f32(a.bias[(size_t)g[q] * N + nc]) : 0.f;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int at = token * t.top_k + min(j, t.top_k - 1);
+            slot[j] = j < t.top_k ? t.slot_idx[at] : -1;
+            expert[j] = t.expert_idx[at];
+            gate[j] = t.gate_w[at];
+            row_scale[j] = i8_scale(t.experts.a_max[(long long)expert[j] * t.experts.a_group_stride + max(slot[j], 0)]);
+        }
+        row_scale[2] = dense ? i8_scale(t.dense_branch.a_max[token]) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < kGatherPieces; ++i) {
+        const int p = tid + i * kTokenThreads;
+        if (p >= pieces) break;
+        float f[8];
+        unpack_bias8(x[i], f);
+        const float inv = i8_inverse(most[i]);
+        uint32_t o[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = i8_code_bits(f[e], inv);
+        *reinterpret_cast<uint2*>(codes + (size_t)p * 8) = make_uint2(i8_pack4(o[0], o[1], o[2], o[3]), i8_pack4(o[4], o[5], o[6], o[7]));
+    }
+    lds_barrier();
+    i32x4_t acc[kGatherGroups];
+#pragma unroll
+    for (int q = 0; q < kGatherGroups; ++q) acc[q] = i32x4_t{0, 0, 0, 0};
+    const int a_row = min(c & 7, t.T - 1);
+    for (int first = 0; first < pairs; first += kGatherAhead * kTokenWaves) {
+#pragma unroll
+        for (int q = 0; q < kGatherGroups; ++q) {
+            if (q >= groups) continue;
+#pragma unroll
+            for (int s = 0; s < kGatherAhead; ++s) {
+                const int pair = first + s * kTokenWaves + w, next = pair + kGatherAhead * kTokenWaves, kb = 2 * pair + half;
+                if (pair >= pairs) continue;
+                i32x4_t a = *reinterpret_cast<const i32x4_t*>(codes + (size_t)(q * t.T + a_row) * bytes + min(kb, nkb - 1) * 64 + kg * 16);
+                if (kb >= nkb) a = i32x4_t{0, 0, 0, 0};
+                acc[q] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, bf[q][s], acc[q], 0, 0, 0);
+                if (next < pairs) bf[q][s] = load_pair(B[q], next);
+            }
+        }
+    }
+    if (kg == half * 2)                                          // D: rows 4 (lane / 16) + r, column lane % 16
+#pragma unroll
+        for (int q = 0; q < kGatherGroups; ++q)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) part[w][q][r][c] = acc[q][r];
+    lds_barrier();
+    if (tid >= t.T * 8 || n >= N) return;                       // (within wave 0)
+    auto result = [&](int q, int r, float scale) {
+        int sum = 0;
+#pragma unroll
+        for (int s = 0; s < kTokenWaves; ++s) sum += part[s][q][r][tid & 7] + part[s][q][r][8 + (tid & 7)];
+        const float cs = q == 0 ? col_scale[0] : q == 1 ? col_scale[1] : q == 2 ? col_scale[2] : col_scale[3];
+        return i8_value(sum, scale * cs, q == 0 ? bias[0] : q == 1 ? bias[1] : q == 2 ? bias[2] : bias[3]);
+    };
+    float v = dense ? result(0, token, row_scale[2]) : 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        if (slot[j] < 0) continue;
+        int q = dense;
+#pragma unroll
+        for (int i = 0; i < kGatherGroups; ++i)
+            if (i >= dense && i < groups && g[i] == expert[j]) q = i;
+        v = fmaf(gate[j], result(q, slot[j], row_scale[j]), v);
+    }
+    t.out[(size_t)token * N + n] = f32_to_bf16(v);
+}
+// Where h's rows are a thread's pieces, and a work-group's weights no more than 128 KB (a compute unit takes in 33 GB/s of them).  us with / without the
+// hand-over, T / groups / K / N: 1 / 1 / 4096 / 1024 10.3 / 5.5; 1 / 3 / 4096 / 1024 11.2 / 8.6; 1 / 2 / 1024 / 4096 13.2 / 6.6; 1 / 1 and 1 / 2 and
+// 1 / 3 / 8192 / 2048 16.2 / 8.5, 17.2 / 12.9, 16.2 / 17.6; 2 / 3 and 2 / 4 / 4096 / 1024 11.1 / 9.6, 11.6 / 11.2; 4 / 4 / 2048 / 512 8.4 / 8.7.
+bool gather_faster(const I8TokenArgs& t) {
+    const long long groups = t.experts.slots + (t.dense ? 1 : 0), bytes = groups * t.experts.K * 2;
+    return t.T <= 4 && groups <= kGatherGroups && bytes <= 16384 && bytes * t.T <= kGatherBytes;
+}
+
 template <int MSMAX> long long token_groups(const I8TokenArgs& t) { return t.experts.slots + (t.dense ? (t.T + 16 * MSMAX - 1) / (16 * MSMAX) : 0); }
 
 template <int MSMAX, int NF> int launch_token(const I8TokenArgs& t, bool second, hipStream_t s) {
@@ -133,6 +267,10 @@ template <int MSMAX, int NF> int launch_token(const I8TokenArgs& t, bool second,
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s) {
     const I8GemmArgs& a = t.experts;
     if (!t.order || a.slots < 1 || a.slots > t.E || a.max_rows > kI8FewRows || a.K % 32 || a.N % 8 || t.top_k > 2) return MOE_ERR_INVALID_ARG;
+    if (second && gather_faster(t)) {
+        hipLaunchKernelGGL(i8_token_gather_kernel, dim3((unsigned)(few_tiles<1>(a.N) * 2)), dim3(kTokenThreads), 0, s, t);
+        return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+    }
     const int most = t.dense && t.T > a.max_rows ? std::min(t.T, kI8FewRows) : a.max_rows;
     const int nf = few_columns(most <= 16 ? token_groups<1>(t) : token_groups<2>(t), most, a.N);
     if (most > 16) return nf == 1 ? launch_token<2, 1>(t, second, s) : launch_token<2, 2>(t, second, s);

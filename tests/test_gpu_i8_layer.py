@@ -218,6 +218,14 @@ def test_every_number_of_tokens(T):
     Layer(T, 64, 136, 4, k=1 + T % 2, C=T, residual=T % 3 == 0, seed=T).check()
 
 
+@pytest.mark.parametrize("T,k,residual", [(T, k, r) for T in (1, 2, 3, 4, 5) for k in (1, 2) for r in (False, True)])
+@pytest.mark.parametrize("d,f,E,C", [(64, 8, 4, 1), (200, 136, 3, 2), (1000, 520, 9, 4), (72, 4104, 2, 4), (136, 5448, 5, 1), (1024, 4096, 128, 4),
+                                     (1032, 8200, 3, 2), (64, 16384, 2, 1)])
+def test_fewest_tokens(T, k, residual, d, f, E, C):
+    """With and without a hand-over between the work-groups; odd numbers of blocks, single columns of a tile, dropped tokens."""
+    Layer(T, d, f, E, k, C, residual, seed=T + f).check()
+
+
 @pytest.mark.parametrize("name", ["step", "step_residual_top2", "tiles_residual"])
 def test_layer_twice_is_the_same(name):
     L = Layer(**LAYERS[name], seed=2)
