@@ -1503,6 +1503,7 @@ I8Ffn i8_ffn(const moe_shape_t* s, bool few, int G, int max_rows, int group_rows
 
 int i8_product(const I8GemmArgs& a, const I8GemmArgs* b, bool few, int epi, hipStream_t st) {
     if (few && b) return MOE_ERR_INVALID_ARG;
+    if (!b && i8_few_faster_alone(a, epi)) few = true;
     return few ? launch_i8_few(a, epi, st) : i8_wide_faster(a, b) ? launch_i8_wide(a, b, epi, st) : launch_i8_tile(a, b, epi, st);
 }
 
@@ -1566,7 +1567,7 @@ int moe_i8_linear(const moe_i8_linear_t* product, const int8_t* codes, int64_t c
     a.A = reinterpret_cast<const uint16_t*>(codes); a.lda = codes_stride / 2; a.a_scale = row_scale; a.B = u16(W); a.b_scale = col_scale;
     a.bias = u16(bias); a.packed = 1; a.fixed_rows = a.max_rows = p->n_rows; a.G = 1; a.K = i8_row_bytes(p->K) / 2; a.N = p->N;
     a.out = u16(out); a.ldo = out_stride; a.out32 = p->out_dtype == MOE_F32; a.ksplit = 1;
-    return i8_product(a, nullptr, i8_few_faster_alone(p->n_rows, p->N), p->gelu ? EPI_GELU : EPI_STORE, static_cast<hipStream_t>(stream));
+    return i8_product(a, nullptr, false, p->gelu ? EPI_GELU : EPI_STORE, static_cast<hipStream_t>(stream));
 }
 
 size_t moe_i8_workspace_bytes(const moe_shape_t* shape) { return check_i8_shape(shape) == MOE_OK ? i8_layout(shape).total : 0; }

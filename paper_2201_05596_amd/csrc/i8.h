@@ -69,12 +69,12 @@ int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s);
 // ceil(N / 128)
 int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipStream_t s);
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s);
-// (i8_few.hip) few rows, bound by the read of the weights; no order, no row map
+// (i8_few.hip) few rows, bound by the read of the weights; `order` is not looked at
 int launch_i8_few(const I8GemmArgs& a, int epi, hipStream_t s);
 constexpr int kI8FewRows = 32;                                   // of a group, where a product makes codes from bf16
 int few_columns(long long groups, int max_rows, int N);          // 16-column fragments of a work-group
 bool i8_few_faster(int groups, int max_rows, int d, int f);      // for both products of FFNs
-bool i8_few_faster_alone(int rows, int N);                       // for one product
+bool i8_few_faster_alone(const I8GemmArgs& a, int epi);          // for one product of codes
 // (i8_token.hip) both products and the combine of a layer whose experts have few rows: the first (with h's largest magnitudes) or the second ones
 // (in 32 bits, into ye and the dense branch's rows, then combined into out)
 struct I8TokenArgs {

@@ -71,12 +71,13 @@ template <int EPI, bool BF16> int launch_few_columns(const I8GemmArgs& a, int NF
 
 // Columns of a work-group: the most that leave enough of them; 128 columns read the rows least often.  us per product: 64 experts of up
 // to 16 rows, 2048 x 8192, with 16 / 32 / 64 / 128 columns 267 / 210 / 178 / 166; one row, 2048 x 6144, 5.9 / 4.2 / 6.4 with 16 / 32 / 64
-// (384, 192, 96 work-groups).
+// (384, 192, 96 work-groups).  More than 32 rows: one work-group for each compute unit, with 16 columns if that is enough.
 long long few_blocks(long long groups, int max_rows, int N, int nf) {
     return groups * (max_rows <= 32 ? 1 : (max_rows + 63) / 64) * ((N + 16 * nf - 1) / (16 * nf));
 }
 int few_columns(long long groups, int max_rows, int N) {
     if (max_rows <= 16 && few_blocks(groups, max_rows, N, 8) >= 512) return 8;
+    if (max_rows > 32) return few_blocks(groups, max_rows, N, 1) > 256 ? 2 : 1;
     for (int nf = max_rows <= 16 ? 4 : 2; nf > 1; nf /= 2)
         if (few_blocks(groups, max_rows, N, nf) >= 160) return nf;
     return 1;
@@ -86,12 +87,17 @@ int few_columns(long long groups, int max_rows, int N) {
 // how many tiles of 256 columns the product with fewer columns has; with 256 of them a tile for each compute unit (64 experts of up to 16 rows, 1024 /
 // 4096: 48 + 56 us here, 44 + 4 + 41 there; 50 experts of a decode step, 2048 / 8192: 138 + 142 and 128 + 4 + 128).
 bool i8_few_faster(int groups, int max_rows, int d, int f) { return max_rows <= kI8FewRows && (long long)groups * (((d < f ? d : f) + 255) / 256) < 192; }
-// One product of codes: 2048 x 6144 with 32 / 64 / 128 rows 7.2 / 9.6 / 15.1 us here, 64 / 128 rows in tiles 12.0 / 12.2.
-bool i8_few_faster_alone(int rows, int N) { return rows <= 64 && N < 192 * 256; }
+// One product of codes, where one work-group of 64 rows x 32 columns for each compute unit is enough: they share K among their waves, which tiles of 256
+// columns do not.  us here / in tiles, N = 2048: 256 rows with K = 512 / 2048 / 8192 5.8 / 5.8, 8.6 / 12.2, 23.6 / 37.3, 384 rows (384 work-groups) 9.3 / 5.8,
+// 15.1 / 12.4, 44 / 38.  Up to 64 rows the weights are read once: 2048 x 6144 with 32 / 64 rows 7.2 / 9.6, in tiles 12.0.
+bool i8_few_faster_alone(const I8GemmArgs& a, int epi) {
+    if (epi == EPI_SCATTER) return false;
+    return few_blocks(a.G, a.max_rows, a.N, 2) <= 256 || (a.G == 1 && a.max_rows <= 64 && a.N < 192 * 256);
+}
 
 int launch_i8_few(const I8GemmArgs& a, int epi, hipStream_t s) {
     if (a.G <= 0 || a.max_rows <= 0) return MOE_OK;
-    if (a.K % 32 || a.N % 8 || a.order) return MOE_ERR_INVALID_ARG;
+    if (a.K % 32 || a.N % 8) return MOE_ERR_INVALID_ARG;
     const bool bf16 = a.a_max != nullptr;
     const int NF = few_columns(a.G, a.max_rows, a.N);
     switch (epi) {

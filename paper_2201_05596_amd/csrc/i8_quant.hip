@@ -270,15 +270,19 @@ int launch_i8_rows(const I8RowsArgs& a, int dtype, hipStream_t s) {
 }
 
 int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipStream_t s) {
+    if (K <= 128) return launch_weights_k<false, 0, 128, 32, false>(codes, packed, nullptr, G, K, N, s);
     return launch_weights_k<false, 0, 512, 32, false>(codes, packed, nullptr, G, K, N, s);
 }
 
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s) {
     if ((long long)G * K * N > (32ll << 20)) {
+        if (K <= 128) return launch_weights_k<true, 1, 256, 64, true>(W, packed, scale, G, K, N, s);
         if (K <= 1024) return launch_weights_k<true, 4, 512, 64, true>(W, packed, scale, G, K, N, s);
         if (K <= 2048) return launch_weights_k<true, 8, 512, 64, true>(W, packed, scale, G, K, N, s);
         return launch_weights_k<true, 0, 1024, 64, true>(W, packed, scale, G, K, N, s);
     }
+    if (K <= 64) return launch_weights_k<true, 1, 64, 32, false>(W, packed, scale, G, K, N, s);
+    if (K <= 256) return launch_weights_k<true, 1, 256, 32, false>(W, packed, scale, G, K, N, s);
     if (K <= 1024) return launch_weights_k<true, 2, 512, 32, false>(W, packed, scale, G, K, N, s);
     if (K <= 4096) return launch_weights_k<true, 8, 512, 32, false>(W, packed, scale, G, K, N, s);
     return launch_weights_k<true, 0, 1024, 32, false>(W, packed, scale, G, K, N, s);
