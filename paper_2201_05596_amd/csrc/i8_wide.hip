@@ -7,19 +7,26 @@ template <int EPI> static int launch_i8_epi(const I8GemmArgs& a, const I8GemmArg
     return a.K % kChunk ? launch_wide_r<256, EPI, true>(a, b, policy, s) : launch_wide_r<256, EPI, false>(a, b, policy, s);
 }
 
-// Against tiles of 128 rows with three work-groups per compute unit (i8_tile.hip), which hide a tile's epilogue and stores and deal finer
-// pieces, but load half as many bytes more per product.  us here / there: 16384 rows, N = 4096, K = 512 / 1024 / 2048 / 4096 / 8192: 69 / 53, 92 / 77,
-// 134 / 127, 230 / 242, 435 / 516; with one tile for each compute unit (4096 rows) 19 / 18, 24 / 24, 34 / 37, 55 / 65, 99 / 123; fewer than 160
-// tiles of 256 rows leave compute units idle (4096 rows, N = 1024, K = 1024: 17.4 / 10.6; 1024 rows, N = 2048, K = 4096: 42 / 26); 64 experts of up to 200
-// rows, 1024 x 4096 and back 78 + 64 / 91 + 90; of up to 128 rows the same; 16 of up to 512 rows, 2048 x 8192: 139 / 149; of groups with more rows, whose
-// weights many row tiles share: 8 experts of up to 1024 rows, 2048 x 8192: 117 / 98; a dense branch of 8192 tokens with 32 experts of up to 320 rows,
-// 1024 x 4096: 134 / 101, back 95 / 97.
+// Against tiles of 128 rows with three work-groups per compute unit (i8_tile.hip), which hide a tile's epilogue and stores and deal finer pieces, but load
+// half as many bytes more per product.  What either takes in us, from products of 1536 to 32768 rows, N = 2048 to 8192, k = 512 to 16384 bytes: a round
+// of 256 tiles here 7.5 + k / 102, there 1.9 + k / 165 (of groups 2.2 + k / 161) with 4 once, and alone on the chip 6 + k / 98.  Here / there, N = 4096: 16384 rows with k = 512 / 1024 /
+// 2048 / 4096 53 / 43, 73 / 67, 116 / 122, 208 / 235; 8192 rows 28 / 26, 39 / 37, 61 / 66, 106 / 124; 4608 rows, 288 tiles, 25 / 17, 35 / 26, 54 / 45, 91 / 83;
+// 2560 rows 14 / 14, 20 / 20, 30 / 32, 51 / 56.  Fewer tiles leave compute units idle that tiles of 64 rows reach (4096 rows, N = 1024, k = 2048: 17 / 11).
+// Rows of groups, by their room: 32 experts of up to 256 rows, 2048 / 8192 260 / 332 for both products, 16 of up to 512 246 / 301, 64 of up to 200 rows,
+// 1024 / 4096 155 / 198; 24 of up to 400 rows, 1024 / 2048 78 / 73, as said here 68; a dense branch of 8192 tokens with 32 experts of up to 320 rows, 1024 / 4096, the layer 293 / 262.  With a
+// short k and 1024 rows of room or more, much of it empty, finer pieces are better (8 experts, 2048 / 8192: 117 / 97 for the first product).
 bool i8_wide_faster(const I8GemmArgs& a, const I8GemmArgs* b) {
-    auto tiles = [](const I8GemmArgs& x) { return (long long)few_groups(x) * ((x.max_rows + 255) / 256) * ((x.N + kWideCols - 1) / kWideCols); };
+    auto tiles = [&](int rows) {
+        auto of = [&](const I8GemmArgs& x) { return (long long)few_groups(x) * ((x.max_rows + rows - 1) / rows); };
+        return (of(a) + (b ? of(*b) : 0)) * ((a.N + kWideCols - 1) / kWideCols);
+    };
     const int most = b && b->max_rows > a.max_rows ? b->max_rows : a.max_rows;
-    if (most <= 128 || tiles(a) + (b ? tiles(*b) : 0) < 160) return false;
-    auto high = [&](const I8GemmArgs& x) { return x.max_rows >= 1024 ? tiles(x) : 0; };
-    return !(a.K <= 1024 && high(a) + (b ? high(*b) : 0) >= 512);        // (pairs of codes)
+    const long long wide = tiles(256), rounds = (tiles(128) + 255) / 256;
+    const double k = 2.0 * a.K;
+    if (most <= 128 || wide < (k >= 4096 ? 112 : 160)) return false;
+    if (a.G > 1 && !b && a.max_rows >= 1024 && k <= 2048 && wide >= 512) return false;
+    const double there = a.G == 1 && !b ? 1.9 + k / 165 : 2.2 + k / 161;
+    return ((wide + 255) / 256) * (7.5 + k / 102) <= (rounds == 1 ? 6 + k / 98 : 4 + rounds * there);
 }
 
 int launch_i8_wide(const I8GemmArgs& first, const I8GemmArgs* second, int epi, hipStream_t s) {
