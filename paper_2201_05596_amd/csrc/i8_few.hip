@@ -63,7 +63,7 @@ template <int EPI, bool BF16> int launch_few_columns(const I8GemmArgs& a, int NF
         case 1: return launch_few_rows<1, EPI, BF16>(a, s);
         case 2: return launch_few_rows<2, EPI, BF16>(a, s);
         case 4: return launch_few_rows<4, EPI, BF16>(a, s);
-        default: return launch_few_rows<8, EPI, BF16>(a, s);
+        default: if constexpr (EPI == EPI_GELU) return launch_few_rows<8, EPI, BF16>(a, s); else return MOE_ERR_INVALID_ARG;
     }
 }
 
@@ -99,7 +99,8 @@ int launch_i8_few(const I8GemmArgs& a, int epi, hipStream_t s) {
     if (a.G <= 0 || a.max_rows <= 0) return MOE_OK;
     if (a.K % 32 || a.N % 8) return MOE_ERR_INVALID_ARG;
     const bool bf16 = a.a_max != nullptr;
-    const int NF = few_columns(a.G, a.max_rows, a.N);
+    // (128 columns: first products of FFNs alone have as many work-groups where they come here at all)
+    const int NF = std::min(few_columns(a.G, a.max_rows, a.N), epi == EPI_GELU ? 8 : 4);
     switch (epi) {
         case EPI_STORE: return bf16 ? launch_few_columns<EPI_STORE, true>(a, NF, s) : launch_few_columns<EPI_STORE, false>(a, NF, s);
         case EPI_GELU: return bf16 ? MOE_ERR_INVALID_ARG : launch_few_columns<EPI_GELU, false>(a, NF, s);

@@ -90,12 +90,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
 template <typename T, int TPR, int NP> int launch_rows_p(const I8RowsArgs& a, hipStream_t s) {
     constexpr int threads = TPR < 256 ? 256 : TPR, per = threads / TPR;
     constexpr int most = 1 << 21;                                // work-groups of a launch, whose threads are counted in 32 bits
+    constexpr bool can_be_big = TPR != 256 || NP > 2;             // (a work-group for each of fewer than 2048 short rows: 32 MB)
     const bool big = (long long)a.n_rows * a.cols * (long long)sizeof(T) > (64ll << 20);
     I8RowsArgs part = a;
     for (long long first = 0; first < a.n_rows; first += (long long)most * per) {
         const dim3 blocks((unsigned)std::min<long long>(most, (a.n_rows - first + per - 1) / per));
         part.first = (int)first;
-        if (big) hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, true>), blocks, dim3(threads), 0, s, part);
+        if (big && can_be_big) hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, can_be_big>), blocks, dim3(threads), 0, s, part);
         else hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, false>), blocks, dim3(threads), 0, s, part);
         part.zero = nullptr;
     }

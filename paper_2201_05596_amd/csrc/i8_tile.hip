@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kTileThreads, ROWS == 128 ? 3 : 2) void i8_tile_ker
             dma16_at<0, NT>(b);
             dma16_at<1024, NT>(b);
             dma16_at<2048, NT>(b);
-            dma16_at<3072, NT>(b);
+            dma16_at<3 * 1024, NT>(b);
         };
         i32x4_t acc[ACT][8];
 #pragma unroll

@@ -153,6 +153,26 @@ def test_ffn(E, C, d, f, bias):
         xe = torch.randn((E, C, d), generator=L.gen, device=DEV).to(torch.bfloat16)
 
 
+@pytest.mark.parametrize("E,C,d,f", [
+    # few rows: 16 to 128 columns of a work-group, K of few blocks and more; 17 rows and more
+    (50, 10, 256, 64), (50, 10, 256, 2000), (30, 10, 200, 64), (30, 10, 200, 2000), (5, 10, 200, 64), (5, 10, 200, 2000), (40, 9, 1024, 2048), (37, 9, 1032, 2048),
+    (64, 16, 1024, 64), (30, 20, 200, 264), (5, 20, 200, 2000),
+    # tiles, with weights in the caches and past them; one row tile and several
+    (41, 100, 1024, 64), (41, 100, 1024, 4104), (41, 50, 1024, 4104), (41, 20, 1024, 4104), (41, 20, 1600, 4104),
+    # tiles of 256 rows
+    (8, 1100, 1024, 64), (8, 1100, 1024, 136), (33, 200, 1024, 4104), (33, 200, 1024, 4224), (17, 300, 1024, 8200), (17, 300, 1024, 8192)])
+def test_ffn_on_every_kernel(E, C, d, f):
+    L = Layer(E * C, d, f, E, C=C, seed=E + C)
+    xe = torch.randn((E, C, d), generator=L.gen, device=DEV).to(torch.bfloat16)
+    counts = [C if e == 0 else (37 * e + 5) % (C + 1) for e in range(E)]
+    rows = torch.tensor(counts, dtype=torch.int32, device=DEV)
+    ye = torch.full((E, C, d), CANARY, dtype=torch.bfloat16, device=DEV)
+    L.ffn(xe, rows, ye)
+    for e, n in enumerate(counts):
+        assert (ye[e, n:] == CANARY).all()
+        assert n == 0 or torch.equal(ye[e, :n], L.expert(xe[e, :n].contiguous(), e)), e
+
+
 def test_ffn_bits_do_not_depend_on_room():
     """The same rows in experts with room for 3, 16, 17, 33, 100, 300: other kernels, the same bits."""
     got = []
@@ -211,6 +231,14 @@ def test_layer(name):
 @pytest.mark.parametrize("name", ["one_token_residual", "step", "step_drops", "step_residual_top2", "mixed", "tiles_drops", "tiles_residual_top2", "prefill"])
 def test_layer_against_the_oracle(name):
     Layer(**LAYERS[name], seed=5).check_oracle()
+
+
+@pytest.mark.parametrize("T,E,C,d,f", [(900, 41, 100, 1024, 64), (3000, 41, 100, 1024, 4104), (1500, 41, 50, 1024, 4104), (600, 41, 20, 1024, 4104), (7000, 8, 1100, 1024, 64),
+                                       (7000, 8, 1100, 1024, 128), (4000, 33, 200, 1024, 4104), (4000, 33, 200, 1024, 4224), (4000, 17, 300, 1024, 8200),
+                                       (4000, 17, 300, 1024, 8192)])
+def test_combine_in_every_tile(T, E, C, d, f):
+    """Top-1 layers, whose second products' tiles put the tokens back: tiles of 32, 64, 128 and 256 rows, weights in the caches and past them."""
+    Layer(T, d, f, E, 1, C, seed=T + f, skew=0.3).check()
 
 
 @pytest.mark.parametrize("T", list(range(1, 20)) + [31, 32, 33, 63, 64, 65, 255, 256, 257])

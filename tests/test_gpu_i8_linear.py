@@ -88,6 +88,33 @@ def test_largest_sums(R):
     assert (got[0, :2] == (np.array([131072 * 127 * 127, -131072 * 127 * 128], np.int64).astype(np.float32) * (p.sr[0] * p.sc[:2]))).all()
 
 
+# few rows, by the columns of a work-group and the waves of it; tiles of 256 rows on a K of whole and half chunks
+@pytest.mark.parametrize("R,K,N", [(R, K, N) for R in (1, 5, 16, 17, 32) for K in (200, 1160) for N in (520, 5128, 10248)] + [(40, 200, 5000), (64, 2056, 4104)] +
+                         [(R, K, N) for R, N in ((2600, 4104), (5000, 2048), (3585, 3080)) for K in (64, 128, 192, 1000)])
+def test_many_columns(R, K, N):
+    p = Product(R, K, N, seed=R + K + N, bias=N % 16 != 0)
+    p.check("bf16")
+    p.check("f32", gelu=True, out_cols=8)
+
+
+@pytest.mark.parametrize("R,K,N", [(200, 4104, 32776), (256, 4224, 32776), (1700, 32776, 4104), (1793, 32768, 4104)])
+def test_weights_past_the_caches(R, K, N):
+    """128 MB of weights and more, read by one row tile and by several; products of integers in 64 bits are exact."""
+    m, g = U.amd(), torch.Generator(device=DEV).manual_seed(R)
+    codes = torch.randint(-127, 128, (R, up(K, 64)), generator=g, device=DEV, dtype=torch.int8)
+    w = torch.randint(-127, 128, (K, N), generator=g, device=DEV, dtype=torch.int8)
+    sr, sc = torch.rand(R, generator=g, device=DEV) + 0.5, (torch.rand(N, generator=g, device=DEV) + 0.5) * (1e-4 * K ** -0.5)
+    acc = torch.cat([codes[:, :K].double() @ w[:, n:n + 4096].double() for n in range(0, N, 4096)], 1)
+    packed = m.moe_i8_pack_weights(w)
+    out = torch.empty((R, N), device=DEV)
+    m.moe_i8_linear(m.make_i8_linear(R, K, N, "f32"), codes, sr, packed, sc, None, out)
+    assert torch.equal(out, acc.float() * (sr[:, None] * sc))
+    exact = out.double()
+    m.moe_i8_linear(m.make_i8_linear(R, K, N, "f32", True), codes, sr, packed, sc, None, out)
+    want = 0.5 * exact * (1 + torch.tanh(0.7978845608028654 * (exact + 0.044715 * exact ** 3)))
+    assert ((out.double() - want).abs() <= 1.13 * 2.0 ** -24 * exact.abs() + 2.0 ** -17 * want.abs() + 1e-9).all()
+
+
 def test_every_number_of_rows_gives_the_same_bits():
     """Tiles, splits and kernels change with the number of rows; integer sums do not."""
     p = Product(700, 776, 264, bias=True)

@@ -86,6 +86,14 @@ def test_rows_behind_4_gib():
     assert (codes.cpu().numpy() == want).all() and (scale.cpu().numpy() == s).all()
 
 
+@pytest.mark.parametrize("dtype,rows,cols", [("bf16", 70000, 512), ("bf16", 40000, 1000), ("bf16", 17000, 2048), ("bf16", 4100, 8192), ("bf16", 1100, 32768),
+                                             ("bf16", 300, 131072), ("f32", 35000, 504), ("f32", 17000, 1024), ("f32", 9000, 2040), ("f32", 5000, 4096),
+                                             ("f32", 2500, 8192), ("f32", 1500, 16384), ("f32", 600, 32768), ("f32", 150, 131072)])
+def test_large_ones(dtype, rows, cols):
+    """Past the caches: 64 MB and more."""
+    check_rows(spread(rows, cols, rows, dtype))
+
+
 def test_more_rows_than_a_launch_has():
     """Launches of 2^21 work-groups, four rows each."""
     n = (1 << 23) + 5
