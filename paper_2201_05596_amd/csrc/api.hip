@@ -1587,9 +1587,11 @@ int moe_i8_expert_ffn(const moe_shape_t* shape, const moe_i8_weights_t* weights,
     float* x_scale = at<float>(ws, L.x_scale);
     I8Ffn p = i8_ffn(shape, i8_few_faster(E, C, d, shape->d_ffn), E, C, C, expert_rows, x, x_scale, weights->W1, weights->s1, weights->b1, weights->W2, weights->s2, weights->b2,
                      at<uint16_t>(ws, L.h), at<uint32_t>(ws, L.words), at<int8_t>(ws, L.hq), at<float>(ws, L.h_scale));
-    // few experts of unknown sizes: each XCD a part of every one (8 experts of up to 1024 rows, 2048 / 8192: 134 + 90 -> 119 + 86 us; 32 of up to 256
-    // 128 + 106 -> 128 + 134)
-    if (E < 16) p.first.spread = p.second.spread = 1;
+    // Experts of unknown sizes: each XCD a part of every one, where there are few (8 experts of up to 1024 rows, 2048 / 8192: 134 + 90 -> 119 + 86 us; 32 of up
+    // to 256 128 + 106 -> 128 + 134), and for the first products, whose rows are short, where they have room for several row tiles (20 of up to 400,
+    // 2048 -> 4096: 109 -> 88, 16 of up to 512, 2048 -> 8192: 137 -> 129, 32 of up to 512, 1024 -> 4096: 83 -> 85)
+    if (E < 16 || C > 256) p.first.spread = 1;
+    if (E < 16) p.second.spread = 1;
     rc = launch_i8_rows(I8RowsArgs{xe, d, i8_row_bytes(d), x, x_scale, expert_rows, C, E * C, E * C, d, p.few ? at<uint32_t>(ws, L.words) : nullptr, (long long)E * C, 0},
                         MOE_BF16, st);
     if (rc != MOE_OK) return rc;
