@@ -1451,7 +1451,6 @@ struct I8Layout {
     WsLayout gate;
     size_t x, x_scale, h, hq, h_scale, ye, dense, words, total;     // h and its codes: the experts' rows [E * C], then the dense branch's [T]
 };
-constexpr int kI8TokenRows = 256;             // tokens of a layer whose experts may have few rows each, at most
 I8Layout i8_layout(const moe_shape_t* s) {
     I8Layout L{};
     const size_t T = s->T, d = s->d_model, E = s->E, C = s->capacity, rows = std::max(T, E * C);
@@ -1627,7 +1626,7 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
 
     // an expert has at most one row of a token
     const int max_rows = std::min(C, T), touched = (int)std::min<long long>((long long)T * k, E);
-    const bool few = T <= kI8TokenRows && i8_few_faster(touched, max_rows, d, shape->d_ffn), dense = shape->residual;
+    const bool dense = shape->residual, few = i8_token_faster(T, touched, max_rows, d, shape->d_ffn, dense);
     uint32_t* words = at<uint32_t>(ws, L.words);
     const int n_maxes = E * max_rows + (dense ? T : 0), n_words = n_maxes + i8_token_tiles(d);
     // few tokens: the gate's one launch finds the rows' largest magnitudes and clears the words

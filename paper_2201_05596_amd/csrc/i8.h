@@ -71,7 +71,7 @@ int launch_i8_pack(const int8_t* codes, void* packed, int G, int K, int N, hipSt
 int launch_i8_weights(const uint16_t* W, void* packed, float* scale, int G, int K, int N, hipStream_t s);
 // (i8_few.hip) few rows, bound by the read of the weights; `order` is not looked at
 int launch_i8_few(const I8GemmArgs& a, int epi, hipStream_t s);
-constexpr int kI8FewRows = 32;                                   // of a group, where a product makes codes from bf16
+constexpr int kI8FewRows = 16;                                   // of a group, where a product makes codes from bf16
 int few_columns(long long groups, int max_rows, int N);          // 16-column fragments of a work-group
 bool i8_few_faster(int groups, int max_rows, int d, int f);      // for both products of FFNs
 bool i8_few_faster_alone(const I8GemmArgs& a, int epi);          // for one product of codes
@@ -88,6 +88,8 @@ struct I8TokenArgs {
 };
 inline int i8_token_tiles(int N) { return (N + 127) / 128 * 8; } // column tiles of a second product, at most
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s);
+constexpr int kI8TokenRows = 64;                                 // tokens of such a layer, at most
+bool i8_token_faster(int T, int touched, int max_rows, int d, int f, bool dense);
 // (i8_tile.hip) tiles of up to 128 rows, two or three work-groups per compute unit
 int launch_i8_tile(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);
 // (i8_wide.hip) tiles of 256 rows

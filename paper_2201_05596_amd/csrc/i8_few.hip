@@ -53,8 +53,7 @@ template <int NF, int EPI, bool BF16> int launch_few_rows(const I8GemmArgs& a, h
         return a.K <= 512 ? launch_few<4, 1, NF, EPI, BF16>(a, s) : launch_few<8, 1, NF, EPI, BF16>(a, s);
     }
     if constexpr (NF <= 2) {                                     // (with 64 columns more registers than there are)
-        if (a.max_rows <= 32) return launch_few<8, 2, NF, EPI, BF16>(a, s);
-        if constexpr (!BF16) return launch_few<8, 4, NF, EPI, false>(a, s);
+        if constexpr (!BF16) return a.max_rows <= 32 ? launch_few<8, 2, NF, EPI, false>(a, s) : launch_few<8, 4, NF, EPI, false>(a, s);
     }
     return MOE_ERR_INVALID_ARG;
 }
@@ -83,7 +82,8 @@ int few_columns(long long groups, int max_rows, int N) {
     return 1;
 }
 
-// Up to 32 rows a group, against tiles of 32 rows with h brought into codes by a launch between the products (4.4 us).  What decides is
+// Up to 16 rows a group, against tiles of 32 rows with h brought into codes by a launch between the products (4.4 us).  (With more rows a wave
+// makes codes of two sub-tiles for each block, and takes longer: 16 experts of up to 17 / 32 rows, 1024 / 4096 57 / 67 us, that way 53 / 54.)  What decides is
 // how many tiles of 256 columns the product with fewer columns has; with 256 of them a tile for each compute unit (64 experts of up to 16 rows, 1024 /
 // 4096: 48 + 56 us here, 44 + 4 + 41 there; 50 experts of a decode step, 2048 / 8192: 138 + 142 and 128 + 4 + 128).
 bool i8_few_faster(int groups, int max_rows, int d, int f) { return max_rows <= kI8FewRows && (long long)groups * (((d < f ? d : f) + 255) / 256) < 192; }

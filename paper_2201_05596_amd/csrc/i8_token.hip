@@ -9,7 +9,7 @@
 // gate's launch.
 // One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 8.6 us behind a gate of 9.2, with a hand-over 6.7 + 11.2; as launches that
 // bring x into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1.  16 tokens, top-2 of 64 experts beside one: 33 + 32 us
-// (212 MB of codes: 3.2 TB/s).  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
+// (27 groups with rows, 113 MB of codes each: 3.4 TB/s).  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
 // a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across the L2s).
 #include "i8_few.h"
 
@@ -19,13 +19,13 @@ namespace {
 
 constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * 64;
 
-// a work-group's tile: columns fastest; the dense branch's row tiles come first, then the experts with rows in the gate's order
+// a work-group's tile: columns fastest; the dense branch comes first, then the experts with rows in the gate's order
 struct TokenTile {
-    int g, nt, m0, groups;
+    int g, nt, groups;
     bool dense, live;
 };
-template <int MSMAX> __device__ __forceinline__ TokenTile token_tile(const I8TokenArgs& t, int n_tiles) {
-    const int group = blockIdx.x / n_tiles, dense = t.dense ? (t.T + 16 * MSMAX - 1) / (16 * MSMAX) : 0;
+__device__ __forceinline__ TokenTile token_tile(const I8TokenArgs& t, int n_tiles) {
+    const int group = blockIdx.x / n_tiles, dense = t.dense ? 1 : 0;
     TokenTile r;
     r.nt = blockIdx.x % n_tiles;
     r.dense = group < dense;
@@ -34,18 +34,17 @@ template <int MSMAX> __device__ __forceinline__ TokenTile token_tile(const I8Tok
     r.groups = __builtin_amdgcn_readfirstlane(dense + live);
     r.live = group < r.groups;
     r.g = __builtin_amdgcn_readfirstlane(expert);
-    r.m0 = r.dense ? group * 16 * MSMAX : 0;
     return r;
 }
 
 // XBF16: x in bf16 with the tokens' largest magnitudes, else codes with scales
-template <int MSMAX, int NF, bool XBF16>
+template <int NF, bool XBF16>
 __global__ __launch_bounds__(kTokenThreads) void i8_token_first_kernel(const I8TokenArgs t) {
-    __shared__ __attribute__((aligned(16))) int part[few_lds_ints<kTokenWaves, MSMAX, NF>()];
-    const TokenTile tile = token_tile<MSMAX>(t, few_tiles<NF>(t.experts.N));
+    __shared__ __attribute__((aligned(16))) int part[few_lds_ints<kTokenWaves, 1, NF>()];
+    const TokenTile tile = token_tile(t, few_tiles<NF>(t.experts.N));
     if (!tile.live) return;
     const I8GemmArgs& a = tile.dense ? t.dense_branch : t.experts;
-    few_tile<kTokenWaves, MSMAX, NF, XBF16>(a, tile.g, tile.nt, tile.m0, part, [&](int row, int n, bool here, float (&v)[NF]) {
+    few_tile<kTokenWaves, 1, NF, XBF16>(a, tile.g, tile.nt, 0, part, [&](int row, int n, bool here, float (&v)[NF]) {
         uint32_t most = 0;
         const long long r = (long long)tile.g * a.o_group_stride + row;
         if (here) {
@@ -60,12 +59,12 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_first_kernel(const I8T
     });
 }
 
-template <int MSMAX, int NF>
+template <int NF>
 __global__ __launch_bounds__(kTokenThreads) void i8_token_second_kernel(const I8TokenArgs t) {
-    __shared__ __attribute__((aligned(16))) int part[few_lds_ints<kTokenWaves, MSMAX, NF>()];
+    __shared__ __attribute__((aligned(16))) int part[few_lds_ints<kTokenWaves, 1, NF>()];
     __shared__ int shared_last;
     const int tid = threadIdx.x, N = t.experts.N;
-    const TokenTile tile = token_tile<MSMAX>(t, few_tiles<NF>(N));
+    const TokenTile tile = token_tile(t, few_tiles<NF>(N));
     if (!tile.live) return;
     // where the results of token tid / 16 will be, in case that this is the last work-group
     struct Source { int slot, expert; float gate; };
@@ -80,7 +79,7 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_second_kernel(const I8
     };
     look_up(tid >> 4);
     const I8GemmArgs& a = tile.dense ? t.dense_branch : t.experts;
-    few_tile<kTokenWaves, MSMAX, NF, true>(a, tile.g, tile.nt, tile.m0, part, [&](int row, int n, bool here, float (&v)[NF]) {
+    few_tile<kTokenWaves, 1, NF, true>(a, tile.g, tile.nt, 0, part, [&](int row, int n, bool here, float (&v)[NF]) {
         if (!here) return;
         float* o = reinterpret_cast<float*>(a.out) + ((long long)tile.g * a.o_group_stride + row) * N + n;
 #pragma unroll
@@ -250,31 +249,38 @@ bool gather_faster(const I8TokenArgs& t) {
     return t.T <= 4 && groups <= kGatherGroups && bytes <= 16384 && bytes * t.T <= kGatherBytes;
 }
 
-template <int MSMAX> long long token_groups(const I8TokenArgs& t) { return t.experts.slots + (t.dense ? (t.T + 16 * MSMAX - 1) / (16 * MSMAX) : 0); }
+long long token_groups(const I8TokenArgs& t) { return t.experts.slots + (t.dense ? 1 : 0); }
 
-template <int MSMAX, int NF> int launch_token(const I8TokenArgs& t, bool second, hipStream_t s) {
-    const long long blocks = token_groups<MSMAX>(t) * few_tiles<NF>(t.experts.N);
+template <int NF> int launch_token(const I8TokenArgs& t, bool second, hipStream_t s) {
+    const long long blocks = token_groups(t) * few_tiles<NF>(t.experts.N);
     if (blocks >= (1ll << 32) / kTokenThreads) return MOE_ERR_UNSUPPORTED;
     const dim3 grid((unsigned)blocks), threads(kTokenThreads);
-    if (second) hipLaunchKernelGGL((i8_token_second_kernel<MSMAX, NF>), grid, threads, 0, s, t);
-    else if (t.experts.a_max) hipLaunchKernelGGL((i8_token_first_kernel<MSMAX, NF, true>), grid, threads, 0, s, t);
-    else hipLaunchKernelGGL((i8_token_first_kernel<MSMAX, NF, false>), grid, threads, 0, s, t);
+    if (second) hipLaunchKernelGGL((i8_token_second_kernel<NF>), grid, threads, 0, s, t);
+    else if (t.experts.a_max) hipLaunchKernelGGL((i8_token_first_kernel<NF, true>), grid, threads, 0, s, t);
+    else hipLaunchKernelGGL((i8_token_first_kernel<NF, false>), grid, threads, 0, s, t);
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
 }  // namespace
 
+// Against the products and what is between them as launches of their own.  us here / there, 1024 / 4096: 16 tokens, top-1 of 64 experts beside a dense branch
+// 48 / 67, 20 tokens 75 / 70 (its rows are two sub-tiles); without one, of 8 experts, 64 tokens 40 / 45, 128 tokens of room for 32 rows 62 / 46; top-1 of
+// 64 with 16 / 24 / 32 tokens 46 / 56, 59 / 61, 65 / 64; top-2 of 128 with 12 / 16 / 20 64 / 68, 73 / 73, 87 / 79.  2048 / 8192, top-2 of 16, 16 / 48 / 128
+// tokens 112 / 118, 124 / 126, 147 / 130, beside a dense branch 16 / 20 tokens 122 / 137, 168 / 142.
+bool i8_token_faster(int T, int touched, int max_rows, int d, int f, bool dense) {
+    return i8_few_faster(touched, max_rows, d, f) && (T <= kI8FewRows || (!dense && T <= kI8TokenRows && touched <= 24));
+}
+
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s) {
     const I8GemmArgs& a = t.experts;
-    if (!t.order || a.slots < 1 || a.slots > t.E || a.max_rows > kI8FewRows || a.K % 32 || a.N % 8 || t.top_k > 2) return MOE_ERR_INVALID_ARG;
+    if (!t.order || a.slots < 1 || a.slots > t.E || a.max_rows > kI8FewRows || (t.dense && t.T > kI8FewRows) || a.K % 32 || a.N % 8 || t.top_k > 2)
+        return MOE_ERR_INVALID_ARG;
     if (second && gather_faster(t)) {
         hipLaunchKernelGGL(i8_token_gather_kernel, dim3((unsigned)(few_tiles<1>(a.N) * 2)), dim3(kTokenThreads), 0, s, t);
         return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
     }
-    const int most = t.dense && t.T > a.max_rows ? std::min(t.T, kI8FewRows) : a.max_rows;
-    const int nf = few_columns(most <= 16 ? token_groups<1>(t) : token_groups<2>(t), most, a.N);
-    if (most > 16) return nf == 1 ? launch_token<2, 1>(t, second, s) : launch_token<2, 2>(t, second, s);
-    return nf == 1 ? launch_token<1, 1>(t, second, s) : nf == 2 ? launch_token<1, 2>(t, second, s) : launch_token<1, 4>(t, second, s);
+    const int nf = std::min(few_columns(token_groups(t), kI8FewRows, a.N), 4);
+    return nf == 1 ? launch_token<1>(t, second, s) : nf == 2 ? launch_token<2>(t, second, s) : launch_token<4>(t, second, s);
 }
 
 }  // namespace moe
