@@ -88,7 +88,7 @@ struct I8TokenArgs {
 };
 inline int i8_token_tiles(int N) { return (N + 127) / 128 * 8; } // column tiles of a second product, at most
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s);
-constexpr int kI8TokenRows = 64;                                 // tokens of such a layer, at most
+constexpr int kI8TokenRows = 128;                                // tokens of such a layer, at most
 bool i8_token_faster(int T, int touched, int max_rows, int d, int f, bool dense);
 // (i8_tile.hip) tiles of up to 128 rows, two or three work-groups per compute unit
 int launch_i8_tile(const I8GemmArgs& a, const I8GemmArgs* b, int epi, hipStream_t s);

@@ -8,6 +8,11 @@ namespace moe {
 
 namespace {
 
+// work-groups of a product, at least
+long long few_blocks(long long groups, int max_rows, int N, int nf) {
+    return groups * (max_rows <= 32 ? 1 : (max_rows + 63) / 64) * ((N + 16 * nf - 1) / (16 * nf));
+}
+
 // NW waves, NF 16-column fragments per work-group, at most 16 MSMAX rows per tile; BF16: rows in bf16 with a_max
 template <int NW, int MSMAX, int NF, int EPI, bool BF16>
 __global__ __launch_bounds__(NW * 64) void i8_few_kernel(const I8GemmArgs a, const int n_tiles, const int m_tiles) {
@@ -49,8 +54,10 @@ template <int NW, int MSMAX, int NF, int EPI, bool BF16> int launch_few(const I8
 }
 template <int NF, int EPI, bool BF16> int launch_few_rows(const I8GemmArgs& a, hipStream_t s) {
     if (a.max_rows <= 16) {
-        // a K of few blocks: four waves (up to two blocks for each of eight)
-        return a.K <= 512 ? launch_few<4, 1, NF, EPI, BF16>(a, s) : launch_few<8, 1, NF, EPI, BF16>(a, s);
+        // Four waves on a K of few blocks (up to two for each of eight), and where there are work-groups enough, of which then three fit a compute unit
+        // (FFN of 16 experts of up to 16 rows, 2048 / 8192: 100 -> 96 us; one row, 8192 x 2048, 128 work-groups: 6.5 with eight, 7.8 with four)
+        const bool four = NF == 8 || a.K <= 512 || few_blocks(a.G, a.max_rows, a.N, NF) >= 512;      // (128 columns: there are 512)
+        return four ? launch_few<4, 1, NF, EPI, BF16>(a, s) : launch_few<NF == 8 ? 4 : 8, 1, NF, EPI, BF16>(a, s);
     }
     if constexpr (NF <= 2) {                                     // (with 64 columns more registers than there are)
         if constexpr (!BF16) return a.max_rows <= 32 ? launch_few<8, 2, NF, EPI, false>(a, s) : launch_few<8, 4, NF, EPI, false>(a, s);
@@ -71,9 +78,6 @@ template <int EPI, bool BF16> int launch_few_columns(const I8GemmArgs& a, int NF
 // Columns of a work-group: the most that leave enough of them; 128 columns read the rows least often.  us per product: 64 experts of up
 // to 16 rows, 2048 x 8192, with 16 / 32 / 64 / 128 columns 267 / 210 / 178 / 166; one row, 2048 x 6144, 5.9 / 4.2 / 6.4 with 16 / 32 / 64
 // (384, 192, 96 work-groups).  More than 32 rows: one work-group for each compute unit, with 16 columns if that is enough.
-long long few_blocks(long long groups, int max_rows, int N, int nf) {
-    return groups * (max_rows <= 32 ? 1 : (max_rows + 63) / 64) * ((N + 16 * nf - 1) / (16 * nf));
-}
 int few_columns(long long groups, int max_rows, int N) {
     if (max_rows <= 16 && few_blocks(groups, max_rows, N, 8) >= 512) return 8;
     if (max_rows > 32) return few_blocks(groups, max_rows, N, 1) > 256 ? 2 : 1;

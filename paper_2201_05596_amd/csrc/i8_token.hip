@@ -7,17 +7,18 @@
 // anybody.  Its hand-over across the XCDs' separate L2s costs about 4 us: results are written with device-scope stores (through the L2), a work-group
 // waits for its stores before it counts itself, and the last one acquires at device scope before its loads.  The counters are cleared by the
 // gate's launch.
-// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 8.6 us behind a gate of 9.2, with a hand-over 6.7 + 11.2; as launches that
-// bring x into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1.  16 tokens, top-2 of 64 experts beside one: 33 + 32 us
-// (27 groups with rows, 113 MB of codes each: 3.4 TB/s).  Tried: both products in one launch, work-groups taking tiles by ticket and those of the second product waiting for
-// a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across the L2s).
+// One token, top-2 of 128 experts beside a dense branch, 1024 / 4096: 6.7 + 8.6 us behind a gate of 9.2, with a hand-over (eight waves) 6.7 + 11.2; as launches that
+// bring x into codes, multiply, multiply and combine 4.2 + 6.3 + 6.0 + 4.1.  Tried: both products in one launch, work-groups taking tiles by ticket and
+// those of the second product waiting for a flag of their group: 27.6 us (11 ns for each ticket, and every hand-over is a chain of stores, count, flag and loads across the L2s).
 #include "i8_few.h"
 
 namespace moe {
 
 namespace {
 
-constexpr int kTokenWaves = 8, kTokenThreads = kTokenWaves * 64;
+// Four waves: a work-group is a chain of trips to memory, and of those with 130 registers a wave three fit a compute unit, with eight waves and more registers
+// one (us for the layer: 16 tokens, top-2 of 64 experts beside a dense branch, 1024 / 4096 72 -> 61, 8 tokens, top-1 of 64, 2048 / 8192 67 -> 60).
+constexpr int kTokenWaves = 4, kTokenThreads = kTokenWaves * 64;
 
 // a work-group's tile: columns fastest; the dense branch comes first, then the experts with rows in the gate's order
 struct TokenTile {
@@ -119,10 +120,10 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_second_kernel(const I8
 // rows become codes in LDS once, while the weights are on their way: kGatherAhead pairs of blocks of 64 k for each wave and group.  A pair is one operand:
 // columns 0 .. 7 are the first block's and 8 .. 15 the same eight of the second, rows 0 .. 7 of the other operand the tokens' codes of the first block and
 // 8 .. 15 those of the second, and of the results the two blocks' own quarters are taken.
-constexpr int kGatherGroups = 4, kGatherAhead = 4, kGatherPieces = 8, kGatherBytes = kTokenThreads * kGatherPieces * 8;
-__global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8TokenArgs t) {
+constexpr int kGatherWaves = 8, kGatherThreads = kGatherWaves * 64, kGatherGroups = 4, kGatherAhead = 4, kGatherPieces = 8, kGatherBytes = kGatherThreads * kGatherPieces * 8;
+__global__ __launch_bounds__(kGatherThreads) void i8_token_gather_kernel(const I8TokenArgs t) {
     __shared__ __attribute__((aligned(16))) int8_t codes[kGatherBytes];                          // [group][token's place][K]
-    __shared__ int part[kTokenWaves][kGatherGroups][4][16];
+    __shared__ int part[kGatherWaves][kGatherGroups][4][16];
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, kg = lane >> 4, half = c >> 3;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int N = t.experts.N, nkb = t.experts.K / 32, bytes = t.experts.K * 2, p_ng = (N + 127) / 128, dense = t.dense ? 1 : 0;
@@ -138,7 +139,7 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8
     uint32_t most[kGatherPieces];
 #pragma unroll
     for (int i = 0; i < kGatherPieces; ++i) {
-        const int p = tid + i * kTokenThreads;
+        const int p = tid + i * kGatherThreads;
         if (p >= pieces) break;
         const int row = p / row_pieces, q = row / t.T, r = row % t.T;
         const bool d = q < dense;
@@ -160,7 +161,7 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8
         if (q >= groups) continue;
 #pragma unroll
         for (int s = 0; s < kGatherAhead; ++s)
-            if (s * kTokenWaves + w < pairs) bf[q][s] = load_pair(B[q], s * kTokenWaves + w);
+            if (s * kGatherWaves + w < pairs) bf[q][s] = load_pair(B[q], s * kGatherWaves + w);
     }
     // what thread (token, column) needs for its result
     const int token = min(tid >> 3, t.T - 1), n = ng * 128 + frag + (col8 + (tid & 7)) * 8, nc = min(n, N - 1);
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8
     }
 #pragma unroll
     for (int i = 0; i < kGatherPieces; ++i) {
-        const int p = tid + i * kTokenThreads;
+        const int p = tid + i * kGatherThreads;
         if (p >= pieces) break;
         float f[8];
         unpack_bias8(x[i], f);
@@ -200,13 +201,13 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8
 #pragma unroll
     for (int q = 0; q < kGatherGroups; ++q) acc[q] = i32x4_t{0, 0, 0, 0};
     const int a_row = min(c & 7, t.T - 1);
-    for (int first = 0; first < pairs; first += kGatherAhead * kTokenWaves) {
+    for (int first = 0; first < pairs; first += kGatherAhead * kGatherWaves) {
 #pragma unroll
         for (int q = 0; q < kGatherGroups; ++q) {
             if (q >= groups) continue;
 #pragma unroll
             for (int s = 0; s < kGatherAhead; ++s) {
-                const int pair = first + s * kTokenWaves + w, next = pair + kGatherAhead * kTokenWaves, kb = 2 * pair + half;
+                const int pair = first + s * kGatherWaves + w, next = pair + kGatherAhead * kGatherWaves, kb = 2 * pair + half;
                 if (pair >= pairs) continue;
                 i32x4_t a = *reinterpret_cast<const i32x4_t*>(codes + (size_t)(q * t.T + a_row) * bytes + min(kb, nkb - 1) * 64 + kg * 16);
                 if (kb >= nkb) a = i32x4_t{0, 0, 0, 0};
@@ -225,7 +226,7 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_gather_kernel(const I8
     auto result = [&](int q, int r, float scale) {
         int sum = 0;
 #pragma unroll
-        for (int s = 0; s < kTokenWaves; ++s) sum += part[s][q][r][tid & 7] + part[s][q][r][8 + (tid & 7)];
+        for (int s = 0; s < kGatherWaves; ++s) sum += part[s][q][r][tid & 7] + part[s][q][r][8 + (tid & 7)];
         const float cs = q == 0 ? col_scale[0] : q == 1 ? col_scale[1] : q == 2 ? col_scale[2] : col_scale[3];
         return i8_value(sum, scale * cs, q == 0 ? bias[0] : q == 1 ? bias[1] : q == 2 ? bias[2] : bias[3]);
     };
@@ -264,11 +265,11 @@ template <int NF> int launch_token(const I8TokenArgs& t, bool second, hipStream_
 }  // namespace
 
 // Against the products and what is between them as launches of their own.  us here / there, 1024 / 4096: 16 tokens, top-1 of 64 experts beside a dense branch
-// 48 / 67, 20 tokens 75 / 70 (its rows are two sub-tiles); without one, of 8 experts, 64 tokens 40 / 45, 128 tokens of room for 32 rows 62 / 46; top-1 of
-// 64 with 16 / 24 / 32 tokens 46 / 56, 59 / 61, 65 / 64; top-2 of 128 with 12 / 16 / 20 64 / 68, 73 / 73, 87 / 79.  2048 / 8192, top-2 of 16, 16 / 48 / 128
-// tokens 112 / 118, 124 / 126, 147 / 130, beside a dense branch 16 / 20 tokens 122 / 137, 168 / 142.
+// 44 / 68 (20 tokens, whose rows in it are two sub-tiles, 75 / 70); without one 16 / 32 / 48 / 64 tokens 42 / 55, 55 / 63, 68 / 70, 81 / 79; top-1 of 32, 64 / 128 /
+// 256 tokens 67 / 78, 78 / 83, 90 / 86; top-2 of 128, 16 / 32 60 / 73, 91 / 91.  512 / 2048, top-2 of 64, 64 / 128 tokens 46 / 50, 60 / 57.  2048 / 8192, top-2 of
+// 16, 16 / 64 / 128 101 / 118, 116 / 126, 122 / 128 (room for 16 rows 134 / 130); room for 32 rows loses (8 experts, 64 tokens 51 / 45).
 bool i8_token_faster(int T, int touched, int max_rows, int d, int f, bool dense) {
-    return i8_few_faster(touched, max_rows, d, f) && (T <= kI8FewRows || (!dense && T <= kI8TokenRows && touched <= 24));
+    return i8_few_faster(touched, max_rows, d, f) && (T <= kI8FewRows || (!dense && T <= (std::min(d, f) >= 1024 ? kI8TokenRows : 64)));
 }
 
 int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s) {
@@ -276,7 +277,7 @@ int launch_i8_token(const I8TokenArgs& t, bool second, hipStream_t s) {
     if (!t.order || a.slots < 1 || a.slots > t.E || a.max_rows > kI8FewRows || (t.dense && t.T > kI8FewRows) || a.K % 32 || a.N % 8 || t.top_k > 2)
         return MOE_ERR_INVALID_ARG;
     if (second && gather_faster(t)) {
-        hipLaunchKernelGGL(i8_token_gather_kernel, dim3((unsigned)(few_tiles<1>(a.N) * 2)), dim3(kTokenThreads), 0, s, t);
+        hipLaunchKernelGGL(i8_token_gather_kernel, dim3((unsigned)(few_tiles<1>(a.N) * 2)), dim3(kGatherThreads), 0, s, t);
         return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
     }
     const int nf = std::min(few_columns(token_groups(t), kI8FewRows, a.N), 4);

@@ -233,10 +233,11 @@ def test_layer_against_the_oracle(name):
     Layer(**LAYERS[name], seed=5).check_oracle()
 
 
-@pytest.mark.parametrize("T", [16, 17, 24, 63, 64, 65])
+@pytest.mark.parametrize("T", [16, 17, 24, 63, 64, 65, 127, 128, 129])
 @pytest.mark.parametrize("E,k,C,residual", [(4, 1, 16, False), (4, 1, 16, True), (4, 2, 17, False), (30, 2, 8, False), (24, 1, 16, False), (30, 1, 16, True)])
 def test_borders_of_the_few_tokens(T, E, k, C, residual):
     Layer(T, 264, 520, E, k, C, residual, seed=T + E).check()
+    Layer(T, 1032, 1024, E, k, C, residual, seed=T + E).check()
 
 
 @pytest.mark.parametrize("T,E,C,d,f", [(900, 41, 100, 1024, 64), (3000, 41, 100, 1024, 4104), (1500, 41, 50, 1024, 4104), (600, 41, 20, 1024, 4104), (7000, 8, 1100, 1024, 64),
