@@ -452,9 +452,9 @@ typedef struct {
  *   h = gelu_tanh(q(xe[e,c,:]) W1[e] + b1[e]) rounded to bf16,   ye[e,c,:] = q(h) W2[e] + b2[e]
  * Other rows of ye are left untouched.
  * moe_i8_layer_forward -- moe_layer_forward with 8-bit experts (and dense branch): the gate on x as it is, then the FFNs as
- * above on q(x), combined in 32 bits.  Layers of up to 16 tokens (without a dense branch 64, or 128 if d and f are at least
- * 1024) with room for up to 16 rows an expert round the sum once, unless their rows touch many experts; others, if top-2 or residual, round the experts' and the dense branch's results to
- * bf16 before they are added up.
+ * above on q(x), whose results stay in 32 bits: with y() for an FFN's result before its rounding, out[t,:] is
+ *   [y(dense branch) +] sum_j g_j y(expert j), choices in order, by one multiply-add each in 32 bits, rounded once to bf16, whatever the
+ * number of tokens.
  * Both: shape.dtype is MOE_BF16, T and E * capacity at most 2^24, (ceil(rows / 128) + E + 8) ceil(max(d, f) / 16) < 2^23 with the
  * larger of the two as rows, shape.flags 0 or MOE_FLAG_PACKED_GATE (layer only has a gate); the dense branch's members of `weights` are not looked at by moe_i8_expert_ffn.
  * ws >= moe_i8_workspace_bytes(shape), 0 for shapes that are rejected. */

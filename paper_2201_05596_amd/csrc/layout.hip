@@ -126,6 +126,55 @@ __global__ __launch_bounds__(256) void combine_bf16_kernel(const uint4* __restri
     }
 }
 
+// The same from results in 32 bits, rounded once: out[t,:] = bf16(dense[t,:] + sum_j keep_j g_j ye[e_j, slot_j, :]), as the kernels of few
+// tokens add them up (i8_token.hip).  Bound by traffic.
+template <int K>
+__global__ __launch_bounds__(256) void combine_sums_kernel(const float4* __restrict__ ye, const int32_t* __restrict__ expert_idx,
+                                                           const int32_t* __restrict__ slot_idx, const float* __restrict__ gate_w,
+                                                           const float4* __restrict__ dense, uint4* __restrict__ out, int T, int C, int row_vecs) {
+    const int lane = threadIdx.x % kWave;
+    const int t = blockIdx.x * (blockDim.x / kWave) + threadIdx.x / kWave;
+    if (t >= T) return;
+    const float4* src[K];
+    float g[K];
+#pragma unroll
+    for (int j = 0; j < K; ++j) {
+        const int s = slot_idx[(size_t)t * K + j];
+        const int e = expert_idx[(size_t)t * K + j];
+        g[j] = gate_w[(size_t)t * K + j];
+        src[j] = s >= 0 ? ye + ((size_t)e * C + s) * row_vecs * 2 : nullptr;
+    }
+    for (int i = lane; i < row_vecs; i += kWave) {
+        float4 acc[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) acc[h] = dense ? dense[(size_t)t * row_vecs * 2 + 2 * i + h] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < K; ++j) {
+            if (!src[j]) continue;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 v = src[j][2 * i + h];
+                acc[h].x = fmaf(g[j], v.x, acc[h].x);
+                acc[h].y = fmaf(g[j], v.y, acc[h].y);
+                acc[h].z = fmaf(g[j], v.z, acc[h].z);
+                acc[h].w = fmaf(g[j], v.w, acc[h].w);
+            }
+        }
+        out[(size_t)t * row_vecs + i] = make_uint4(pack_bf16x2(acc[0].x, acc[0].y), pack_bf16x2(acc[0].z, acc[0].w),
+                                                   pack_bf16x2(acc[1].x, acc[1].y), pack_bf16x2(acc[1].z, acc[1].w));
+    }
+}
+
+int launch_combine_sums(const float* ye, const int32_t* expert_idx, const int32_t* slot_idx, const float* gate_w, const float* dense,
+                        void* out, int T, int k, int C, int d, hipStream_t s) {
+    const int rpb = 256 / kWave;
+    const dim3 grid((T + rpb - 1) / rpb), block(256);
+    auto kernel = k == 1 ? &combine_sums_kernel<1> : &combine_sums_kernel<2>;
+    hipLaunchKernelGGL(kernel, grid, block, 0, s, reinterpret_cast<const float4*>(ye), expert_idx, slot_idx, gate_w,
+                       reinterpret_cast<const float4*>(dense), static_cast<uint4*>(out), T, C, d / 8);
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
 int launch_combine(const void* ye, int dtype, const int32_t* expert_idx, const int32_t* slot_idx, const float* gate_w,
                    const void* addend, void* out, int T, int k, int C, int d, hipStream_t s, const PartSums& dense) {
     if (dense.partial && (dtype != MOE_BF16 || dense.ksplit < 1 || dense.ksplit > kLinearMaxSplit)) return MOE_ERR_INVALID_ARG;

@@ -189,6 +189,9 @@ int launch_combine(const void* ye, int dtype, const int32_t* expert_idx, const i
                    const float* gate_w, const void* addend, void* out,
                    int T, int k, int C, int d, hipStream_t s,
                    const PartSums& dense = PartSums{});
+// the same of results in 32 bits (ye, and dense [T, d] or nullptr), rounded once to bf16
+int launch_combine_sums(const float* ye, const int32_t* expert_idx, const int32_t* slot_idx, const float* gate_w, const float* dense,
+                        void* out, int T, int k, int C, int d, hipStream_t s);
 
 // What a grouped GEMM does with a finished row.
 enum WsEpilogue {
