@@ -1624,8 +1624,8 @@ int moe_i8_layer_forward(const moe_shape_t* shape, const moe_i8_weights_t* weigh
     int8_t* xq = at<int8_t>(ws, L.x);
     float* x_scale = at<float>(ws, L.x_scale);
 
-    // an expert has at most one row of a token
-    const int max_rows = std::min(C, T), touched = (int)std::min<long long>((long long)T * k, E);
+    // (a token whose logits are all NaN has expert E - 1 as both of its choices)
+    const int max_rows = (int)std::min<long long>(C, (long long)T * k), touched = (int)std::min<long long>((long long)T * k, E);
     const bool dense = shape->residual, few = i8_token_faster(T, touched, max_rows, d, shape->d_ffn, dense);
     uint32_t* words = at<uint32_t>(ws, L.words);
     const int n_maxes = E * max_rows + (dense ? T : 0), n_words = n_maxes + i8_token_tiles(d);

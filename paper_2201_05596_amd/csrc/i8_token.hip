@@ -118,32 +118,35 @@ __global__ __launch_bounds__(kTokenThreads) void i8_token_second_kernel(const I8
 
 // The second products and the combine of the fewest tokens, without a hand-over: a work-group has 8 columns of every group, its waves split K.  h's
 // rows become codes in LDS once, while the weights are on their way: kGatherAhead pairs of blocks of 64 k for each wave and group.  A pair is one operand:
-// columns 0 .. 7 are the first block's and 8 .. 15 the same eight of the second, rows 0 .. 7 of the other operand the tokens' codes of the first block and
-// 8 .. 15 those of the second, and of the results the two blocks' own quarters are taken.
-constexpr int kGatherWaves = 8, kGatherThreads = kGatherWaves * 64, kGatherGroups = 4, kGatherAhead = 4, kGatherPieces = 8, kGatherBytes = kGatherThreads * kGatherPieces * 8;
+// columns 0 .. 7 are the first block's and 8 .. 15 the same eight of the second, rows 0 .. 7 of the other operand the codes of a group's rows in the first
+// block and 8 .. 15 those in the second, and of the results the two blocks' own quarters are taken.  A group has up to kGatherRows rows.
+constexpr int kGatherWaves = 8, kGatherThreads = kGatherWaves * 64, kGatherGroups = 4, kGatherRows = 4, kGatherAhead = 4, kGatherPieces = 8, kGatherBytes = kGatherThreads * kGatherPieces * 8;
+// places of a group's rows
+__host__ __device__ __forceinline__ int gather_places(const I8TokenArgs& t) { return t.dense && t.T > t.experts.max_rows ? t.T : t.experts.max_rows; }
 __global__ __launch_bounds__(kGatherThreads) void i8_token_gather_kernel(const I8TokenArgs t) {
-    __shared__ __attribute__((aligned(16))) int8_t codes[kGatherBytes];                          // [group][token's place][K]
-    __shared__ int part[kGatherWaves][kGatherGroups][4][16];
+    __shared__ __attribute__((aligned(16))) int8_t codes[kGatherBytes];                          // [group][row's place][K]
+    __shared__ int part[kGatherWaves][kGatherGroups][kGatherRows][16];
     const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, kg = lane >> 4, half = c >> 3;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int N = t.experts.N, nkb = t.experts.K / 32, bytes = t.experts.K * 2, p_ng = (N + 127) / 128, dense = t.dense ? 1 : 0;
+    const int places = gather_places(t);
     const int ng = blockIdx.x >> 4, frag = blockIdx.x >> 1 & 7, col8 = (blockIdx.x & 1) * 8;     // columns 128 ng + frag + 8 (col8 .. col8 + 7)
     const int groups = __builtin_amdgcn_readfirstlane(dense + (t.order[t.E] >> 1));
     int g[kGatherGroups];
 #pragma unroll
     for (int q = 0; q < kGatherGroups; ++q) g[q] = __builtin_amdgcn_readfirstlane(q < groups && q >= dense ? t.order[q - dense] : 0);
 
-    // h: a thread's pieces of 8 values (rows that no token has hold anything: nobody looks at what becomes of them)
-    const int row_pieces = bytes / 8, pieces = groups * t.T * row_pieces;
+    // h: a thread's pieces of 8 values (places behind a group's rows repeat one of them or hold anything: nobody looks at what becomes of them)
+    const int row_pieces = bytes / 8, pieces = groups * places * row_pieces;
     uint4 x[kGatherPieces];
     uint32_t most[kGatherPieces];
 #pragma unroll
     for (int i = 0; i < kGatherPieces; ++i) {
         const int p = tid + i * kGatherThreads;
         if (p >= pieces) break;
-        const int row = p / row_pieces, q = row / t.T, r = row % t.T;
+        const int row = p / row_pieces, q = row / places, r = row % places;
         const bool d = q < dense;
-        const long long at = d ? r : (long long)(q == 0 ? g[0] : q == 1 ? g[1] : q == 2 ? g[2] : g[3]) * t.experts.a_group_stride +
+        const long long at = d ? min(r, t.T - 1) : (long long)(q == 0 ? g[0] : q == 1 ? g[1] : q == 2 ? g[2] : g[3]) * t.experts.a_group_stride +
                                          min(r, (int)t.experts.a_group_stride - 1);
         x[i] = *reinterpret_cast<const uint4*>((d ? t.dense_branch.A : t.experts.A) + at * t.experts.lda + (p % row_pieces) * 8);
         most[i] = (d ? t.dense_branch.a_max : t.experts.a_max)[at];
@@ -200,7 +203,7 @@ __global__ __launch_bounds__(kGatherThreads) void i8_token_gather_kernel(const I
     i32x4_t acc[kGatherGroups];
 #pragma unroll
     for (int q = 0; q < kGatherGroups; ++q) acc[q] = i32x4_t{0, 0, 0, 0};
-    const int a_row = min(c & 7, t.T - 1);
+    const int a_row = min(c & 7, places - 1);
     for (int first = 0; first < pairs; first += kGatherAhead * kGatherWaves) {
 #pragma unroll
         for (int q = 0; q < kGatherGroups; ++q) {
@@ -209,7 +212,7 @@ __global__ __launch_bounds__(kGatherThreads) void i8_token_gather_kernel(const I
             for (int s = 0; s < kGatherAhead; ++s) {
                 const int pair = first + s * kGatherWaves + w, next = pair + kGatherAhead * kGatherWaves, kb = 2 * pair + half;
                 if (pair >= pairs) continue;
-                i32x4_t a = *reinterpret_cast<const i32x4_t*>(codes + (size_t)(q * t.T + a_row) * bytes + min(kb, nkb - 1) * 64 + kg * 16);
+                i32x4_t a = *reinterpret_cast<const i32x4_t*>(codes + (size_t)(q * places + a_row) * bytes + min(kb, nkb - 1) * 64 + kg * 16);
                 if (kb >= nkb) a = i32x4_t{0, 0, 0, 0};
                 acc[q] = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, bf[q][s], acc[q], 0, 0, 0);
                 if (next < pairs) bf[q][s] = load_pair(B[q], next);
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(kGatherThreads) void i8_token_gather_kernel(const I
 // 1 / 3 / 8192 / 2048 16.2 / 8.5, 17.2 / 12.9, 16.2 / 17.6; 2 / 3 and 2 / 4 / 4096 / 1024 11.1 / 9.6, 11.6 / 11.2; 4 / 4 / 2048 / 512 8.4 / 8.7.
 bool gather_faster(const I8TokenArgs& t) {
     const long long groups = t.experts.slots + (t.dense ? 1 : 0), bytes = groups * t.experts.K * 2;
-    return t.T <= 4 && groups <= kGatherGroups && bytes <= 16384 && bytes * t.T <= kGatherBytes;
+    return t.T <= 4 && gather_places(t) <= kGatherRows && groups <= kGatherGroups && bytes <= 16384 && bytes * gather_places(t) <= kGatherBytes;
 }
 
 long long token_groups(const I8TokenArgs& t) { return t.experts.slots + (t.dense ? 1 : 0); }
