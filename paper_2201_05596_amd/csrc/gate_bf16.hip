@@ -556,7 +556,10 @@ static int launch_decode_cfg(const uint16_t* x, const uint16_t* frags, const flo
 #define MOE_DECODE(PLAIN, MAXES) \
     launch_decode_p<MA, RK, NV, PLAIN, MAXES>(x, PLAIN ? nullptr : frags, PLAIN ? Wg : nullptr, bg, logits, T, d, E, ET, C, expert_idx, slot_idx, \
                                               gate_w, expert_rows, slot_token, expert_order, flags, tag, rows, s)
-    if (rows.max) return frags ? MOE_DECODE(false, true) : MOE_DECODE(true, true);
+    if constexpr (MA == 1) {                     // (layers that want the rows' largest magnitudes have up to 128 tokens)
+        if (rows.max) return frags ? MOE_DECODE(false, true) : MOE_DECODE(true, true);
+    }
+    if (rows.max) return MOE_ERR_INVALID_ARG;
     return frags ? MOE_DECODE(false, false) : MOE_DECODE(true, false);
 #undef MOE_DECODE
 }
