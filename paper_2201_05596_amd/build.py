@@ -27,8 +27,9 @@ FLAGS = [
 ]
 
 
-# Sources whose kernels must keep nothing in scratch memory: a build that does not is refused
-NO_SCRATCH = ("tree_attn_bf16.hip", "tree_attn_fp8.hip", "tree_attn_fp4.hip")
+# Sources whose kernels must keep nothing in scratch memory: a build that does not is refused.  (Not among them: the tiles of 256 rows, ffn_wide*.hip and
+# i8_wide.hip, which take every register; some keep up to three of the epilogue's values there, outside of the main loop.)
+NO_SCRATCH = ("tree_attn_bf16.hip", "tree_attn_fp8.hip", "tree_attn_fp4.hip", "i8_quant.hip", "i8_few.hip", "i8_token.hip", "i8_tile.hip")
 
 
 def kernels_in_scratch(remarks: str) -> list:

@@ -104,7 +104,7 @@ constexpr bool wide_hints(int epi) { return epi == EPI_STORE || epi == EPI_GELU 
 template <int BM, int EPI, bool RAGGED, int POLICY, class Args>
 __global__ __launch_bounds__(kWideThreads, 1) void wide_kernel(const Args a0, const Args a1, const int split) {
     constexpr bool I8 = std::is_same<Args, I8GemmArgs>::value;
-    const bool second = (int)blockIdx.x >= split;                // uniform over the work-group
+    const bool second = !(I8 && EPI == EPI_SCATTER) && (int)blockIdx.x >= split;   // uniform over the work-group (codes: a combine is alone)
     const Args& a = second ? a1 : a0;
     const int block = second ? (int)blockIdx.x - split : (int)blockIdx.x;
 

@@ -23,20 +23,48 @@ template <> struct Piece<uint16_t> {
     __device__ __forceinline__ void get(float (&f)[8]) const { unpack_bias8(v, f); }
 };
 template <> struct Piece<float> {
-    float4 a, b;
+    u32x4_t a, b;
     template <bool BIG> __device__ __forceinline__ void load(const float* p) {
-        a = BIG ? __builtin_bit_cast(float4, load_stream16(p)) : reinterpret_cast<const float4*>(p)[0];
-        b = BIG ? __builtin_bit_cast(float4, load_stream16(p + 4)) : reinterpret_cast<const float4*>(p)[1];
+        const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
+        a = BIG ? __builtin_nontemporal_load(v) : v[0];
+        b = BIG ? __builtin_nontemporal_load(v + 1) : v[1];
     }
-    __device__ __forceinline__ void none() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+    __device__ __forceinline__ void none() { a = b = u32x4_t{0, 0, 0, 0}; }
     __device__ __forceinline__ void get(float (&f)[8]) const {
-        f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            f[q] = __uint_as_float(a[q]);
+            f[4 + q] = __uint_as_float(b[q]);
+        }
     }
 };
 
-// TPR threads (a wave or a work-group) hold a row of up to 8 NP TPR values from its one read to its codes.
+template <typename T> __device__ __forceinline__ uint32_t piece_max_bits(const Piece<T>& p) {
+    float f[8];
+    p.get(f);
+    uint32_t m = 0;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) m = max(m, __float_as_uint(f[q]) & 0x7fffffffu);
+    return m;
+}
+template <typename T> __device__ __forceinline__ u32x2_t piece_codes(const Piece<T>& p, uint32_t m, float inv) {
+    float f[8];
+    p.get(f);
+    uint32_t c[8];
+#pragma unroll
+    for (int q = 0; q < 8; ++q) c[q] = m < 0x7f800000u ? i8_code_bits(f[q], inv) : 0u;
+    return u32x2_t{i8_pack4(c[0], c[1], c[2], c[3]), i8_pack4(c[4], c[5], c[6], c[7])};
+}
+template <bool BIG> __device__ __forceinline__ void store_codes(int8_t* to, const u32x2_t o) {
+    if (BIG) __builtin_nontemporal_store(o, reinterpret_cast<u32x2_t*>(to));
+    else *reinterpret_cast<u32x2_t*>(to) = o;
+}
+
+// TPR threads (a wave or a work-group) hold the first 8 NP TPR values of a row from their one read to their codes.  LONG: there are more, which are read
+// again for their codes (rows of more than 65536 columns, whose float values do not fit a work-group's registers: 150 x 131072 24.5 us, 300 in bf16 28.9; held,
+// partly in scratch memory, 37.8 and 40.4).
 // BIG: rows and codes past the caches
-template <typename T, int TPR, int NP, bool BIG>
+template <typename T, int TPR, int NP, bool LONG, bool BIG>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8RowsArgs a) {
     constexpr int PER = TPR < 256 ? 256 / TPR : 1;               // rows of a work-group
     __shared__ uint32_t part[TPR / kWave];
@@ -56,12 +84,13 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
     }
     uint32_t m = 0;
 #pragma unroll
-    for (int i = 0; i < NP; ++i) {
-        float f[8];
-        p[i].get(f);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) m = max(m, __float_as_uint(f[q]) & 0x7fffffffu);
-    }
+    for (int i = 0; i < NP; ++i) m = max(m, piece_max_bits(p[i]));
+    if constexpr (LONG)
+        for (int at = tid + NP * TPR; at < pieces; at += TPR) {
+            Piece<T> v;
+            v.template load<false>(x + (size_t)at * 8);
+            m = max(m, piece_max_bits(v));
+        }
     m = wave_max_bits(m);
     if constexpr (TPR > kWave) {
         if (tid % kWave == 0) part[tid / kWave] = m;
@@ -75,19 +104,19 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void i8_rows_kernel(const I8
 #pragma unroll
     for (int i = 0; i < NP; ++i) {
         const int at = tid + i * TPR;
-        float f[8];
-        p[i].get(f);
-        uint32_t c[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) c[q] = m < 0x7f800000u ? i8_code_bits(f[q], inv) : 0u;
-        const u32x2_t o = {i8_pack4(c[0], c[1], c[2], c[3]), i8_pack4(c[4], c[5], c[6], c[7])};
-        if (at >= padded) continue;                              // zeros behind the row's end
-        if (BIG) __builtin_nontemporal_store(o, reinterpret_cast<u32x2_t*>(out + (size_t)at * 8));
-        else *reinterpret_cast<u32x2_t*>(out + (size_t)at * 8) = o;
+        const u32x2_t o = piece_codes(p[i], m, inv);
+        if (at < padded) store_codes<BIG>(out + (size_t)at * 8, o);                              // zeros behind the row's end
     }
+    if constexpr (LONG)
+        for (int at = tid + NP * TPR; at < padded; at += TPR) {
+            Piece<T> v;
+            v.none();
+            if (at < pieces) v.template load<BIG>(x + (size_t)at * 8);
+            store_codes<BIG>(out + (size_t)at * 8, piece_codes(v, m, inv));
+        }
 }
 
-template <typename T, int TPR, int NP> int launch_rows_p(const I8RowsArgs& a, hipStream_t s) {
+template <typename T, int TPR, int NP, bool LONG = false> int launch_rows_p(const I8RowsArgs& a, hipStream_t s) {
     constexpr int threads = TPR < 256 ? 256 : TPR, per = threads / TPR;
     constexpr int most = 1 << 21;                                // work-groups of a launch, whose threads are counted in 32 bits
     constexpr bool can_be_big = TPR != 256 || NP > 2;             // (a work-group for each of fewer than 2048 short rows: 32 MB)
@@ -96,8 +125,8 @@ template <typename T, int TPR, int NP> int launch_rows_p(const I8RowsArgs& a, hi
     for (long long first = 0; first < a.n_rows; first += (long long)most * per) {
         const dim3 blocks((unsigned)std::min<long long>(most, (a.n_rows - first + per - 1) / per));
         part.first = (int)first;
-        if (big && can_be_big) hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, can_be_big>), blocks, dim3(threads), 0, s, part);
-        else hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, false>), blocks, dim3(threads), 0, s, part);
+        if (big && can_be_big) hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, LONG, can_be_big>), blocks, dim3(threads), 0, s, part);
+        else hipLaunchKernelGGL((i8_rows_kernel<T, TPR, NP, LONG, false>), blocks, dim3(threads), 0, s, part);
         part.zero = nullptr;
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
@@ -115,7 +144,7 @@ template <typename T> int launch_rows_t(const I8RowsArgs& a, hipStream_t s) {
     if (p <= 1024) return launch_rows_p<T, 256, 4>(a, s);
     if (p <= 2048) return launch_rows_p<T, 256, 8>(a, s);
     if (p <= 8192) return launch_rows_p<T, 1024, 8>(a, s);
-    return launch_rows_p<T, 1024, 16>(a, s);
+    return launch_rows_p<T, 1024, 8, true>(a, s);
 }
 
 // COLS columns of a group, all of K, by a work-group of THREADS: four consecutive k-rows of 8 columns for each thread and round, so that
@@ -125,7 +154,7 @@ template <typename T> int launch_rows_t(const I8RowsArgs& a, hipStream_t s) {
 // LARGE: W's last reading and the result past the caches.
 // 64 columns are whole cache lines of W; with 32 there are twice the work-groups, for a single matrix.  Neighbouring tiles, which then share
 // lines, are eight work-groups apart: on the same XCD.  us with 32 / 64 columns: 1000 x 4000 9.0 / 10.2; 64 x 2048 x 8192 876 / 773, past the
-// caches 928 / 692 (3.2 GB: 4.7 TB/s; a thread for 8 columns of one row with the transposition byte by byte in LDS 1083); 16 x 8192 x 2048, read twice,
+// caches 928 / 692, without values in scratch memory 666 (3.2 GB: 4.8 TB/s; a thread for 8 columns of one row with the transposition byte by byte in LDS 1083); 16 x 8192 x 2048, read twice,
 // 315 / 285, past the caches 346 / 244.
 template <bool QUANTISE, int KEEP, int THREADS, int COLS, bool LARGE>
 __global__ __launch_bounds__(THREADS, KEEP > 4 ? 2 : 4) void i8_weights_kernel(const void* __restrict__ W, int8_t* __restrict__ packed,
@@ -141,14 +170,15 @@ __global__ __launch_bounds__(THREADS, KEEP > 4 ? 2 : 4) void i8_weights_kernel(c
     const int n0 = tile % tiles * COLS, n = n0 + cp * 8;
     if (tile >= all) return;
     const int KB = (K + 63) / 64, NG = (N + 127) / 128, rounds = (K + ROWS - 1) / ROWS;
-    const uint16_t* wb = static_cast<const uint16_t*>(W) + (size_t)g * K * N + n;
+    const uint16_t* wb = static_cast<const uint16_t*>(W) + (size_t)g * K * N + min(n, N - 8);
     const int8_t* wc = static_cast<const int8_t*>(W) + (size_t)g * K * N + n;
+    // A thread's four rows of a round, and its eight columns, are there or not (K and N are multiples of 8); if not, others stand in, which the maxima do
+    // not mind and whose codes are made zero: loads under a condition were waited for one by one.
+    auto there = [&](int round) { return round * ROWS + quad * 4 < K && n < N; };
     auto load = [&](int round, uint4 (&v)[4], bool last) {       // last: nobody reads it again
+        const uint16_t* p = wb + (size_t)min(round * ROWS + quad * 4, K - 4) * N;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = round * ROWS + quad * 4 + i;
-            v[i] = k < K && n < N ? (LARGE && last ? load_stream16(wb + (size_t)k * N) : *reinterpret_cast<const uint4*>(wb + (size_t)k * N)) : make_uint4(0, 0, 0, 0);
-        }
+        for (int i = 0; i < 4; ++i, p += N) v[i] = LARGE && last ? load_stream16(p) : *reinterpret_cast<const uint4*>(p);
     };
     uint4 held[KEEP > 0 ? KEEP : 1][4];
     float inv[8];
@@ -166,13 +196,23 @@ __global__ __launch_bounds__(THREADS, KEEP > 4 ? 2 : 4) void i8_weights_kernel(c
         if constexpr (KEEP > 0) {
 #pragma unroll
             for (int i = 0; i < KEEP; ++i) load(i, held[i], true);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int i = 0; i < KEEP; ++i) see(held[i]);
+            for (int i = 0; i < KEEP; ++i) {
+                see(held[i]);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) asm volatile("" : "+v"(m[q]));       // all of a round's maxima here, not one column after the other,
+            }
+            // and the values as loaded: left to itself the compiler keeps what it unpacked for the maxima, more than there are registers
+#pragma unroll
+            for (int i = 0; i < KEEP; ++i)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) asm volatile("" : "+v"(held[i][q].x), "+v"(held[i][q].y), "+v"(held[i][q].z), "+v"(held[i][q].w));
         } else {
             uint4 next[4];
             load(0, held[0], false);
             for (int i = 0; i < rounds; ++i) {
-                load(i + 1, next, false);                        // (zeros behind K)
+                load(i + 1, next, false);
                 see(held[0]);
 #pragma unroll
                 for (int q = 0; q < 4; ++q) held[0][q] = next[q];
@@ -199,19 +239,21 @@ __global__ __launch_bounds__(THREADS, KEEP > 4 ? 2 : 4) void i8_weights_kernel(c
         uint32_t o[8];                                           // word q: column q's four codes
         if constexpr (QUANTISE) {
             float f[4][8];
+            const uint32_t mask = there(round) ? ~0u : 0u;       // zeros behind K and N
 #pragma unroll
             for (int i = 0; i < 4; ++i) unpack_bias8(v[i], f[i]);
 #pragma unroll
             for (int q = 0; q < 8; ++q) {
                 o[q] = i8_pack4(i8_code_bits(f[0][q], inv[q]), i8_code_bits(f[1][q], inv[q]), i8_code_bits(f[2][q], inv[q]), i8_code_bits(f[3][q], inv[q]));
                 if (inv[q] != inv[q]) o[q] = 0;                  // a column that is not all numbers
+                o[q] &= mask;
             }
         } else {
             u32x2_t r[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int k = round * ROWS + quad * 4 + i;
-                r[i] = k < K && n < N ? *reinterpret_cast<const u32x2_t*>(wc + (size_t)k * N) : u32x2_t{0, 0};
+                r[i] = there(round) ? *reinterpret_cast<const u32x2_t*>(wc + (size_t)k * N) : u32x2_t{0, 0};
             }
 #pragma unroll
             for (int q = 0; q < 8; ++q) {

@@ -23,7 +23,7 @@ template <int ROWS, int EPI, bool NT>
 __global__ __launch_bounds__(kTileThreads, ROWS == 128 ? 3 : 2) void i8_tile_kernel(const I8GemmArgs a0, const I8GemmArgs a1, const int split) {
     constexpr int NS = tile_stages(ROWS), STAGE = 64 * (ROWS + kTileCols);               // bytes of a stage: activations, then weights
     static_assert((ROWS == 128 ? 3 : 2) * NS * STAGE <= 160 * 1024 && NS * STAGE >= 4 * 1280, "work-groups per compute unit; room for the epilogue's tables");
-    const bool second = (int)blockIdx.x >= split;                // uniform over the work-group
+    const bool second = EPI != EPI_SCATTER && (int)blockIdx.x >= split;   // uniform over the work-group (a combine is a launch of its own)
     const I8GemmArgs& a = second ? a1 : a0;
     const int block = second ? (int)blockIdx.x - split : (int)blockIdx.x;
     extern __shared__ __attribute__((aligned(16))) char lds[];

@@ -1,4 +1,4 @@
-"""What the built library holds for 8-bit experts: no kernel that no call reaches."""
+"""What the built library holds for 8-bit experts: no kernel that no call reaches, none that keeps values in scratch memory."""
 import os
 import re
 import subprocess
@@ -29,3 +29,12 @@ def test_gate_finds_rows_maxima_for_few_tokens_only(kernels):
     found = [tuple(map(int, re.findall(r"L[ib](\d+)E", n))) for n in kernels if "gate_decode_kernel" in n]
     assert len(set(found)) == len(found) and {m for m in found if not m[4]} == {(ma, rk, nv, plain, 0) for ma in (1, 2) for rk in (1, 2) for nv in (1, 2, 4, 8) for plain in (0, 1)}
     assert {m for m in found if m[4]} == {(1, rk, nv, plain, 1) for rk in (1, 2) for nv in (1, 2, 4, 8) for plain in (0, 1)}
+
+
+@pytest.mark.parametrize("name", ["i8_rows_kernel", "i8_weights_kernel", "i8_few_kernel", "i8_token_first_kernel", "i8_token_second_kernel",
+                                  "i8_token_gather_kernel", "i8_tile_kernel"])
+def test_nothing_in_scratch_memory(kernels, name):
+    """Rows and weights are held in registers between their largest magnitude and their codes; and the build refuses a source that does otherwise."""
+    found = {n: v for n, v in kernels.items() if name in n}
+    assert found and not {n: v for n, v in found.items() if v[1]}
+    assert {f"i8_{s}.hip" for s in ("quant", "few", "token", "tile")} <= set(B.NO_SCRATCH)
