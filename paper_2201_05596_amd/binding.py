@@ -702,7 +702,7 @@ def _i8_rows(t, device: int, dtype, rows: int, cols: int, name: str):
     between, inside = t.stride()
     if inside != 1:
         raise ValueError(f"{name}: the elements of a row have to be adjacent")
-    return t.data_ptr(), between if rows > 1 else shape[1]
+    return t.data_ptr(), between if rows > 1 else cols
 
 
 def moe_i8_quantize_rows(x, codes, scale) -> None:
