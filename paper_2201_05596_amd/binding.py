@@ -658,7 +658,12 @@ def moe_draft_block_forward(shape, cache, n_draft: int, rope, weights: dict, x, 
 _BF16, _F32, _INT8 = torch.bfloat16, torch.float32, torch.int8
 _get_device, _get_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
+_MOST = (1 << 31) - 1          # ctypes passes what is left of a larger size in 32 bits
+
+
 def moe_i8_weights_bytes(G: int, K: int, N: int) -> int:
+    if not (0 < G <= _MOST and 0 < K <= _MOST and 0 < N <= _MOST):
+        return 0
     return int(load_library().moe_i8_weights_bytes(int(G), int(K), int(N)))
 
 
@@ -713,6 +718,8 @@ def moe_i8_quantize_rows(x, codes, scale) -> None:
     dtype = x.dtype
     if dtype is not _BF16 and dtype is not _F32:
         raise ValueError(f"x: expected float32 or bfloat16, got {dtype}")
+    if rows > _MOST or cols > _MOST:
+        raise MoeError("moe_i8_quantize_rows", -2, "unsupported size")
     dev = _get_device()
     xp, xs = _rows(x, dev, dtype, rows, cols, "x")
     cp, cs = _i8_rows(codes, dev, _INT8, rows, (cols + 63) // 64 * 64, "codes")
