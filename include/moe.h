@@ -403,7 +403,7 @@ int moe_draft_block_forward(const moe_shape_t* shape, const moe_cache_shape_t* c
                             const int32_t* lens, const int32_t* tree, void* qkv, void* out, void* x1_out, void* moe_in_out,
                             float* logits_out, void* ws, size_t ws_bytes, void* stream);
 
-/* ---- experts in 8-bit integers: weights of half the size, products at twice the rate ----
+/* ---- experts in 8-bit integers: weights of half the size ----
  *
  * A row of activations, or a column of weights, is held as codes and a scale.  With m the largest magnitude of its values,
  *   M = max(m, 2^-100),  r = 127 / M,  s = M / 127      (r and s rounded to 32 bits)

@@ -93,7 +93,8 @@ int few_columns(long long groups, int max_rows, int N) {
 bool i8_few_faster(int groups, int max_rows, int d, int f) { return max_rows <= kI8FewRows && (long long)groups * (((d < f ? d : f) + 255) / 256) < 192; }
 // One product of codes, where one work-group of 64 rows x 32 columns for each compute unit is enough: they share K among their waves, which tiles of 256
 // columns do not.  us here / in tiles, N = 2048: 256 rows with K = 512 / 2048 / 8192 5.8 / 5.8, 8.6 / 12.2, 23.6 / 37.3, 384 rows (384 work-groups) 9.3 / 5.8,
-// 15.1 / 12.4, 44 / 38.  Up to 64 rows the weights are read once: 2048 x 6144 with 32 / 64 rows 7.2 / 9.6, in tiles 12.0.
+// 15.1 / 12.4, 44 / 38.  (A long K is far from the read of its weights either way, about 3 us with K = 8192: every work-group
+// reads all rows, and no two share a K.  Not built.)  Up to 64 rows the weights are read once: 2048 x 6144 with 32 / 64 rows 7.2 / 9.6, in tiles 12.0.
 bool i8_few_faster_alone(const I8GemmArgs& a, int epi) {
     if (epi == EPI_SCATTER) return false;
     return few_blocks(a.G, a.max_rows, a.N, 2) <= 256 || (a.G == 1 && a.max_rows <= 64 && a.N < 192 * 256);

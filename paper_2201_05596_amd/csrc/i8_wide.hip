@@ -13,7 +13,7 @@ template <int EPI> static int launch_i8_epi(const I8GemmArgs& a, const I8GemmArg
 // 2048 / 4096 53 / 43, 73 / 67, 116 / 122, 208 / 235; 8192 rows 28 / 26, 39 / 37, 61 / 66, 106 / 124; 4608 rows, 288 tiles, 25 / 17, 35 / 26, 54 / 45, 91 / 83;
 // 2560 rows 14 / 14, 20 / 20, 30 / 32, 51 / 56.  Fewer tiles leave compute units idle that tiles of 64 rows reach (4096 rows, N = 1024, k = 2048: 17 / 11).
 // Rows of groups, by their room: 32 experts of up to 256 rows, 2048 / 8192 260 / 332 for both products, 16 of up to 512 246 / 301, 64 of up to 200 rows,
-// 1024 / 4096 155 / 198; 24 of up to 400 rows, 1024 / 2048 78 / 73, as said here 68; a dense branch of 8192 tokens with 32 experts of up to 320 rows, 1024 / 4096, the layer 293 / 262.  Without
+// 1024 / 4096 155 / 198; 24 of up to 400 rows, 1024 / 2048 78 / 73, as said here 68; a dense branch of 8192 tokens with 32 experts of up to 320 rows, 1024 / 4096, the layer 293 / 262 (with results in bf16).  Without
 // a gate's order nobody knows how much of the room is filled: tiles of 256 rows that are part empty cost less, 0.85 of a round here (24 experts of 0 to 512 rows,
 // 8192 -> 2048: 174 / 195, 20 of 0 to 400, 4096 -> 2048: 87 / 103).  With a short k and 768 rows of room or more finer pieces are better
 // (8 experts of 0 to 1024, 2048 -> 8192: 117 / 97, 16 of 0 to 1000, 1024 -> 4096: 85 / 65).
